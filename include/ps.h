@@ -219,6 +219,35 @@ int32_t ps_apply(ps_ctx* ctx, ps_mode mode, float lr, float scale, const int32_t
 int32_t ps_apply_stale(ps_ctx* ctx, ps_mode mode, float lr, float scale, const int32_t* order, float clip_norm,
                        float staleness_alpha, ps_apply_result* out);
 
+/* What an AdamW update takes (decoupled weight decay: Loshchilov and Hutter, 2019).  With t the update's number, counted from 1:
+ *   g = f * gradient
+ *   m = beta1 m + (1 - beta1) g ;   v = beta2 v + (1 - beta2) g^2
+ *   p = p (1 - lr weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ * in fp32; the moments' operations are rounded one by one, the quotient is within 8 units in the last place, and the constants are made in fp64
+ * and rounded once.  f = grad_scale * min(1, clip_norm / norm), norm
+ * being that of grad_scale * gradient; clip_norm 0 = no clipping.  A gradient that is not finite makes its own element's moments and weight NaN. */
+typedef struct ps_adamw_hyper {
+  double   lr, beta1, beta2, eps;   /* finite; 0 <= beta < 1; eps >= 2^-126 (as fp32) */
+  double   grad_scale;              /* 1 = none */
+  double   clip_norm;               /* >= 0; 0 = no clipping */
+  int64_t  step;                    /* t of this update, >= 1.  0: the device counts (ps_adamw_step only) */
+  uint64_t seed;                    /* of the 8-bit second moments' stochastic rounding (ps_adamw_step only) */
+  const float* lr_dev;              /* dev; if not NULL it is read in place of lr (ps_adamw_step only) */
+  int32_t  skip_nonfinite;          /* 1: a step whose gradient norm is not finite changes nothing (ps_adamw_step only) */
+  int32_t  reserved;
+} ps_adamw_hyper;
+
+/* ps_apply with AdamW as the server's optimizer.  The gradients are taken as in ps_apply_stale, without the learning rate:
+ *   PS_SYNC / PS_REPLAY   one update with grad_scale * scale / K (or / W_tick) * sum of the queued gradients ; version + 1
+ *   PS_ASYNC              one update per gradient in order, with grad_scale * scale * g_k; update k counts as step h->step + k
+ * clip_norm and staleness_alpha act on every queued gradient by itself (clip_norm on the gradient as queued), as in ps_apply_stale.
+ * m_dev, v_dev: the moments, PS_PARAM_STRIDE floats each (dev, 16-byte aligned, read and written; zeros before the first step; their padding
+ * is written zero).  They are the caller's: ps_restore, ps_failover and ps_import_params leave them alone, and a caller who rolls the weights
+ * back decides whether to keep, restore or clear them.  Versions, checkpoints, replication, order and result are as in ps_apply.
+ * Errors: PS_ERR_DOWN, PS_ERR_BAD_ARG; nothing is changed then. */
+int32_t ps_apply_adamw(ps_ctx* ctx, ps_mode mode, const ps_adamw_hyper* h, double weight_decay, float* m_dev, float* v_dev, float scale,
+                       const int32_t* order, float staleness_alpha, ps_apply_result* out);
+
 /* The synchronous server step from the sum that workers_grad_step_summed produces: theta <- theta - lr * scale / n_workers * grad_sum; version + 1;
  * checkpoint and replication as in ps_apply(PS_SYNC), whose result it equals up to rounding when grad_sum is the sum
  * of the n_workers queued gradients.  The queue must be empty (PS_ERR_BAD_ARG).  `applied` reports n_workers. */
@@ -348,6 +377,63 @@ int32_t ps_profile_read(ps_ctx* ctx, int32_t kernel, const char** name, double* 
 int32_t ps_replay_sum_static(const float* queue_dev, int64_t K, const float* theta_in_dev,
                              float* theta_out_dev, float coef, void* stream);
 const char* ps_replay_sum_static_error(void);
+
+/* ---- operators for models of any shape (no context) ----------------------------------------------------------------------
+ * The paper's method is not tied to its CNN.  These are its two heavy parts for other models: the optimizer's step over all of a model's
+ * tensors, and the dense layer of W workers.  Types: */
+enum { PS_TYPE_FP32 = 0, PS_TYPE_BF16 = 1, PS_TYPE_FP16 = 2 };
+
+/* AdamW over many tensors at once.  A ps_adamw holds the list of a model's tensors; ps_adamw_step updates all of them with one launch (two with
+ * clip_norm, skip_nonfinite, lr_dev or step 0).  Weights, gradients, moments and copies are the caller's and must live as long as it. */
+#define PS_ADAMW_MAX_TENSORS 1048576
+#define PS_ADAMW_BLOCK 256          /* elements that share a scale (8-bit moments) */
+typedef struct ps_adamw ps_adamw;   /* opaque; owned by the library */
+
+typedef struct {
+  int64_t     n;             /* elements; 0 is allowed (nothing is read or written then) */
+  void*       param;         /* [n] param_type, read and written */
+  const void* grad;          /* [n] grad_type, read */
+  void*       copy;          /* [n] copy_type, written: the new weight rounded to nearest; NULL in every tensor = none */
+  void*       m;             /* first moments, read and written: [n] float, or [n] e4m3 codes (state_bits 8) */
+  void*       v;             /* second moments: [n] float, or [n] e5m2 codes */
+  uint8_t*    m_scale;       /* state_bits 8: [ceil(n / 256)] scales, element i stands for code[i] * 2^(scale[i / 256] - 127); a zero moment is */
+  uint8_t*    v_scale;       /*   code 0, with any scale.  Zeroed buffers are zero moments. */
+  double      weight_decay;  /* >= 0 */
+} ps_adamw_tensor;
+
+typedef struct {
+  int32_t  param_type, grad_type;   /* PS_TYPE_* */
+  int32_t  copy_type;               /* PS_TYPE_BF16 or PS_TYPE_FP16, with FP32 weights; ignored without copies */
+  int32_t  state_bits;              /* 32, or 8: blocks of 256 elements with a power-of-two scale.  The first moment is rounded to nearest even, the
+                                     * second, which must not be smaller than zero, stochastically: element i of tensor j at step t takes half word i % 8
+                                     * of Philox4x32-10 with counter (i / 8 lo, hi, j, t lo) and key (seed lo, hi), and a positive one never becomes zero.
+                                     * What is not finite becomes NaN and has no part in its block's scale.  The step itself uses the moments before
+                                     * they are rounded. */
+  void*    arena;                   /* dev, 256-byte aligned, caller-owned */
+  uint64_t arena_bytes;
+  void*    stream;                  /* cudaStream_t; all work is enqueued there */
+} ps_adamw_config;
+
+/* Size of the arena for these tensors (of which n and copy are read). */
+int32_t ps_adamw_query_bytes(const ps_adamw_config* cfg, const ps_adamw_tensor* tensors, int32_t n_tensors, uint64_t* arena_bytes);
+/* Lays the list out in the arena; synchronous.  Call it with the arena's device current.  Tensors need only their type's alignment; those that
+ * start on 32 bytes (fp32), 16 (16 bits) or 8 (codes) are read in vectors.  Errors: PS_ERR_BAD_ARG, PS_ERR_ARENA_TOO_SMALL, PS_ERR_CUDA. */
+int32_t ps_adamw_create(const ps_adamw_config* cfg, const ps_adamw_tensor* tensors, int32_t n_tensors, ps_adamw** out);
+int32_t ps_adamw_destroy(ps_adamw* opt);      /* synchronises the stream; frees host state only */
+/* Gives the following steps other gradients (host array [n_tensors] of dev pointers).  Not to be captured into a graph. */
+int32_t ps_adamw_set_grads(ps_adamw* opt, const void* const* grads);
+/* One step.  Values in *h are read at the call: a step captured into a graph repeats them, so a graph gives step 0 (the device counts its own
+ * steps, from 1, leaving out those that skip_nonfinite skips) and, for a schedule, lr_dev.  A given step does not touch that count.  One step of
+ * an optimizer at a time: its state is not shared between streams.  Errors: PS_ERR_BAD_ARG (nothing is launched then), PS_ERR_CUDA. */
+int32_t ps_adamw_step(ps_adamw* opt, const ps_adamw_hyper* h);
+
+typedef struct {
+  int64_t counted_steps;     /* steps taken with step 0 */
+  int64_t skipped_steps;
+  float   grad_norm;         /* of the last step with clip_norm or skip_nonfinite (of grad_scale * gradient) */
+  float   grad_factor;       /* f of the last step that was not skipped, of those with clip_norm, skip_nonfinite, lr_dev or step 0 */
+} ps_adamw_info;
+int32_t ps_adamw_read_info(ps_adamw* opt, ps_adamw_info* out);      /* synchronises the stream */
 
 const char* ps_last_error(ps_ctx* ctx);
 

@@ -1,0 +1,584 @@
+// One AdamW step over many tensors at once (ps_adamw_* in include/ps.h): every tensor is cut into pieces of PIECE elements, and one
+// launch covers the pieces of all of them, whatever their sizes.
+//
+// Bytes per element: weight, gradient, copy and the moments, each read or written once: 28 with everything in fp32, 16 with a bf16
+// gradient and copy and moments in 8 bits.  Nothing is computed twice and nothing is reused, so HBM is the bound; a thread takes eight
+// consecutive elements with one load of 32 (fp32), 16 or 8 bytes per array, and enough CTAs are resident to keep the memory busy.
+// Clipping by global norm needs the norm before the first update: it reads the gradients once more, in a kernel of its own.
+//
+// Moments in 8 bits: blocks of 256 elements (one warp: eight elements a lane) with a power-of-two scale each, so that scaling rounds
+// nothing.  The first moment is held in e4m3, rounded to nearest even.  The second is held in e5m2 (its square needs the range) and
+// rounded stochastically: a step changes it by 1 - b2, a thousandth, where neighbouring codes are 14 to 25 % apart, so to nearest it would
+// never fall again; with sixteen random bits (Philox, the repository's generator) it follows in the mean.  A positive second moment is never
+// rounded to zero: the next step would divide by eps alone.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <exception>
+#include <type_traits>
+#include <vector>
+
+#include "adamw.cuh"
+#include "device_common.cuh"
+#include "error.h"
+#include "kernels.h"
+#include "ps.h"
+
+namespace psk {
+
+namespace {
+
+constexpr int TPB = 256, PER = 8, PIECE = TPB * PER;      // 2,048 elements: eight blocks of 8-bit moments
+constexpr int BLOCK8 = 32 * PER;                          // elements that share a scale
+constexpr int NORM_CTAS = 148 * 8;
+constexpr int64_t MAX_ELEMENTS = (int64_t)1 << 40;
+
+struct DevTensor {
+  void* p; const void* g; void* copy; void* m; void* v;
+  uint8_t *m_scale, *v_scale;
+  int64_t n;
+  double wd;
+  int32_t wide_g, wide;      // may the gradient / all arrays be read in vectors?
+};
+
+// Where the pieces lie: piece `i` of the call is piece i - first of `tensor`.
+struct PieceRef { int32_t tensor, piece; };
+
+// Device-side state of an optimizer.
+struct DevState {
+  AdamScalars s;
+  double lr;                 // as used by the step under way
+  int64_t step;              // steps taken, where the device counts them; the step under way
+  int64_t counted;
+  int64_t skipped;
+  int32_t skip;
+  float norm;
+  uint32_t ticket;
+};
+
+struct Call {
+  AdamScalars s;             // where the host knows them all
+  AdamHyper h;
+  double grad_scale, clip;
+  const float* lr_dev;
+  int64_t step;              // 0: the device counts
+  uint64_t seed;
+  int32_t skip_nonfinite;
+};
+
+template <typename T> __device__ __forceinline__ float as_float(T x);
+template <> __device__ __forceinline__ float as_float(float x) { return x; }
+template <> __device__ __forceinline__ float as_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+template <> __device__ __forceinline__ float as_float(__half x) { return __half2float(x); }
+template <typename T> __device__ __forceinline__ T from_float(float x);
+template <> __device__ __forceinline__ float from_float(float x) { return x; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_float(float x) { return __float2bfloat16_rn(x); }
+template <> __device__ __forceinline__ __half from_float(float x) { return __float2half_rn(x); }
+
+// Eight consecutive values: 32 bytes of fp32 in one access, 16 of the narrow types, 8 of codes.  Streamed: none of it is used again.
+__device__ __forceinline__ void load8(const float* p, float (&x)[PER]) {
+  asm volatile("ld.global.L1::no_allocate.v8.f32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]), "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7]) : "l"(p));
+}
+__device__ __forceinline__ void store8(float* p, const float (&x)[PER]) {
+  asm volatile("st.global.v8.f32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+               ::"l"(p), "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7]) : "memory");
+}
+template <typename T> __device__ __forceinline__ void load8(const T* p, float (&x)[PER]) {
+  const uint4 w = __ldcs(reinterpret_cast<const uint4*>(p));
+  T t[PER];
+  memcpy(t, &w, 16);
+#pragma unroll
+  for (int i = 0; i < PER; ++i) x[i] = as_float<T>(t[i]);
+}
+template <typename T> __device__ __forceinline__ void store8(T* p, const float (&x)[PER]) {
+  T t[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) t[i] = from_float<T>(x[i]);
+  uint4 w;
+  memcpy(&w, t, 16);
+  *reinterpret_cast<uint4*>(p) = w;
+}
+// n of eight values from i0 on, the others zero / left alone
+template <typename T> __device__ __forceinline__ void load_some(const T* p, int64_t i0, int n, float (&x)[PER]) {
+#pragma unroll
+  for (int i = 0; i < PER; ++i) x[i] = i < n ? as_float<T>(p[i0 + i]) : 0.f;
+}
+template <typename T> __device__ __forceinline__ void store_some(T* p, int64_t i0, int n, const float (&x)[PER]) {
+#pragma unroll
+  for (int i = 0; i < PER; ++i)
+    if (i < n) p[i0 + i] = from_float<T>(x[i]);
+}
+
+// ---- moments in 8 bits
+__device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }            // 2^(byte - 127), byte 1 .. 254; 0: 0
+__device__ __forceinline__ float inverse_scale_of(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
+__device__ __forceinline__ void decode_e4m3(uint2 codes, float scale, float (&x)[PER]) {
+#pragma unroll
+  for (int i = 0; i < PER / 2; ++i) {
+    const uint16_t two = (uint16_t)((i < 2 ? codes.x : codes.y) >> (16 * (i & 1)));
+    uint32_t h2;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h2) : "h"(two));
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h2));
+    x[2 * i] = f.x * scale;
+    x[2 * i + 1] = f.y * scale;
+  }
+}
+__device__ __forceinline__ void decode_e5m2(uint2 codes, float scale, float (&x)[PER]) {      // a half whose low byte is zero
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const uint32_t c = ((i < 4 ? codes.x : codes.y) >> (8 * (i & 3))) & 0xFFu;
+    x[i] = __half2float(__ushort_as_half((unsigned short)(c << 8))) * scale;
+  }
+}
+__device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & 0x7F800000u) != 0x7F800000u; }
+// The scale that puts the block's largest finite value at 1.75 * 2^top at most (the types' largest values), one warp per block.
+__device__ __forceinline__ uint32_t block_scale(const float (&x)[PER], int top) {
+  uint32_t most = 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) most = max(most, finite(x[i]) ? __float_as_uint(x[i]) & 0x7FFFFFFFu : 0u);
+  most = __reduce_max_sync(0xffffffffu, most);
+  return (uint32_t)min(max((int)((most + 0x1FFFFFu) >> 23) - top, 1), 254);
+}
+__device__ __forceinline__ uint2 encode_e4m3(const float (&x)[PER], float inv) {
+  uint32_t w[2] = {0u, 0u};
+#pragma unroll
+  for (int i = 0; i < PER / 2; ++i) {
+    const float lo = finite(x[2 * i]) ? x[2 * i] * inv : __uint_as_float(0x7FFFFFFFu), hi = finite(x[2 * i + 1]) ? x[2 * i + 1] * inv : __uint_as_float(0x7FFFFFFFu);
+    uint16_t two;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(two) : "f"(hi), "f"(lo));
+    w[i >> 1] |= (uint32_t)two << (16 * (i & 1));
+  }
+  return make_uint2(w[0], w[1]);
+}
+__device__ __forceinline__ uint32_t encode_e5m2(float x, float inv, uint32_t random16) {
+  if (!finite(x)) return 0x7Fu;
+  const float u = x * inv;      // 0 .. 57,344
+  // below 2^-14 the codes are evenly spaced: adding 2^-14 brings them to the places of one binade
+  const bool low = u < 6.103515625e-05f;
+  const uint32_t bits = __float_as_uint(low ? __fadd_rn(u, 6.103515625e-05f) : u) + (random16 << 5);
+  const uint32_t c = (bits >> 21) - (low ? 113u * 4u : 112u * 4u);
+  return u > 0.f ? max(c, 1u) : c;
+}
+
+// ---- one step
+template <typename P, typename G, typename C, bool HAS_COPY, int BITS>
+__global__ void __launch_bounds__(TPB) adamw_step(const DevTensor* __restrict__ tensors, const PieceRef* __restrict__ pieces, Call call, const DevState* state) {
+  pdl_enter();
+  const PieceRef ref = pieces[blockIdx.x];
+  const DevTensor t = tensors[ref.tensor];
+  AdamScalars s = call.s;
+  double lr = call.h.lr;
+  uint32_t step = (uint32_t)call.step;
+  if (state) {
+    if (state->skip) return;
+    s = state->s;
+    lr = state->lr;
+    step = (uint32_t)state->step;
+  }
+  const float decay = adam_decay(lr, t.wd);
+  const int64_t i0 = (int64_t)ref.piece * PIECE + threadIdx.x * PER;
+  const int n = (int)min((int64_t)PER, max((int64_t)0, t.n - i0));
+  const bool vec = t.wide && n == PER;
+  if (BITS == 32 && n == 0) return;
+  float p[PER], g[PER], m[PER], v[PER];
+  uint32_t sm = 0, sv = 0;
+  const int64_t block = i0 / BLOCK8;
+  const bool in_block = block * BLOCK8 < t.n;      // the same for a warp
+  if (BITS == 8 && !in_block) return;
+  if (vec) {
+    load8(reinterpret_cast<const P*>(t.p) + i0, p);
+    load8(reinterpret_cast<const G*>(t.g) + i0, g);
+  } else {
+    load_some(reinterpret_cast<const P*>(t.p), i0, n, p);
+    load_some(reinterpret_cast<const G*>(t.g), i0, n, g);
+  }
+  if constexpr (BITS == 32) {
+    if (vec) {
+      load8(reinterpret_cast<const float*>(t.m) + i0, m);
+      load8(reinterpret_cast<const float*>(t.v) + i0, v);
+    } else {
+      load_some(reinterpret_cast<const float*>(t.m), i0, n, m);
+      load_some(reinterpret_cast<const float*>(t.v), i0, n, v);
+    }
+  } else {
+    uint2 cm = make_uint2(0u, 0u), cv = cm;
+    const uint8_t *pm = reinterpret_cast<const uint8_t*>(t.m) + i0, *pv = reinterpret_cast<const uint8_t*>(t.v) + i0;
+    if (vec) {
+      cm = __ldcs(reinterpret_cast<const uint2*>(pm));
+      cv = __ldcs(reinterpret_cast<const uint2*>(pv));
+    } else {
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+        if (i < n) {
+          (i < 4 ? cm.x : cm.y) |= (uint32_t)pm[i] << (8 * (i & 3));
+          (i < 4 ? cv.x : cv.y) |= (uint32_t)pv[i] << (8 * (i & 3));
+        }
+    }
+    decode_e4m3(cm, scale_of(t.m_scale[block]), m);
+    decode_e5m2(cv, scale_of(t.v_scale[block]), v);
+  }
+#pragma unroll
+  for (int i = 0; i < PER; ++i) adam_update(p[i], __fmul_rn(g[i], s.factor), m[i], v[i], s, decay);
+  if (vec) store8(reinterpret_cast<P*>(t.p) + i0, p);
+  else store_some(reinterpret_cast<P*>(t.p), i0, n, p);
+  if constexpr (HAS_COPY) {
+    if (vec) store8(reinterpret_cast<C*>(t.copy) + i0, p);
+    else store_some(reinterpret_cast<C*>(t.copy), i0, n, p);
+  }
+  if constexpr (BITS == 32) {
+    if (vec) {
+      store8(reinterpret_cast<float*>(t.m) + i0, m);
+      store8(reinterpret_cast<float*>(t.v) + i0, v);
+    } else {
+      store_some(reinterpret_cast<float*>(t.m), i0, n, m);
+      store_some(reinterpret_cast<float*>(t.v), i0, n, v);
+    }
+  } else {
+    // lanes past the tensor's end hold zero moments: they had zero gradients and moments
+    sm = block_scale(m, 8);
+    sv = block_scale(v, 15);
+    const uint64_t j = (uint64_t)(i0 / PER);
+    const uint4 r = philox4x32_10(make_uint4((uint32_t)j, (uint32_t)(j >> 32), (uint32_t)ref.tensor, step),
+                                  make_uint2((uint32_t)call.seed, (uint32_t)(call.seed >> 32)));
+    const uint32_t words[4] = {r.x, r.y, r.z, r.w};
+    const uint2 cm = encode_e4m3(m, inverse_scale_of(sm));
+    const float inv = inverse_scale_of(sv);
+    uint32_t cv[2] = {0u, 0u};
+#pragma unroll
+    for (int i = 0; i < PER; ++i) cv[i >> 2] |= encode_e5m2(v[i], inv, (words[i >> 1] >> (16 * (i & 1))) & 0xFFFFu) << (8 * (i & 3));
+    uint8_t *pm = reinterpret_cast<uint8_t*>(t.m) + i0, *pv = reinterpret_cast<uint8_t*>(t.v) + i0;
+    if (vec) {
+      *reinterpret_cast<uint2*>(pm) = cm;
+      *reinterpret_cast<uint2*>(pv) = make_uint2(cv[0], cv[1]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+        if (i < n) {
+          pm[i] = (uint8_t)((i < 4 ? cm.x : cm.y) >> (8 * (i & 3)));
+          pv[i] = (uint8_t)(cv[i >> 2] >> (8 * (i & 3)));
+        }
+    }
+    if ((threadIdx.x & 31) == 0) {
+      t.m_scale[block] = (uint8_t)sm;
+      t.v_scale[block] = (uint8_t)sv;
+    }
+  }
+}
+
+// What the device has to find out before the step: the norm, and the constants of a step that it counts itself.
+__device__ void finish_state(double total, bool has_norm, const Call& call, DevState* st) {
+  double factor = call.grad_scale;
+  bool skip = false;
+  if (has_norm) {
+    const double norm = fabs(call.grad_scale) * sqrt(total);
+    st->norm = (float)norm;
+    skip = call.skip_nonfinite && !isfinite(norm);
+    if (call.clip > 0.0) factor *= fmin(1.0, call.clip / norm);      // a zero gradient keeps its factor (clip / 0 = inf)
+  }
+  st->skip = skip ? 1 : 0;
+  if (skip) { st->skipped += 1; return; }
+  if (call.step == 0) st->counted += 1;
+  st->step = call.step == 0 ? st->counted : call.step;
+  AdamHyper h = call.h;
+  if (call.lr_dev) h.lr = (double)*call.lr_dev;
+  st->lr = h.lr;
+  st->s = adam_scalars(h, st->step, factor);
+}
+
+__global__ void adamw_begin(Call call, DevState* st) {
+  pdl_enter();
+  finish_state(0.0, false, call, st);
+}
+
+// The sum of all gradients' squares in fp64 (squares of fp32 values are exact in it), in an order that depends on the sizes alone; the CTA
+// that finishes last adds the CTAs' sums in their order and makes the step's constants.
+template <typename G>
+__global__ void __launch_bounds__(TPB) adamw_norm(const DevTensor* __restrict__ tensors, const PieceRef* __restrict__ pieces, int64_t n_pieces, Call call,
+                                                  double* partial, DevState* st) {
+  __shared__ double warp_sum[TPB / 32];
+  __shared__ bool last;
+  pdl_enter();
+  double acc[2] = {0.0, 0.0};
+  for (int64_t c = blockIdx.x; c < n_pieces; c += gridDim.x) {
+    const PieceRef ref = pieces[c];
+    const DevTensor& t = tensors[ref.tensor];
+    const int64_t i0 = (int64_t)ref.piece * PIECE + threadIdx.x * PER;
+    const int n = (int)min((int64_t)PER, max((int64_t)0, t.n - i0));
+    float g[PER];
+    if (t.wide_g && n == PER) load8(reinterpret_cast<const G*>(t.g) + i0, g);
+    else load_some(reinterpret_cast<const G*>(t.g), i0, n, g);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) acc[i & 1] = fma((double)g[i], (double)g[i], acc[i & 1]);
+  }
+  auto cta_sum = [&](double x) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) warp_sum[threadIdx.x >> 5] = x;
+    __syncthreads();
+    double r = 0.0;
+#pragma unroll
+    for (int w = 0; w < TPB / 32; ++w) r += warp_sum[w];
+    return r;
+  };
+  const double mine = cta_sum(acc[0] + acc[1]);
+  if (threadIdx.x == 0) {
+    partial[blockIdx.x] = mine;
+    __threadfence();
+    last = atomicAdd(&st->ticket, 1u) == gridDim.x - 1;
+  }
+  __syncthreads();
+  if (!last) return;
+  __threadfence();
+  double x = 0.0;
+  for (int i = threadIdx.x; i < (int)gridDim.x; i += TPB) x += __ldcg(partial + i);
+  const double total = cta_sum(x);
+  if (threadIdx.x == 0) {
+    st->ticket = 0;
+    finish_state(total, true, call, st);
+  }
+}
+
+uint64_t align256(uint64_t v) { return (v + 255) / 256 * 256; }
+size_t type_size(int32_t t) { return t == PS_TYPE_FP32 ? 4 : 2; }
+bool known_type(int32_t t) { return t == PS_TYPE_FP32 || t == PS_TYPE_BF16 || t == PS_TYPE_FP16; }
+// eight values of `size` bytes in one access (32, 16 or 8 bytes)
+bool wide_ok(const void* p, size_t size) { return ((uintptr_t)p & (size * PER - 1)) == 0; }
+
+}  // namespace
+
+}  // namespace psk
+
+struct ps_adamw {
+  ps_adamw_config cfg;
+  cudaStream_t st;
+  int device = 0;
+  bool copies = false;
+  int64_t n_pieces = 0;
+  std::vector<psk::DevTensor> host;
+  psk::DevTensor* tensors;
+  psk::PieceRef* pieces;
+  double* partial;
+  psk::DevState* state;
+};
+
+namespace psk {
+namespace {
+
+bool has_copies(const ps_adamw_tensor* t, int32_t n) {      // as the first tensor with anything in it
+  for (int32_t i = 0; i < n; ++i)
+    if (t[i].n > 0) return t[i].copy != nullptr;
+  return false;
+}
+
+int32_t check(const ps_adamw_config* c, const ps_adamw_tensor* t, int32_t n, bool pointers, int64_t* pieces_out) {
+  if (!c || !t) return fail(PS_ERR_BAD_ARG, "NULL argument");
+  if (n < 1 || n > PS_ADAMW_MAX_TENSORS) return fail(PS_ERR_BAD_ARG, "n_tensors must be 1..%d", PS_ADAMW_MAX_TENSORS);
+  if (!known_type(c->param_type) || !known_type(c->grad_type)) return fail(PS_ERR_BAD_ARG, "unknown param_type or grad_type");
+  if (c->state_bits != 32 && c->state_bits != 8) return fail(PS_ERR_BAD_ARG, "state_bits must be 32 or 8");
+  const bool copies = has_copies(t, n);
+  if (copies && (c->param_type != PS_TYPE_FP32 || (c->copy_type != PS_TYPE_BF16 && c->copy_type != PS_TYPE_FP16)))
+    return fail(PS_ERR_BAD_ARG, "copies are BF16 or FP16, of FP32 weights");
+  int64_t pieces = 0;
+  for (int32_t i = 0; i < n; ++i) {
+    if (t[i].n < 0 || t[i].n > MAX_ELEMENTS) return fail(PS_ERR_BAD_ARG, "tensor %d has %lld elements", i, (long long)t[i].n);
+    if (!(t[i].weight_decay >= 0.0) || !std::isfinite(t[i].weight_decay)) return fail(PS_ERR_BAD_ARG, "weight_decay of tensor %d must be >= 0", i);
+    pieces += (t[i].n + PIECE - 1) / PIECE;
+    if (!pointers || t[i].n == 0) continue;
+    if (!t[i].param || !t[i].grad || !t[i].m || !t[i].v) return fail(PS_ERR_BAD_ARG, "tensor %d lacks a buffer", i);
+    if (c->state_bits == 8 && (!t[i].m_scale || !t[i].v_scale)) return fail(PS_ERR_BAD_ARG, "tensor %d lacks its scales", i);
+    if ((t[i].copy != nullptr) != copies) return fail(PS_ERR_BAD_ARG, "either every tensor has a copy or none");
+    const size_t state = c->state_bits == 32 ? 4 : 1;
+    if ((uintptr_t)t[i].param % type_size(c->param_type) || (uintptr_t)t[i].grad % type_size(c->grad_type) || (uintptr_t)t[i].m % state ||
+        (uintptr_t)t[i].v % state || (copies && (uintptr_t)t[i].copy % 2))
+      return fail(PS_ERR_BAD_ARG, "a buffer of tensor %d is not aligned to its type", i);
+  }
+  if (pieces > 0x7FFFFFFFll) return fail(PS_ERR_BAD_ARG, "too many elements");
+  *pieces_out = pieces;
+  return PS_OK;
+}
+
+uint64_t arena_layout(ps_adamw* o, void* base, int32_t n, int64_t pieces) {
+  uint64_t at = 0;
+  auto take = [&](uint64_t bytes) { const uint64_t a = (uint64_t)base + at; at = align256(at + bytes); return a; };
+  const uint64_t a = take(sizeof(DevTensor) * (uint64_t)n), b = take(sizeof(PieceRef) * (uint64_t)pieces), c = take(sizeof(double) * NORM_CTAS), d = take(sizeof(DevState));
+  if (o) {
+    o->tensors = (DevTensor*)a; o->pieces = (PieceRef*)b; o->partial = (double*)c; o->state = (DevState*)d;
+  }
+  return at;
+}
+
+void set_wide(const ps_adamw_config& c, DevTensor& t) {
+  const size_t state = c.state_bits == 32 ? 4 : 1;
+  t.wide_g = wide_ok(t.g, type_size(c.grad_type)) ? 1 : 0;
+  t.wide = t.wide_g && wide_ok(t.p, type_size(c.param_type)) && wide_ok(t.m, state) && wide_ok(t.v, state) && (!t.copy || wide_ok(t.copy, 2));
+}
+
+int32_t upload_tensors(ps_adamw* o) {      // the copy's source is pageable: it has been read when the call returns
+  const cudaError_t e = cudaMemcpyAsync(o->tensors, o->host.data(), o->host.size() * sizeof(DevTensor), cudaMemcpyHostToDevice, o->st);
+  return e == cudaSuccess ? PS_OK : fail(PS_ERR_CUDA, "table upload: %s", cudaGetErrorString(e));
+}
+
+template <typename P, typename G, typename C, bool HAS_COPY>
+void launch_step(const ps_adamw* o, const Call& call, const DevState* state) {
+  const dim3 grid((unsigned)o->n_pieces);
+  if (o->cfg.state_bits == 32) launch_pdl(adamw_step<P, G, C, HAS_COPY, 32>, grid, TPB, 0, o->st, o->tensors, o->pieces, call, state);
+  else launch_pdl(adamw_step<P, G, C, HAS_COPY, 8>, grid, TPB, 0, o->st, o->tensors, o->pieces, call, state);
+}
+template <typename P, typename G>
+void launch_copy(const ps_adamw* o, const Call& call, const DevState* state) {
+  if constexpr (std::is_same<P, float>::value) {
+    if (o->copies && o->cfg.copy_type == PS_TYPE_BF16) return launch_step<P, G, __nv_bfloat16, true>(o, call, state);
+    if (o->copies) return launch_step<P, G, __half, true>(o, call, state);
+  }
+  launch_step<P, G, float, false>(o, call, state);
+}
+template <typename P>
+void launch_grad(const ps_adamw* o, const Call& call, const DevState* state) {
+  if (o->cfg.grad_type == PS_TYPE_FP32) launch_copy<P, float>(o, call, state);
+  else if (o->cfg.grad_type == PS_TYPE_BF16) launch_copy<P, __nv_bfloat16>(o, call, state);
+  else launch_copy<P, __half>(o, call, state);
+}
+template <typename G>
+void launch_norm(const ps_adamw* o, const Call& call) {
+  launch_pdl(adamw_norm<G>, dim3((unsigned)std::min<int64_t>(o->n_pieces, NORM_CTAS)), TPB, 0, o->st, o->tensors, o->pieces, o->n_pieces, call, o->partial, o->state);
+}
+
+}  // namespace
+
+int32_t check_adamw_hyper(const ps_adamw_hyper* h) {
+  if (!h) return fail(PS_ERR_BAD_ARG, "hyper is NULL");
+  if (!std::isfinite(h->lr)) return fail(PS_ERR_BAD_ARG, "lr must be finite");
+  if (!(h->beta1 >= 0.0 && h->beta1 < 1.0) || !(h->beta2 >= 0.0 && h->beta2 < 1.0)) return fail(PS_ERR_BAD_ARG, "beta1 and beta2 must be in [0, 1)");
+  if (!((float)h->eps >= 1.17549435e-38f) || !std::isfinite((float)h->eps)) return fail(PS_ERR_BAD_ARG, "eps must be a normal positive fp32 value");
+  if (!(h->clip_norm >= 0.0)) return fail(PS_ERR_BAD_ARG, "clip_norm must be >= 0");
+  if (h->step < 0) return fail(PS_ERR_BAD_ARG, "step must be >= 0");
+  return PS_OK;
+}
+
+}  // namespace psk
+
+using namespace psk;
+
+extern "C" {
+
+int32_t ps_adamw_query_bytes(const ps_adamw_config* cfg, const ps_adamw_tensor* tensors, int32_t n_tensors, uint64_t* arena_bytes) {
+  int64_t pieces = 0;
+  int32_t rc = check(cfg, tensors, n_tensors, false, &pieces);
+  if (rc != PS_OK) return rc;
+  if (!arena_bytes) return fail(PS_ERR_BAD_ARG, "NULL argument");
+  *arena_bytes = arena_layout(nullptr, nullptr, n_tensors, pieces);
+  return PS_OK;
+}
+
+int32_t ps_adamw_create(const ps_adamw_config* cfg, const ps_adamw_tensor* tensors, int32_t n_tensors, ps_adamw** out) {
+  int64_t n_pieces = 0;
+  int32_t rc = check(cfg, tensors, n_tensors, true, &n_pieces);
+  if (rc != PS_OK) return rc;
+  if (!out) return fail(PS_ERR_BAD_ARG, "NULL argument");
+  if (!cfg->arena || ((uint64_t)cfg->arena & 255) != 0) return fail(PS_ERR_BAD_ARG, "arena must be a 256-byte aligned device pointer");
+  const uint64_t need = arena_layout(nullptr, nullptr, n_tensors, n_pieces);
+  if (cfg->arena_bytes < need) return fail(PS_ERR_ARENA_TOO_SMALL, "arena has %llu bytes, %llu needed", (unsigned long long)cfg->arena_bytes, (unsigned long long)need);
+  ps_adamw* o = nullptr;
+  std::vector<PieceRef> pieces;
+  try {
+    o = new ps_adamw();
+    o->host.resize((size_t)n_tensors);
+    pieces.reserve((size_t)n_pieces);
+  } catch (const std::exception&) {
+    delete o;
+    return fail(PS_ERR_BAD_ARG, "out of host memory");
+  }
+  o->cfg = *cfg;
+  o->st = (cudaStream_t)cfg->stream;
+  o->copies = has_copies(tensors, n_tensors);
+  o->n_pieces = n_pieces;
+  arena_layout(o, cfg->arena, n_tensors, n_pieces);
+  for (int32_t i = 0; i < n_tensors; ++i) {
+    const ps_adamw_tensor& t = tensors[i];
+    DevTensor& d = o->host[(size_t)i];
+    d.p = t.param; d.g = t.grad; d.copy = t.copy; d.m = t.m; d.v = t.v; d.m_scale = t.m_scale; d.v_scale = t.v_scale;
+    d.n = t.n; d.wd = t.weight_decay;
+    set_wide(o->cfg, d);
+    for (int64_t c = 0; c * PIECE < t.n; ++c) pieces.push_back(PieceRef{i, (int32_t)c});
+  }
+  cudaError_t e = cudaGetDevice(&o->device);
+  rc = PS_OK;
+  if (e == cudaSuccess) rc = upload_tensors(o);
+  if (rc == PS_OK && e == cudaSuccess && n_pieces) e = cudaMemcpyAsync(o->pieces, pieces.data(), pieces.size() * sizeof(PieceRef), cudaMemcpyHostToDevice, o->st);
+  if (rc == PS_OK && e == cudaSuccess) e = cudaMemsetAsync(o->state, 0, sizeof(DevState), o->st);
+  if (rc == PS_OK && e == cudaSuccess) e = cudaStreamSynchronize(o->st);
+  if (rc != PS_OK || e != cudaSuccess) {
+    delete o;
+    return rc != PS_OK ? rc : fail(PS_ERR_CUDA, "ps_adamw_create: %s", cudaGetErrorString(e));
+  }
+  *out = o;
+  return PS_OK;
+}
+
+int32_t ps_adamw_destroy(ps_adamw* o) {
+  if (!o) return fail(PS_ERR_BAD_ARG, "optimizer is NULL");
+  const cudaError_t e = cudaStreamSynchronize(o->st);
+  delete o;
+  return e == cudaSuccess ? PS_OK : fail(PS_ERR_CUDA, "ps_adamw_destroy: %s", cudaGetErrorString(e));
+}
+
+int32_t ps_adamw_set_grads(ps_adamw* o, const void* const* grads) {
+  if (!o || !grads) return fail(PS_ERR_BAD_ARG, "NULL argument");
+  const size_t size = type_size(o->cfg.grad_type);
+  for (size_t i = 0; i < o->host.size(); ++i)
+    if (o->host[i].n > 0 && (!grads[i] || (uintptr_t)grads[i] % size)) return fail(PS_ERR_BAD_ARG, "gradient %zu is NULL or not aligned to its type", i);
+  for (size_t i = 0; i < o->host.size(); ++i) {
+    o->host[i].g = grads[i];
+    set_wide(o->cfg, o->host[i]);
+  }
+  return upload_tensors(o);
+}
+
+int32_t ps_adamw_step(ps_adamw* o, const ps_adamw_hyper* h) {
+  if (!o) return fail(PS_ERR_BAD_ARG, "optimizer is NULL");
+  int32_t rc = check_adamw_hyper(h);
+  if (rc != PS_OK) return rc;
+  if (!std::isfinite(h->grad_scale)) return fail(PS_ERR_BAD_ARG, "grad_scale must be finite");
+  int device = -1;
+  if (cudaGetDevice(&device) != cudaSuccess || device != o->device) return fail(PS_ERR_BAD_ARG, "the optimizer lives on device %d, the current one is %d", o->device, device);
+  if (o->n_pieces == 0) return PS_OK;
+  Call c;
+  c.h = AdamHyper{h->lr, h->beta1, h->beta2, h->eps};
+  c.grad_scale = h->grad_scale; c.clip = h->clip_norm; c.lr_dev = h->lr_dev; c.step = h->step; c.seed = h->seed;
+  c.skip_nonfinite = h->skip_nonfinite;
+  const bool norm = h->clip_norm > 0.0 || h->skip_nonfinite, on_device = norm || h->step == 0 || h->lr_dev;
+  c.s = on_device ? AdamScalars{} : adam_scalars(c.h, h->step, h->grad_scale);
+  if (norm) {
+    if (o->cfg.grad_type == PS_TYPE_FP32) launch_norm<float>(o, c);
+    else if (o->cfg.grad_type == PS_TYPE_BF16) launch_norm<__nv_bfloat16>(o, c);
+    else launch_norm<__half>(o, c);
+  } else if (on_device) {
+    launch_pdl(adamw_begin, dim3(1), 1, 0, o->st, c, o->state);
+  }
+  const DevState* state = on_device ? o->state : nullptr;
+  if (o->cfg.param_type == PS_TYPE_FP32) launch_grad<float>(o, c, state);
+  else if (o->cfg.param_type == PS_TYPE_BF16) launch_grad<__nv_bfloat16>(o, c, state);
+  else launch_grad<__half>(o, c, state);
+  const cudaError_t e = cudaGetLastError();
+  return e == cudaSuccess ? PS_OK : fail(PS_ERR_CUDA, "adamw launch: %s", cudaGetErrorString(e));
+}
+
+int32_t ps_adamw_read_info(ps_adamw* o, ps_adamw_info* out) {
+  if (!o || !out) return fail(PS_ERR_BAD_ARG, "NULL argument");
+  DevState s;
+  cudaError_t e = cudaMemcpyAsync(&s, o->state, sizeof(s), cudaMemcpyDeviceToHost, o->st);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(o->st);
+  if (e != cudaSuccess) return fail(PS_ERR_CUDA, "ps_adamw_read_info: %s", cudaGetErrorString(e));
+  out->counted_steps = s.counted;
+  out->skipped_steps = s.skipped;
+  out->grad_norm = s.norm;
+  out->grad_factor = s.s.factor;
+  return PS_OK;
+}
+
+}  // extern "C"

@@ -47,6 +47,36 @@ __device__ __forceinline__ float2 compensated(u64 acc, u64 err) {
   return make_float2(isfinite(e0) ? a0 + e0 : a0, isfinite(e1) ? a1 + e1 : a1);
 }
 
+// What becomes of a column's sum s of gradients (and the factor c that they share): t - c s, or AdamW of c s.
+struct Sgd {
+  __device__ __forceinline__ float4 operator()(int, float4 t, float c, const float4& s) const {
+    t.x = fmaf(-c, s.x, t.x); t.y = fmaf(-c, s.y, t.y);
+    t.z = fmaf(-c, s.z, t.z); t.w = fmaf(-c, s.w, t.w);
+    return t;
+  }
+};
+constexpr int FIRST_PADDED = P / 4;      // the column with the vector's end in it; it and those behind hold padding
+__device__ __forceinline__ float4 without_padding(int col, float4 v) {
+  if (col >= FIRST_PADDED) {
+    v.x = 4 * col < P ? v.x : 0.f; v.y = 4 * col + 1 < P ? v.y : 0.f;
+    v.z = 4 * col + 2 < P ? v.z : 0.f; v.w = 4 * col + 3 < P ? v.w : 0.f;
+  }
+  return v;
+}
+struct AdamW {
+  AdamColumns a;
+  __device__ __forceinline__ float4 operator()(int col, float4 t, float c, const float4& s) const {
+    float4 m = reinterpret_cast<const float4*>(a.m)[col], v = reinterpret_cast<const float4*>(a.v)[col];
+    adam_update(t.x, __fmul_rn(c, s.x), m.x, v.x, a.s, a.decay);
+    adam_update(t.y, __fmul_rn(c, s.y), m.y, v.y, a.s, a.decay);
+    adam_update(t.z, __fmul_rn(c, s.z), m.z, v.z, a.s, a.decay);
+    adam_update(t.w, __fmul_rn(c, s.w), m.w, v.w, a.s, a.decay);
+    reinterpret_cast<float4*>(a.m)[col] = without_padding(col, m);
+    reinterpret_cast<float4*>(a.v)[col] = without_padding(col, v);
+    return without_padding(col, t);
+  }
+};
+
 // Sum of slots [k0, k1) of one float4 column, in a fixed order: eight interleaved running sums
 // (slot k goes to sum k mod 8 relative to k0), combined pairwise at the end.  With WEIGHTED every slot is
 // multiplied by its own factor coef_k[k] (the stale-gradient treatments) as it is added.
@@ -80,10 +110,10 @@ __device__ __forceinline__ float4 column_sum(const float4* __restrict__ q, int64
 }
 
 // theta_out = theta_in - coef * sum_k g_k (or - sum_k coef_k[k] g_k), whole queue in one pass (small K).
-template <bool WEIGHTED>
+template <bool WEIGHTED, class Update>
 __global__ void __launch_bounds__(TPB) sum_apply_direct(const float4* __restrict__ queue, int64_t K,
                                                         const float4* theta_in, float4* theta_out,
-                                                        float4* __restrict__ replica, float coef, const float* __restrict__ coef_k) {
+                                                        float4* __restrict__ replica, float coef, const float* __restrict__ coef_k, Update update) {
   // theta_in and theta_out may be the same buffer (a ring of depth one): each thread reads its column before it
   // writes it, and the two pointers carry no no-alias promise
   int col = blockIdx.x * TPB + threadIdx.x;
@@ -91,8 +121,7 @@ __global__ void __launch_bounds__(TPB) sum_apply_direct(const float4* __restrict
   pdl_enter();
   float4 s = column_sum<WEIGHTED>(queue + col, 0, K, coef_k);
   float4 t = theta_in[col];
-  t.x = fmaf(-coef, s.x, t.x); t.y = fmaf(-coef, s.y, t.y);
-  t.z = fmaf(-coef, s.z, t.z); t.w = fmaf(-coef, s.w, t.w);
+  t = update(col, t, coef, s);
   theta_out[col] = t;
   if (replica) replica[col] = t;
 }
@@ -112,17 +141,17 @@ __global__ void __launch_bounds__(TPB) sum_partial(const float4* __restrict__ qu
 }
 
 // Stage 2: sums the partials in slot order and applies the update.
+template <class Update>
 __global__ void __launch_bounds__(TPB) sum_finish(const float4* __restrict__ partial, int n_split,
                                                   const float4* theta_in, float4* theta_out,   // may alias (see above)
-                                                  float4* __restrict__ replica, float coef) {
+                                                  float4* __restrict__ replica, float coef, Update update) {
   int col = blockIdx.x * TPB + threadIdx.x;
   if (col >= P_VEC4) return;
   pdl_enter();
   float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int i = 0; i < n_split; ++i) add4(s, partial[(int64_t)i * P_VEC4 + col]);
   float4 t = theta_in[col];
-  t.x = fmaf(-coef, s.x, t.x); t.y = fmaf(-coef, s.y, t.y);
-  t.z = fmaf(-coef, s.z, t.z); t.w = fmaf(-coef, s.w, t.w);
+  t = update(col, t, coef, s);
   theta_out[col] = t;
   if (replica) replica[col] = t;
 }
@@ -158,6 +187,45 @@ __global__ void __launch_bounds__(TPB) async_apply(AsyncApplyArgs a, AsyncOrder 
       }
     }
   }
+}
+
+// The same with AdamW: the moments stay in registers as well, and every update has its own constants.
+__global__ void __launch_bounds__(TPB) async_adamw(const __grid_constant__ AsyncApplyArgs a, const __grid_constant__ AsyncOrder ord, const __grid_constant__ AsyncAdam adam) {
+  int col = blockIdx.x * TPB + threadIdx.x;
+  if (col >= P_VEC4) return;
+  pdl_enter();
+  const float4* q = reinterpret_cast<const float4*>(a.queue) + col;
+  float4 t = reinterpret_cast<const float4*>(a.theta_in)[col];
+  float4 m = reinterpret_cast<const float4*>(adam.col.m)[col], v = reinterpret_cast<const float4*>(adam.col.v)[col];
+  AdamScalars s = adam.col.s;
+  constexpr int U = 8;
+  for (int k0 = 0; k0 < a.K; k0 += U) {
+    float4 g[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (k0 + u < a.K) g[u] = ld_stream(q + (int64_t)ord.slot[k0 + u] * P_VEC4);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      int k = k0 + u;
+      if (k < a.K) {
+        const float c = a.coef_k ? a.coef_k[ord.slot[k]] : a.coef;
+        s.step_size = adam.step_size[k];
+        s.rs2 = adam.rs2[k];
+        adam_update(t.x, __fmul_rn(c, g[u].x), m.x, v.x, s, adam.col.decay);
+        adam_update(t.y, __fmul_rn(c, g[u].y), m.y, v.y, s, adam.col.decay);
+        adam_update(t.z, __fmul_rn(c, g[u].z), m.z, v.z, s, adam.col.decay);
+        adam_update(t.w, __fmul_rn(c, g[u].w), m.w, v.w, s, adam.col.decay);
+        if (k >= a.first_stored) {
+          int slot = (int)((a.v0 + (uint64_t)k + 1) % (uint64_t)a.ring_depth);
+          reinterpret_cast<float4*>(a.ring[slot])[col] = without_padding(col, t);
+        }
+        for (int i = 0; i < a.n_mirror; ++i)
+          if (k == a.mirror_k[i]) reinterpret_cast<float4*>(a.replica[i])[col] = without_padding(col, t);
+      }
+    }
+  }
+  reinterpret_cast<float4*>(adam.col.m)[col] = without_padding(col, m);
+  reinterpret_cast<float4*>(adam.col.v)[col] = without_padding(col, v);
 }
 
 // Copies rows of P_PAD floats; used for the copying form of enqueue.
@@ -250,9 +318,10 @@ static_assert(sizeof(ClipShared) <= CS_MISC, "shared memory");
 // Sixteen or more runs, so that what their own roundings add stays below the last one's; longer ones than 32 save no time.
 inline int clip_fold(int64_t K) { return (int)(K / 16 < 1 ? 1 : (K / 16 > 32 ? 32 : K / 16)); }
 
+template <class Update>
 __global__ void __launch_bounds__(CS_THREADS, 1) clip_sum_apply(const float4* __restrict__ queue, int K, int cols, int slots, int fold, float clip,
                                                                 const float* __restrict__ coef_k, u64* words, const float4* theta_in,
-                                                                float4* theta_out, float4* __restrict__ replica, uint32_t* status) {
+                                                                float4* theta_out, float4* __restrict__ replica, uint32_t* status, Update update) {
   extern __shared__ __align__(128) uint8_t sm[];
   ClipShared* sh = reinterpret_cast<ClipShared*>(sm);
   float4* ring = reinterpret_cast<float4*>(sm + CS_MISC);
@@ -315,7 +384,7 @@ __global__ void __launch_bounds__(CS_THREADS, 1) clip_sum_apply(const float4* __
         if (i < n) {
           float4 t = theta_in[col0 + i];
           const float2 lo = compensated(acc[2 * j], err[2 * j]), hi = compensated(acc[2 * j + 1], err[2 * j + 1]);
-          t.x -= lo.x; t.y -= lo.y; t.z -= hi.x; t.w -= hi.y;
+          t = update(col0 + i, t, 1.0f, make_float4(lo.x, lo.y, hi.x, hi.y));
           theta_out[col0 + i] = t;
           if (replica) replica[col0 + i] = t;
         }
@@ -418,6 +487,25 @@ const char* kernel_name(int id) {
   return id >= 0 && id < K_COUNT ? names[id] : "?";
 }
 
+template <class Update>
+static int run_sum_apply(const SumApplyArgs& a, int n_split, const float4* q, const float4* tin, float4* tout, float4* rep, const Update& update, cudaStream_t st, Profiler* prof) {
+  int launches = 0;
+  const float* ck = a.coef_k;
+  const float coef = ck ? 1.0f : a.coef;      // the per-gradient factors already carry the step size
+  if (n_split <= 1) {
+    if (ck) TIMED(K_SUM_APPLY_DIRECT, (sum_apply_direct<true, Update><<<COL_BLOCKS, TPB, 0, st>>>(q, a.K, tin, tout, rep, coef, ck, update)));
+    else TIMED(K_SUM_APPLY_DIRECT, launch_pdl(sum_apply_direct<false, Update>, dim3(COL_BLOCKS), TPB, 0, st, q, a.K, tin, tout, rep, coef, nullptr, update));
+    launches = 1;
+  } else {
+    float4* part = reinterpret_cast<float4*>(a.partial);
+    if (ck) TIMED(K_SUM_PARTIAL, (sum_partial<true><<<dim3(COL_BLOCKS, n_split), TPB, 0, st>>>(q, a.K, n_split, part, ck)));
+    else TIMED(K_SUM_PARTIAL, launch_pdl(sum_partial<false>, dim3(COL_BLOCKS, n_split), TPB, 0, st, q, a.K, n_split, part, nullptr));
+    TIMED(K_SUM_FINISH, launch_pdl(sum_finish<Update>, dim3(COL_BLOCKS), TPB, 0, st, part, n_split, tin, tout, rep, coef, update));
+    launches = 2;
+  }
+  return cudaGetLastError() == cudaSuccess ? launches : -1;
+}
+
 int launch_sum_apply(const SumApplyArgs& a, cudaStream_t st, Profiler* prof) {
   const float4* q = reinterpret_cast<const float4*>(a.queue);
   const float4* tin = reinterpret_cast<const float4*>(a.theta_in);
@@ -428,21 +516,7 @@ int launch_sum_apply(const SumApplyArgs& a, cudaStream_t st, Profiler* prof) {
     int64_t want = (a.K + 31) / 32;
     n_split = (int)(want < a.max_split ? want : a.max_split);
   }
-  int launches = 0;
-  const float* ck = a.coef_k;
-  const float coef = ck ? 1.0f : a.coef;      // the per-gradient factors already carry the learning rate
-  if (n_split <= 1) {
-    if (ck) TIMED(K_SUM_APPLY_DIRECT, (sum_apply_direct<true><<<COL_BLOCKS, TPB, 0, st>>>(q, a.K, tin, tout, rep, coef, ck)));
-    else TIMED(K_SUM_APPLY_DIRECT, launch_pdl(sum_apply_direct<false>, dim3(COL_BLOCKS), TPB, 0, st, q, a.K, tin, tout, rep, coef, nullptr));
-    launches = 1;
-  } else {
-    float4* part = reinterpret_cast<float4*>(a.partial);
-    if (ck) TIMED(K_SUM_PARTIAL, (sum_partial<true><<<dim3(COL_BLOCKS, n_split), TPB, 0, st>>>(q, a.K, n_split, part, ck)));
-    else TIMED(K_SUM_PARTIAL, launch_pdl(sum_partial<false>, dim3(COL_BLOCKS, n_split), TPB, 0, st, q, a.K, n_split, part, nullptr));
-    TIMED(K_SUM_FINISH, launch_pdl(sum_finish, dim3(COL_BLOCKS), TPB, 0, st, part, n_split, tin, tout, rep, coef));
-    launches = 2;
-  }
-  return cudaGetLastError() == cudaSuccess ? launches : -1;
+  return a.adam.m ? run_sum_apply(a, n_split, q, tin, tout, rep, AdamW{a.adam}, st, prof) : run_sum_apply(a, n_split, q, tin, tout, rep, Sgd{}, st, prof);
 }
 
 int launch_clip_factors(const float* queue, int64_t K, float clip, float* coef_k, float* norm_part, cudaStream_t st, Profiler* prof) {
@@ -452,7 +526,7 @@ int launch_clip_factors(const float* queue, int64_t K, float clip, float* coef_k
 }
 
 int configure_apply_kernels() {
-  return allow_smem((const void*)clip_sum_apply, CS_SMEM) == cudaSuccess ? 0 : -1;
+  return allow_smem((const void*)clip_sum_apply<Sgd>, CS_SMEM) == cudaSuccess && allow_smem((const void*)clip_sum_apply<AdamW>, CS_SMEM) == cudaSuccess ? 0 : -1;
 }
 
 // The one-pass kernel's shape on a device of `sms` SMs: a CTA per SM, its columns, its ring of gradients.  A CTA's threads cover
@@ -485,9 +559,12 @@ int launch_clip_sum_apply(const SumApplyArgs& a, float clip, uint64_t* words, ui
   cfg.attrs = &at;
   cfg.numAttrs = 1;
   cudaError_t e = cudaSuccess;
-  TIMED(K_CLIP_SUM, e = cudaLaunchKernelEx(&cfg, clip_sum_apply, reinterpret_cast<const float4*>(a.queue), (int)a.K, c.cols, c.slots, clip_fold(a.K),
-                                           clip, a.coef_k, reinterpret_cast<u64*>(words), reinterpret_cast<const float4*>(a.theta_in),
-                                           reinterpret_cast<float4*>(a.theta_out), reinterpret_cast<float4*>(a.replica), status));
+  auto run = [&](auto kernel, auto update) {
+    return cudaLaunchKernelEx(&cfg, kernel, reinterpret_cast<const float4*>(a.queue), (int)a.K, c.cols, c.slots, clip_fold(a.K), clip, a.coef_k,
+                              reinterpret_cast<u64*>(words), reinterpret_cast<const float4*>(a.theta_in), reinterpret_cast<float4*>(a.theta_out),
+                              reinterpret_cast<float4*>(a.replica), status, update);
+  };
+  TIMED(K_CLIP_SUM, e = a.adam.m ? run(clip_sum_apply<AdamW>, AdamW{a.adam}) : run(clip_sum_apply<Sgd>, Sgd{}));
   if (e == cudaErrorCooperativeLaunchTooLarge) {      // a stream that may use part of the device only
     cudaGetLastError();
     return 0;
@@ -497,6 +574,11 @@ int launch_clip_sum_apply(const SumApplyArgs& a, float clip, uint64_t* words, ui
 
 int launch_async_apply(const AsyncApplyArgs& a, const AsyncOrder& ord, cudaStream_t st, Profiler* prof) {
   TIMED(K_ASYNC_APPLY, launch_pdl(async_apply, dim3(COL_BLOCKS), TPB, 0, st, a, ord));
+  return cudaGetLastError() == cudaSuccess ? 1 : -1;
+}
+
+int launch_async_adamw(const AsyncApplyArgs& a, const AsyncOrder& ord, const AsyncAdam& adam, cudaStream_t st, Profiler* prof) {
+  TIMED(K_ASYNC_APPLY, launch_pdl(async_adamw, dim3(COL_BLOCKS), TPB, 0, st, a, ord, adam));
   return cudaGetLastError() == cudaSuccess ? 1 : -1;
 }
 

@@ -5,6 +5,10 @@
 
 #include <vector>
 
+#include "adamw.cuh"
+
+struct ps_adamw_hyper;
+
 namespace psk {
 
 constexpr int P = 813258;
@@ -220,6 +224,14 @@ int launch_fc1_dw_tc5(const GradStepArgs& a, const WorkerTable& wt, const GroupT
                       cudaStream_t st, Profiler* prof);
 
 // Part B.
+// AdamW in place of the subtraction: the constants of the (first) update, and the moments [P_PAD] each, whose padding is written zero.
+struct AdamColumns {
+  AdamScalars s;
+  float decay;
+  float *m, *v;             // nullptr: SGD
+};
+int32_t check_adamw_hyper(const ps_adamw_hyper* h);      // PS_OK or the error, with its text
+
 struct SumApplyArgs {
   const float* queue;       // slot 0 of the gradient queue; slot k at queue + k*P_PAD
   int64_t K;                // gradients to sum (slots 0..K-1)
@@ -230,6 +242,7 @@ struct SumApplyArgs {
   float* partial;           // [max_split][P_PAD] scratch
   int max_split;
   const float* coef_k;      // per-gradient factors [K] that replace coef (the stale-gradient treatments), or nullptr
+  AdamColumns adam = {};    // then coef and coef_k carry no learning rate
 };
 int launch_sum_apply(const SumApplyArgs& a, cudaStream_t st, Profiler* prof);
 
@@ -250,6 +263,11 @@ struct AsyncApplyArgs {
   const float* coef_k;      // per-gradient factors indexed by queue slot that replace coef, or nullptr
 };
 int launch_async_apply(const AsyncApplyArgs& a, const AsyncOrder& ord, cudaStream_t st, Profiler* prof);
+struct AsyncAdam {
+  AdamColumns col;
+  float step_size[ASYNC_SEG], rs2[ASYNC_SEG];      // of every update
+};
+int launch_async_adamw(const AsyncApplyArgs& a, const AsyncOrder& ord, const AsyncAdam& adam, cudaStream_t st, Profiler* prof);
 
 int launch_copy_rows(float* dst, const float* src, int64_t rows, cudaStream_t st, Profiler* prof);
 

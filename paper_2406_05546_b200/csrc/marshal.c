@@ -22,6 +22,8 @@ static int32_t (*f_enqueue)(ps_ctx*, int32_t, const int64_t*, const float*, cons
 static int32_t (*f_apply)(ps_ctx*, ps_mode, float, float, const int32_t*, ps_apply_result*);
 static int32_t (*f_apply_stale)(ps_ctx*, ps_mode, float, float, const int32_t*, float, float, ps_apply_result*);
 static int32_t (*f_apply_summed)(ps_ctx*, const float*, int32_t, float, float, ps_apply_result*);
+static int32_t (*f_apply_adamw)(ps_ctx*, ps_mode, const ps_adamw_hyper*, double, float*, float*, float, const int32_t*, float, ps_apply_result*);
+static int32_t (*f_adamw_step)(ps_adamw*, const ps_adamw_hyper*);
 static const char* (*f_error)(ps_ctx*);
 static PyObject *snapshot_type, *error_type;
 static PyObject *as_array;       /* as_array(object, kind): numpy's conversion to a contiguous array */
@@ -58,6 +60,24 @@ static int as_float(PyObject* o, float* v) {       /* anything float() takes */
   if (!f) return -1;
   *v = (float)PyFloat_AS_DOUBLE(f);
   Py_DECREF(f);
+  return 0;
+}
+
+static int as_double(PyObject* o, double* v) {
+  PyObject* f = PyNumber_Float(o);
+  if (!f) return -1;
+  *v = PyFloat_AS_DOUBLE(f);
+  Py_DECREF(f);
+  return 0;
+}
+/* (lr, beta1, beta2, eps, step, clip_norm, grad_scale) from a[0] on */
+static int hyper(PyObject* const* a, ps_adamw_hyper* h) {
+  uint64_t step;
+  memset(h, 0, sizeof(*h));
+  if (as_double(a[0], &h->lr) || as_double(a[1], &h->beta1) || as_double(a[2], &h->beta2) || as_double(a[3], &h->eps) || as_u64(a[4], &step) ||
+      as_double(a[5], &h->clip_norm) || as_double(a[6], &h->grad_scale))
+    return -1;
+  h->step = (int64_t)step;
   return 0;
 }
 
@@ -138,7 +158,8 @@ static PyObject* bind(PyObject* m, PyObject* const* a, Py_ssize_t nargs) {
   static const struct { const char* name; void** f; } table[] = {
       {"ps_pull_snapshot", (void**)&f_pull}, {"ps_queue_reserve", (void**)&f_reserve}, {"workers_grad_step", (void**)&f_grad},
       {"workers_grad_step_summed", (void**)&f_summed}, {"workers_eval", (void**)&f_eval}, {"ps_enqueue", (void**)&f_enqueue},
-      {"ps_apply", (void**)&f_apply}, {"ps_apply_stale", (void**)&f_apply_stale}, {"ps_apply_summed", (void**)&f_apply_summed}, {"ps_last_error", (void**)&f_error}};
+      {"ps_apply", (void**)&f_apply}, {"ps_apply_stale", (void**)&f_apply_stale}, {"ps_apply_summed", (void**)&f_apply_summed}, {"ps_last_error", (void**)&f_error},
+      {"ps_apply_adamw", (void**)&f_apply_adamw}, {"ps_adamw_step", (void**)&f_adamw_step}};
   for (size_t i = 0; i < sizeof(table) / sizeof(table[0]); ++i) {
     PyObject* addr = PyDict_GetItemString(a[0], table[i].name);
     if (!addr) { PyErr_SetString(PyExc_KeyError, table[i].name); return NULL; }
@@ -332,9 +353,41 @@ static PyObject* apply_summed(PyObject* m, PyObject* const* a, Py_ssize_t nargs)
   return rc ? raise(rc) : result(&r);
 }
 
+/* (ctx, mode, lr, beta1, beta2, eps, step, clip_norm, grad_scale, weight_decay, m, v, scale, order int32[K] | None, staleness_alpha) -> dict */
+static PyObject* apply_adamw(PyObject* m, PyObject* const* a, Py_ssize_t nargs) {
+  WANT(15)
+  void *ctx, *pm, *pv;
+  int32_t mode;
+  ps_adamw_hyper h;
+  double decay;
+  float scale, alpha;
+  Py_buffer order;
+  ps_apply_result r = {0, 0, 0, 0};
+  if (as_ptr(a[0], &ctx) || i32(a[1], &mode) || hyper(a + 2, &h) || as_double(a[9], &decay) || as_ptr(a[10], &pm) || as_ptr(a[11], &pv) ||
+      as_float(a[12], &scale) || as_float(a[14], &alpha) || array(a[13], &order, I32))
+    return NULL;
+  int32_t rc;
+  CALL(f_apply_adamw((ps_ctx*)ctx, (ps_mode)mode, &h, decay, (float*)pm, (float*)pv, scale, (const int32_t*)order.buf, alpha, &r))
+  done(&order);
+  return rc ? raise(rc) : result(&r);
+}
+
+/* (optimizer, lr, beta1, beta2, eps, step, clip_norm, grad_scale, seed, lr_dev | None, skip_nonfinite) */
+static PyObject* adamw_step(PyObject* m, PyObject* const* a, Py_ssize_t nargs) {
+  WANT(11)
+  void *opt, *lr_dev;
+  ps_adamw_hyper h;
+  if (as_ptr(a[0], &opt) || hyper(a + 1, &h) || as_u64(a[8], &h.seed) || as_ptr(a[9], &lr_dev) || i32(a[10], &h.skip_nonfinite)) return NULL;
+  h.lr_dev = (const float*)lr_dev;
+  int32_t rc;
+  CALL(f_adamw_step((ps_adamw*)opt, &h))
+  if (rc) return raise(rc);
+  Py_RETURN_NONE;
+}
+
 #define FAST(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, NULL}
 static PyMethodDef methods[] = {FAST(bind), FAST(pull), FAST(reserve), FAST(grad_step), FAST(grad_step_summed), FAST(eval),
-                                FAST(enqueue), FAST(apply), FAST(apply_stale), FAST(apply_summed), {NULL, NULL, 0, NULL}};
+                                FAST(enqueue), FAST(apply), FAST(apply_stale), FAST(apply_summed), FAST(apply_adamw), FAST(adamw_step), {NULL, NULL, 0, NULL}};
 static struct PyModuleDef def = {PyModuleDef_HEAD_INIT, "_marshal", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
 PyMODINIT_FUNC PyInit__marshal(void) {

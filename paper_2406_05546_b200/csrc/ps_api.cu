@@ -16,6 +16,8 @@
 #include <string>
 #include <vector>
 
+#include "adamw.cuh"
+#include "error.h"
 #include "kernels.h"
 #include "ps.h"
 
@@ -48,6 +50,16 @@ struct Carver {
 };
 
 }  // namespace
+
+int32_t psk::fail(int32_t code, const char* fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof(buf), fmt, ap);
+  va_end(ap);
+  g_err = buf;
+  return code;
+}
 
 struct ps_ctx {
   ps_config cfg;
@@ -95,15 +107,7 @@ struct ps_ctx {
 
 namespace {
 
-int32_t fail(int32_t code, const char* fmt, ...) {
-  char buf[512];
-  va_list ap;
-  va_start(ap, fmt);
-  vsnprintf(buf, sizeof(buf), fmt, ap);
-  va_end(ap);
-  g_err = buf;
-  return code;
-}
+using psk::fail;
 
 int32_t cuda_fail(cudaError_t e, const char* what) {
   return fail(PS_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
@@ -587,8 +591,10 @@ int32_t ps_replicate(ps_ctx* x, uint64_t* version_out) {
 // gradient then gets a factor of its own (learning rate included), staged on the host and uploaded.  For clipping it is
 // multiplied on the device by min(1, clip_norm / ||g||): by the kernel that also sums and applies (sync and replay), or,
 // in the ordered mode and where that kernel does not fit, after a pass over the queue that takes the norms.
+// With `adam` the gradients (their sum, or one by one) go through AdamW instead of being subtracted: the factors then carry no learning rate.
+struct AdamApply { psk::AdamHyper h; double weight_decay; int64_t step; float *m, *v; };
 static int32_t apply_impl(ps_ctx* x, ps_mode mode, float lr, float scale, const int32_t* order, float clip_norm,
-                          float staleness_alpha, ps_apply_result* out) {
+                          float staleness_alpha, ps_apply_result* out, const AdamApply* adam = nullptr) {
   if (!x) return fail(PS_ERR_BAD_ARG, "ctx is NULL");
   if (!x->up || x->weights_lost) return fail(PS_ERR_DOWN, "server is down");
   if (mode != PS_SYNC && mode != PS_ASYNC && mode != PS_REPLAY) return fail(PS_ERR_BAD_ARG, "unknown mode %d", (int)mode);
@@ -613,8 +619,9 @@ static int32_t apply_impl(ps_ctx* x, ps_mode mode, float lr, float scale, const 
   if (treated) {
     // factor of the gradient in queue slot k: the step size of its mode times 1 / (1 + alpha * staleness), where the
     // staleness is the version the update is applied to minus the version the worker had read
-    const double step = mode == PS_ASYNC ? (double)lr * (double)scale
-                                         : (double)lr * (double)scale / (double)(mode == PS_SYNC ? K : (int64_t)x->w_tick);
+    const double rate = adam ? 1.0 : (double)lr;
+    const double step = mode == PS_ASYNC ? rate * (double)scale
+                                         : rate * (double)scale / (double)(mode == PS_SYNC ? K : (int64_t)x->w_tick);
     CUDA_TRY(cudaEventSynchronize(x->coef_uploaded));      // an earlier treated apply has read the staging buffer
     for (int64_t j = 0; j < K; ++j) {
       const int64_t k = (mode == PS_ASYNC && order) ? order[j] : j;
@@ -643,9 +650,11 @@ static int32_t apply_impl(ps_ctx* x, ps_mode mode, float lr, float scale, const 
     const bool mirror = rep && ((x->version + 1) % R == 0);
     if (mirror) { int32_t rc = shift_chain(x, 1); if (rc != PS_OK) return rc; }
     a.replica = mirror ? rep->buf : nullptr;
-    a.coef = lr * scale / (float)(mode == PS_SYNC ? K : (int64_t)x->w_tick);
+    const int64_t divisor = mode == PS_SYNC ? K : (int64_t)x->w_tick;
+    a.coef = adam ? (float)((double)scale / (double)divisor) : lr * scale / (float)divisor;
     a.partial = x->partial; a.max_split = MAX_SPLIT;
     a.coef_k = treated ? x->coef_dev : nullptr;
+    if (adam) a.adam = psk::AdamColumns{psk::adam_scalars(adam->h, adam->step, 1.0), psk::adam_decay(adam->h.lr, adam->weight_decay), adam->m, adam->v};
     int n = clip_norm > 0.f ? psk::launch_clip_sum_apply(a, clip_norm, x->clip_words, x->status_dev, x->st, &x->prof) : 0;
     if (n == 0) {      // nothing to clip, or no room for the kernel that clips and sums in one pass
       if (clip_norm > 0.f) { int32_t rc = clip_factors(); if (rc != PS_OK) return rc; }
@@ -677,7 +686,7 @@ static int32_t apply_impl(ps_ctx* x, ps_mode mode, float lr, float scale, const 
       for (int i = 0; i < psk::MAX_RING; ++i) a.ring[i] = i < x->cfg.ring_depth ? x->ring[i] : nullptr;
       a.ring_depth = x->cfg.ring_depth; a.v0 = x->version;
       a.first_stored = (int)std::max<int64_t>(0, seg - (int64_t)depth);
-      a.n_mirror = 0; a.coef = lr * scale;
+      a.n_mirror = 0; a.coef = adam ? scale : lr * scale;
       a.coef_k = treated ? x->coef_dev : nullptr;
       if (rep) {
         // replication events inside this segment: versions that are multiples of R.  The i-th live server behind
@@ -699,7 +708,16 @@ static int32_t apply_impl(ps_ctx* x, ps_mode mode, float lr, float scale, const 
         }
       }
       for (int64_t u = 0; u < seg; ++u) ord.slot[u] = order ? order[pos + u] : (int32_t)(pos + u);
-      int n = psk::launch_async_apply(a, ord, x->st, &x->prof);
+      psk::AsyncAdam aa;
+      if (adam) {
+        aa.col = psk::AdamColumns{psk::adam_scalars(adam->h, adam->step + pos, 1.0), psk::adam_decay(adam->h.lr, adam->weight_decay), adam->m, adam->v};
+        for (int64_t u = 0; u < seg; ++u) {
+          const psk::AdamScalars s = psk::adam_scalars(adam->h, adam->step + pos + u, 1.0);
+          aa.step_size[u] = s.step_size;
+          aa.rs2[u] = s.rs2;
+        }
+      }
+      int n = adam ? psk::launch_async_adamw(a, ord, aa, x->st, &x->prof) : psk::launch_async_apply(a, ord, x->st, &x->prof);
       if (n < 0) return cuda_fail(cudaGetLastError(), "async apply launch");
       x->launches += n;
       x->version += (uint64_t)seg;
@@ -728,6 +746,22 @@ int32_t ps_apply_stale(ps_ctx* x, ps_mode mode, float lr, float scale, const int
                        float staleness_alpha, ps_apply_result* out) {
   if (!(clip_norm >= 0.f) || !(staleness_alpha >= 0.f)) return fail(PS_ERR_BAD_ARG, "clip_norm and staleness_alpha must be >= 0");
   return apply_impl(x, mode, lr, scale, order, clip_norm, staleness_alpha, out);
+}
+
+int32_t ps_apply_adamw(ps_ctx* x, ps_mode mode, const ps_adamw_hyper* h, double weight_decay, float* m_dev, float* v_dev, float scale,
+                       const int32_t* order, float staleness_alpha, ps_apply_result* out) {
+  if (!x) return fail(PS_ERR_BAD_ARG, "ctx is NULL");
+  int32_t rc = psk::check_adamw_hyper(h);
+  if (rc != PS_OK) return rc;
+  if (h->step < 1) return fail(PS_ERR_BAD_ARG, "step must be >= 1");
+  if (h->lr_dev || h->skip_nonfinite) return fail(PS_ERR_BAD_ARG, "lr_dev and skip_nonfinite are the many-tensor step's");
+  if (!(weight_decay >= 0.0) || !std::isfinite(weight_decay)) return fail(PS_ERR_BAD_ARG, "weight_decay must be >= 0");
+  if (!(staleness_alpha >= 0.f)) return fail(PS_ERR_BAD_ARG, "staleness_alpha must be >= 0");
+  if (!std::isfinite(h->grad_scale) || !std::isfinite((float)(h->grad_scale * scale))) return fail(PS_ERR_BAD_ARG, "grad_scale and scale must be finite");
+  if (!m_dev || !v_dev || m_dev == v_dev || ((uintptr_t)m_dev & 15) != 0 || ((uintptr_t)v_dev & 15) != 0)
+    return fail(PS_ERR_BAD_ARG, "m_dev and v_dev must be two 16-byte aligned device vectors of PS_PARAM_STRIDE floats");
+  const AdamApply adam = {{h->lr, h->beta1, h->beta2, h->eps}, weight_decay, h->step, m_dev, v_dev};
+  return apply_impl(x, mode, 1.f, (float)(h->grad_scale * scale), order, (float)h->clip_norm, staleness_alpha, out, &adam);
 }
 
 int32_t ps_kill(ps_ctx* x, int32_t server) {

@@ -15,6 +15,8 @@ P = 813258
 P_PAD = 813312
 SYNC, ASYNC, REPLAY = 0, 1, 2
 FP32, TF32, BF16 = 0, 1, 2
+TYPE_FP32, TYPE_BF16, TYPE_FP16 = 0, 1, 2
+ADAMW_BLOCK = 256
 
 ERRORS = {-1: "PS_ERR_BAD_ARG", -2: "PS_ERR_DOWN", -3: "PS_ERR_QUEUE_FULL", -4: "PS_ERR_NO_CHECKPOINT",
           -5: "PS_ERR_VERSION_EVICTED", -6: "PS_ERR_NO_REPLICA", -7: "PS_ERR_ARENA_TOO_SMALL",
@@ -24,7 +26,8 @@ EXPORTS = ["ps_query_bytes", "ps_create", "ps_destroy", "ps_pull_snapshot", "ps_
            "workers_grad_step", "workers_grad_step_summed", "ps_apply_summed", "workers_eval", "ps_dropout_mask", "ps_enqueue", "ps_apply", "ps_apply_stale", "ps_checkpoint", "ps_restore", "ps_replicate",
            "ps_kill", "ps_failover", "ps_import_params", "ps_export_params", "ps_stats", "ps_tick_host",
            "ps_tick_host_submit", "ps_tick_host_wait",
-           "ps_profile", "ps_profile_read", "ps_selftest_wait_timeout", "ps_last_error", "ps_replay_sum_static", "ps_replay_sum_static_error"]
+           "ps_profile", "ps_profile_read", "ps_selftest_wait_timeout", "ps_last_error", "ps_replay_sum_static", "ps_replay_sum_static_error",
+           "ps_apply_adamw", "ps_adamw_query_bytes", "ps_adamw_create", "ps_adamw_destroy", "ps_adamw_set_grads", "ps_adamw_step", "ps_adamw_read_info"]
 
 
 class PSError(RuntimeError):
@@ -57,6 +60,26 @@ class Stats(C.Structure):
                 ("applied_total", C.c_int64), ("up", C.c_int32), ("live_replicas", C.c_int32),
                 ("checkpoints", C.c_int32), ("device_status", C.c_uint32), ("replica_version", C.c_uint64),
                 ("last_ckpt_version", C.c_uint64), ("kernel_launches", C.c_int64)]
+
+
+class AdamWTensor(C.Structure):
+    _fields_ = [("n", C.c_int64), ("param", C.c_void_p), ("grad", C.c_void_p), ("copy", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p),
+                ("m_scale", C.c_void_p), ("v_scale", C.c_void_p), ("weight_decay", C.c_double)]
+
+
+class AdamWConfig(C.Structure):
+    _fields_ = [("param_type", C.c_int32), ("grad_type", C.c_int32), ("copy_type", C.c_int32), ("state_bits", C.c_int32), ("arena", C.c_void_p),
+                ("arena_bytes", C.c_uint64), ("stream", C.c_void_p)]
+
+
+class AdamWHyper(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("grad_scale", C.c_double),
+                ("clip_norm", C.c_double), ("step", C.c_int64), ("seed", C.c_uint64), ("lr_dev", C.c_void_p), ("skip_nonfinite", C.c_int32),
+                ("reserved", C.c_int32)]
+
+
+class AdamWInfo(C.Structure):
+    _fields_ = [("counted_steps", C.c_int64), ("skipped_steps", C.c_int64), ("grad_norm", C.c_float), ("grad_factor", C.c_float)]
 
 
 _lib = None
@@ -97,6 +120,13 @@ def load(path=None):
         "ps_tick_host_submit": [vp, i32, i32, vp, vp, vp, u64, u64, i32, f32, f32, vp, vp, vp],
         "ps_tick_host_wait": [vp, C.POINTER(ApplyResult)],
     }
+    sig["ps_apply_adamw"] = [vp, i32, C.POINTER(AdamWHyper), C.c_double, vp, vp, f32, vp, f32, C.POINTER(ApplyResult)]
+    sig["ps_adamw_query_bytes"] = [C.POINTER(AdamWConfig), vp, i32, C.POINTER(u64)]
+    sig["ps_adamw_create"] = [C.POINTER(AdamWConfig), vp, i32, C.POINTER(vp)]
+    sig["ps_adamw_destroy"] = [vp]
+    sig["ps_adamw_set_grads"] = [vp, vp]
+    sig["ps_adamw_step"] = [vp, C.POINTER(AdamWHyper)]
+    sig["ps_adamw_read_info"] = [vp, C.POINTER(AdamWInfo)]
     sig["ps_profile"] = [vp, i32]
     sig["ps_selftest_wait_timeout"] = [vp, i64]
     sig["ps_profile_read"] = [vp, i32, C.POINTER(C.c_char_p), C.POINTER(C.c_double), C.POINTER(i64)]
@@ -115,7 +145,8 @@ def load(path=None):
         from . import _marshal as m
         m.bind({n: C.cast(getattr(L, n), C.c_void_p).value for n in
                 ("ps_pull_snapshot", "ps_queue_reserve", "workers_grad_step", "workers_grad_step_summed", "workers_eval",
-                 "ps_enqueue", "ps_apply", "ps_apply_stale", "ps_apply_summed", "ps_last_error")}, Snapshot, PSError,
+                 "ps_enqueue", "ps_apply", "ps_apply_stale", "ps_apply_summed", "ps_apply_adamw",
+                 "ps_adamw_step", "ps_last_error")}, Snapshot, PSError,
                lambda o, kind: np.ascontiguousarray(o, dtype=(np.int32, np.int64, np.uint64)[kind]),
                lambda snaps, n: (Snapshot * n)(*snaps))
         _lib, _marshal = L, m
@@ -142,6 +173,113 @@ def ps_replay_sum_static(queue_dev, theta_in_dev, theta_out_dev, coef, stream=No
 
 def _np_ptr(a):
     return a.ctypes.data if a is not None else None
+
+
+def _type(t):
+    import torch
+    kinds = {torch.float32: TYPE_FP32, torch.bfloat16: TYPE_BF16, torch.float16: TYPE_FP16}
+    if t.dtype not in kinds:
+        raise TypeError(f"float32, bfloat16 or float16 is wanted, not {t.dtype}")
+    return kinds[t.dtype]
+
+
+class AdamW:
+    """AdamW over a list of tensors; every step is one launch over all of them (two where the device has to find something out first).
+    params, grads: lists of contiguous cuda tensors of equal sizes, each list of one type (float32, bfloat16 or float16).  state_bits 32 or 8
+    (include/ps.h says what the 8-bit moments are); m, v, and with 8 bits m_scale, v_scale: lists of tensors to keep the moments in, zeros of
+    the optimizer's own where not given (float32, or uint8 with a scale per 256 elements).  weight_decay: a number or one per tensor.  copies:
+    bfloat16 or float16 tensors that receive the new weights as well.  The optimizer holds on to all of them, and works on `stream`, or the
+    stream current when it is made; that is where the tensors have to be ready."""
+
+    def __init__(self, params, grads, state_bits=32, weight_decay=0.01, copies=None, m=None, v=None, m_scale=None, v_scale=None, stream=None):
+        import torch
+        self.lib = load()
+        self.params, self.grads = list(params), list(grads)
+        n = len(self.params)
+        if n == 0:
+            raise ValueError("no tensors")
+        dev = self.device = self.params[0].device
+        decay = [float(weight_decay)] * n if np.isscalar(weight_decay) else [float(d) for d in weight_decay]
+        state_bits = int(state_bits)
+        code = torch.float32 if state_bits == 32 else torch.uint8
+        blocks = lambda p: (p.numel() + ADAMW_BLOCK - 1) // ADAMW_BLOCK
+        own = lambda given, size, kind: list(given) if given is not None else [torch.zeros(size(p), dtype=kind, device=dev) for p in self.params]
+        self.m, self.v = own(m, lambda p: p.numel(), code), own(v, lambda p: p.numel(), code)
+        self.m_scale = self.v_scale = None
+        if state_bits == 8:
+            self.m_scale, self.v_scale = own(m_scale, blocks, torch.uint8), own(v_scale, blocks, torch.uint8)
+        elif m_scale is not None or v_scale is not None:
+            raise ValueError("scales go with state_bits=8")
+        self.copies = list(copies) if copies is not None else None
+        lists = [("params", self.params, None, None), ("grads", self.grads, self.grads[0].dtype if self.grads else None, None), ("copies", self.copies, None, None),
+                 ("m", self.m, code, None), ("v", self.v, code, None), ("m_scale", self.m_scale, torch.uint8, blocks), ("v_scale", self.v_scale, torch.uint8, blocks)]
+        for name, ts, kind, size in lists:
+            if ts is None:
+                continue
+            if len(ts) != n:
+                raise ValueError(f"{name}: {len(ts)} tensors for {n} weights")
+            for t, p in zip(ts, self.params):
+                if t.device != dev or not t.is_cuda or not t.is_contiguous() or t.dtype != (kind or ts[0].dtype) or t.numel() != (size(p) if size else p.numel()):
+                    raise ValueError(f"{name}: contiguous tensors on {dev}, of one type and of the weights' sizes, are wanted")
+        if len(decay) != n:
+            raise ValueError(f"weight_decay: {len(decay)} values for {n} weights")
+        table = (AdamWTensor * n)()
+        ptr = lambda ts, i: ts[i].data_ptr() if ts is not None else None
+        for i, p in enumerate(self.params):
+            table[i] = AdamWTensor(p.numel(), p.data_ptr(), self.grads[i].data_ptr(), ptr(self.copies, i), self.m[i].data_ptr(), self.v[i].data_ptr(),
+                                   ptr(self.m_scale, i), ptr(self.v_scale, i), decay[i])
+        cfg = AdamWConfig()
+        cfg.param_type, cfg.grad_type, cfg.state_bits = _type(self.params[0]), _type(self.grads[0]), state_bits
+        cfg.copy_type = _type(self.copies[0]) if self.copies is not None else 0
+        size, opt = C.c_uint64(), C.c_void_p()
+        with torch.cuda.device(dev):
+            self.stream = stream if stream is not None else torch.cuda.current_stream()
+            self._check(self.lib.ps_adamw_query_bytes(C.byref(cfg), table, n, C.byref(size)))
+            self.arena = torch.empty(size.value, dtype=torch.uint8, device=dev)
+            cfg.arena, cfg.arena_bytes, cfg.stream = self.arena.data_ptr(), size.value, self.stream.cuda_stream
+            self.stream.wait_stream(torch.cuda.current_stream())
+            self._check(self.lib.ps_adamw_create(C.byref(cfg), table, n, C.byref(opt)))
+        self.opt, self._addr = opt, opt.value
+
+    def _check(self, rc):
+        if rc != 0:
+            raise PSError(rc, self.lib.ps_last_error(None).decode())
+
+    def ps_adamw_step(self, lr, beta1=0.9, beta2=0.999, eps=1e-8, step=0, clip_norm=0.0, grad_scale=1.0, seed=0, lr_dev=None, skip_nonfinite=False):
+        """One step; step: its number from 1, or 0 to let the device count.  lr_dev: a float32 cuda tensor whose first element is read in place of lr."""
+        if lr_dev is not None:
+            import torch
+            assert lr_dev.device == self.device and lr_dev.dtype == torch.float32 and lr_dev.numel() >= 1
+            lr_dev = lr_dev.data_ptr()
+        _marshal.adamw_step(self._addr, lr, beta1, beta2, eps, step, clip_norm, grad_scale, seed, lr_dev, skip_nonfinite)
+
+    def ps_adamw_set_grads(self, grads):
+        """Other gradient tensors for the following steps."""
+        grads = list(grads)
+        if len(grads) != len(self.params):
+            raise ValueError(f"grads: {len(grads)} tensors for {len(self.params)} weights")
+        for t, g, p in zip(grads, self.grads, self.params):
+            if t.device != self.device or not t.is_contiguous() or t.dtype != g.dtype or t.numel() != p.numel():
+                raise ValueError("grads: contiguous tensors of the weights' device and sizes and the first gradients' type are wanted")
+        self._check(self.lib.ps_adamw_set_grads(self.opt, (C.c_void_p * len(grads))(*[t.data_ptr() for t in grads])))
+        self.grads = grads
+
+    def ps_adamw_read_info(self):
+        """counted_steps, skipped_steps, grad_norm, grad_factor; waits for the stream."""
+        i = AdamWInfo()
+        self._check(self.lib.ps_adamw_read_info(self.opt, C.byref(i)))
+        return {k: getattr(i, k) for k, _ in AdamWInfo._fields_}
+
+    def close(self):
+        if getattr(self, "opt", None):
+            self.lib.ps_adamw_destroy(self.opt)
+            self.opt = self._addr = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
 
 
 class ParameterServer:
@@ -275,6 +413,14 @@ class ParameterServer:
     def ps_apply_stale(self, mode, lr, scale=1.0, order=None, clip_norm=0.0, staleness_alpha=0.0):
         return _marshal.apply_stale(self._addr, mode, lr, scale, order, clip_norm, staleness_alpha)
 
+    def ps_apply_adamw(self, mode, m_dev, v_dev, lr, beta1=0.9, beta2=0.999, eps=1e-8, step=1, weight_decay=0.01, scale=1.0, order=None, clip_norm=0.0,
+                       staleness_alpha=0.0, grad_scale=1.0):
+        """The server step with AdamW.  m_dev, v_dev: float32 cuda tensors [P_PAD] with the moments; step: the (first) update's number from 1."""
+        for t in (m_dev, v_dev):
+            assert t.device == self.arena.device and t.dtype == self._torch.float32 and t.is_contiguous() and t.numel() == P_PAD
+        return _marshal.apply_adamw(self._addr, mode, lr, beta1, beta2, eps, step, clip_norm, grad_scale, weight_decay, m_dev.data_ptr(), v_dev.data_ptr(),
+                                    scale, order, staleness_alpha)
+
     def _version_call(self, fn):
         v = C.c_uint64()
         self._check(fn(self.ctx, C.byref(v)))
@@ -376,3 +522,8 @@ class ParameterServer:
         torch = self._torch
         off = self.ps_slot_ptr(slot) - self.arena.data_ptr()
         return self.arena[off:off + P_PAD * 4].view(torch.float32)
+
+    def head_tensor(self):
+        """A [P_PAD] float32 cuda view of the head weights (borrowed memory: valid as long as the snapshot of that version is)."""
+        off = self.ps_pull_snapshot(0).dev_ptr - self.arena.data_ptr()
+        return self.arena[off:off + P_PAD * 4].view(self._torch.float32)
