@@ -435,6 +435,79 @@ typedef struct {
 } ps_adamw_info;
 int32_t ps_adamw_read_info(ps_adamw* opt, ps_adamw_info* out);      /* synchronises the stream */
 
+/* The dense layer of `groups` workers, each with a mini-batch of its own length and on a weight snapshot of its own choice, forward and backward.
+ * The rows of the groups lie one after another in every matrix of rows; a group may have none; rows behind the last group's are neither read nor
+ * written.  BF16 or FP16 operands, FP32 accumulation, every result rounded once.  Matrices have their columns next to each other and any pitch
+ * (elements from row to row) not below their width.  x, weight and dy are read by tile copies, which want a base on 16 bytes and pitches and
+ * strides that are multiples of 8: others are first laid out anew in the workspace (workers_dense_workspace says how much; 0 if nothing has to be).
+ * rows and weight_of are read at the call, so a captured graph repeats them; everything on the device must stay until the work is done.  The
+ * entry points keep nothing between calls and may be used from several threads and streams at once, each call with its own workspace. */
+enum { PS_ACT_NONE = 0, PS_ACT_RELU = 1, PS_ACT_GELU = 2 /* z (1 + erf(z / sqrt 2)) / 2 */, PS_ACT_SILU = 3 /* z / (1 + e^-z) */ };
+
+typedef struct {
+  int32_t        groups;          /* 1..PS_MAX_WORKERS */
+  int32_t        n_weights;       /* 1..65535 snapshots */
+  const int32_t* rows;            /* host [groups], >= 0 */
+  const int32_t* weight_of;       /* host [groups], the snapshot that a group uses; NULL = its own number */
+  int32_t        in_features, out_features;      /* 1..2^20 */
+  int32_t        type;            /* of x, weight, bias, residual, pre, dy, dx...: PS_TYPE_BF16 or PS_TYPE_FP16 */
+  int32_t        activation;      /* PS_ACT_*; backward: the activation that x went through */
+  const void*    x;               /* dev [sum of rows][in_features] */
+  int64_t        x_pitch;
+  const void*    weight;          /* dev [n_weights][out_features][in_features] */
+  int64_t        weight_pitch, weight_stride;    /* elements from row to row, from snapshot to snapshot */
+  void*          workspace;       /* dev; NULL if none is needed */
+  uint64_t       workspace_bytes;
+  void*          stream;          /* cudaStream_t of the current device */
+} ps_dense_layer;
+
+typedef struct {
+  const void* bias;               /* dev [n_weights][out_features] or NULL */
+  int64_t     bias_stride;
+  const void* residual;           /* dev [rows][out_features] or NULL */
+  int64_t     residual_pitch;
+  void*       y;                  /* dev [rows][out_features], written */
+  int64_t     y_pitch;
+  int32_t     y_type;             /* `type`, or PS_TYPE_FP32 */
+  int32_t     reserved;
+  void*       pre;                /* dev [rows][out_features] or NULL, written */
+  int64_t     pre_pitch;
+} ps_dense_output;
+
+/* pre = x W^T + bias ;  y = activation(pre) + residual  (of the sum before it is rounded to pre).
+ * Errors: PS_ERR_BAD_ARG, PS_ERR_ARENA_TOO_SMALL (workspace), PS_ERR_CUDA; nothing of the product is launched then. */
+int32_t workers_dense_forward(const ps_dense_layer* layer, const ps_dense_output* out);
+
+typedef struct {
+  const void* dy;                 /* dev [rows][out_features]: the gradient with respect to x W^T + bias */
+  int64_t     dy_pitch;
+  const void* dx_add;             /* dev [rows][in_features] or NULL: a gradient that reaches x by another way (a residual) */
+  int64_t     dx_add_pitch;
+  const void* x_pre;              /* dev [rows][in_features]: what x was before its activation (the layer below's pre); read for dx_pre only */
+  int64_t     x_pre_pitch;
+  void*       dx;                 /* dev [rows][in_features] or NULL, written */
+  int64_t     dx_pitch;
+  void*       dx_pre;             /* dev [rows][in_features] or NULL, written: the layer below's dy */
+  int64_t     dx_pre_pitch;
+  void*       dw;                 /* dev [groups][out_features][in_features] or NULL: a gradient per worker, as for the gradient queue */
+  int64_t     dw_pitch, dw_stride;
+  void*       db;                 /* dev [groups][out_features] or NULL */
+  int64_t     db_stride;
+  int32_t     dw_type;            /* of dw and db: `type`, or PS_TYPE_FP32 */
+  int32_t     accumulate;         /* 1: dw and db are added to */
+} ps_dense_gradients;
+
+/* dx = dy W + dx_add ;  dx_pre = dx * activation'(x_pre)  (of dx before it is rounded; with PS_ACT_RELU zero wherever x_pre is not above zero) ;
+ * dw_g = dy_g^T x_g and db_g = the column sums of dy_g over the rows of group g, zero for a group without rows.  Each may be left out (NULL).
+ * No output may overlap an input, but for dx and dx_add.  Errors as workers_dense_forward. */
+int32_t workers_dense_backward(const ps_dense_layer* layer, const ps_dense_gradients* out);
+
+/* Workspace bytes of a call with these operands; dy NULL: of the forward call. */
+int32_t workers_dense_workspace(const ps_dense_layer* layer, const void* dy, int64_t dy_pitch, uint64_t* bytes);
+
+/* Synchronises the stream; PS_ERR_DEVICE_STATUS if a bounded wait of a dense-layer kernel on the current device gave up since the last call. */
+int32_t workers_dense_status(void* stream);
+
 const char* ps_last_error(ps_ctx* ctx);
 
 #ifdef __cplusplus

@@ -1,0 +1,1055 @@
+// The dense layer of W workers with ragged mini-batches (workers_dense_forward / workers_dense_backward in include/ps.h), on the
+// fifth-generation tensor cores: BF16 or FP16 operands, FP32 accumulation.
+//   forward          pre[m][n] = sum_k x[m][k] W[n][k] + b[n] ;  y = act(pre) + r         (rows m of the workers that hold W)
+//   input gradient   dx[m][k]  = sum_n dy[m][n] W[n][k] + dx_add ;  dx_pre = dx * act'(x_pre)
+//   weight gradient  dW[n][k]  = sum_m dy[m][n] x[m][k]                                   (m = the rows of one worker)
+// Every operand is read as it lies, with k contiguous or its row index contiguous (128-byte swizzle, blocks of 64), and every result is
+// rounded once, in the epilogue that also does everything elementwise.
+//
+// Tiles, by the work there is (plan_*):
+//   Pair   256 x 256 by two CTAs that share each MMA (cta_group::2): half of the right operand each, so that a CTA brings in 32 KB for
+//          128 x 256 x 64 products.  Two accumulators of 256 columns are used in turn: one is read out while the other fills.
+//   Single 128 x 256 by one CTA: workers with less than 256 rows.
+//   Split  128 x 128, the blocks of k dealt out over a cluster of CTAs whose partial tiles are added through distributed shared memory
+//          in a fixed order: few tiles.
+//   Few    weights as the left operand, 128 of their rows x 16, 32 or 64 rows of a worker, split likewise: bound by reading the weights.
+// Pair and Single run one CTA (pair) per SM that walks over the tiles; the others one cluster per tile.
+//
+// Precision: the accumulators drop the low bits of every sum, always towards zero (bf16x3.cuh).  For results in FP32 the sums over 512 values
+// of k are handed to registers and added there, rounded; for 16-bit results their own rounding is 100 times what is lost.
+//
+// Ragged reductions (weight gradient): a tile's last block of 64 rows may reach into the next worker's.  Those rows are zeroed in shared
+// memory, in both operands (a NaN times zero would stay), before the MMA reads them.
+//
+// Every wait on an mbarrier is bounded; a CTA that gives up sets a status word that workers_dense_status reads.
+#include <cooperative_groups.h>
+#include <cuda.h>
+#include <cuda_fp16.h>
+
+#include <algorithm>
+#include <cmath>
+#include <mutex>
+
+#include "device_common.cuh"
+#include "error.h"
+#include "kernels.h"
+#include "ps.h"
+#include "tc5_common.cuh"
+
+namespace psk {
+
+namespace {
+
+namespace cg = cooperative_groups;
+
+enum { D_FWD = 0, D_DX = 1, D_DW = 2 };
+constexpr int BM = 128, BK = 64;
+constexpr int DRAIN_BLOCKS = 8;      // blocks of k whose sums share an accumulator where the result is FP32
+constexpr int SMEM_MOST = 227 * 1024, BARRIER_BYTES = 256;
+
+template <int OP_, int CTAS_, int BN_, int STAGES_, bool SPLIT_, bool FEW_, bool DRAIN_> struct DenseShape {
+  static constexpr int OP = OP_, CTAS = CTAS_, BN = BN_, STAGES = STAGES_, TM = BM * CTAS;
+  static constexpr bool SPLIT = SPLIT_, FEW = FEW_, DRAIN = DRAIN_;
+  static constexpr bool A_MN = FEW ? OP == D_DX : OP == D_DW, B_MN = !FEW && OP != D_FWD;      // is the operand's row index contiguous?
+  static constexpr int B_ROWS = BN / CTAS;
+  static constexpr int A_BYTES = BM * BK * 2, B_BYTES = B_ROWS * BK * 2, STAGE = A_BYTES + B_BYTES;
+  static constexpr int BUFS = SPLIT ? 1 : 2, ACC = BN < 32 ? 32 : BN;
+  static constexpr int EPI_WARPS = FEW ? 4 : 8, THREADS = 64 + 32 * EPI_WARPS, COLS = FEW ? BN : BN / 2;
+  static constexpr int OUT_BYTES = SPLIT ? 0 : EPI_WARPS * 4096;      // a 32 x 32 block per warp on its way to whole rows
+  static constexpr int SMEM = 1024 + STAGES * STAGE + OUT_BYTES + BARRIER_BYTES;
+  static constexpr int PART_PITCH = FEW ? BM + 4 : BN + 4, PART_BYTES = (FEW ? BN : BM) * PART_PITCH * 4;
+  static_assert(SMEM <= SMEM_MOST && STAGE % 1024 == 0 && ACC * BUFS <= 512, "tile shape");
+  static_assert(!SPLIT || PART_BYTES <= STAGES * STAGE, "the partial tile takes the operands' place");
+  static_assert(!SPLIT || CTAS == 1, "a pair's tile is not split");
+};
+template <int OP, bool DRAIN> using Pair = DenseShape<OP, 2, 256, 6, false, false, DRAIN>;
+template <int OP, bool DRAIN> using Single = DenseShape<OP, 1, 256, 4, false, false, DRAIN>;
+template <int OP> using Split = DenseShape<OP, 1, 128, 3, true, false, true>;
+template <int OP, int BN> using Few = DenseShape<OP, 1, BN, BN == 64 ? 4 : 5, true, true, true>;
+
+// Groups of rows [row0[g], row0[g + 1]) with weight matrix w[g]; tile0: prefix sums of their tiles (weight gradient: not used).
+struct DenseTab {
+  int32_t groups;
+  int32_t row0[PS_MAX_WORKERS + 1];
+  int32_t tile0[PS_MAX_WORKERS + 1];
+  uint16_t w[PS_MAX_WORKERS];
+};
+
+// What the epilogue adds and where it writes (pitches in elements).  forward: in0 bias, in1 residual, out0 y, out1 pre; input gradient: in1
+// dx_add, in2 x_pre, out0 dx, out1 dx_pre; weight gradient: out0 dW.
+struct DenseEpi {
+  const void *in0, *in1, *in2;
+  void *out0, *out1;
+  int64_t in0_stride, in1_pitch, in2_pitch, out0_pitch, out0_stride, out1_pitch;
+  int32_t act, bf16, out0_fp32, accumulate;
+  int32_t v_in0, v_in1, v_in2, v_out0, v_out1;      // may four values be moved at once?
+};
+
+struct DenseArgs {
+  int32_t n_tiles, m_tiles, n_side, n_tiles_n;      // tiles; weight gradient: tiles along the left side; length and tiles of the right side (Few: of the left)
+  int32_t m_side;                                   // weight gradient: length of the left side
+  int32_t red;                                      // reduction length (weight gradient: the group's rows)
+  int32_t chunk;                                    // blocks of k per accumulator
+  uint32_t idesc;
+};
+
+// Set when a wait gives up, until workers_dense_status reads it: these entry points have no context to keep it in.
+__device__ uint32_t g_dense_status;
+
+struct DenseMaps { CUtensorMap a, b; };
+
+// ---- element types -------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ float widen(uint32_t half_word, int bf16) {
+  return bf16 ? __uint_as_float(half_word << 16) : __half2float(__ushort_as_half((unsigned short)half_word));
+}
+__device__ __forceinline__ uint32_t narrow2(float lo, float hi, int bf16) {
+  if (bf16) return bf16_pair(lo, hi);
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+// Four consecutive 16-bit values from element i on, of which n exist.
+__device__ __forceinline__ float4 load4(const void* base, int64_t i, int n, int vec, int bf16) {
+  const uint16_t* p = reinterpret_cast<const uint16_t*>(base) + i;
+  if (vec && n >= 4) {
+    const uint2 w = *reinterpret_cast<const uint2*>(p);
+    return make_float4(widen(w.x & 0xFFFFu, bf16), widen(w.x >> 16, bf16), widen(w.y & 0xFFFFu, bf16), widen(w.y >> 16, bf16));
+  }
+  return make_float4(widen(p[0], bf16), n > 1 ? widen(p[1], bf16) : 0.f, n > 2 ? widen(p[2], bf16) : 0.f, n > 3 ? widen(p[3], bf16) : 0.f);
+}
+__device__ __forceinline__ void store4(void* base, int64_t i, int n, int vec, int bf16, const float4& v) {
+  uint16_t* p = reinterpret_cast<uint16_t*>(base) + i;
+  const uint32_t a = narrow2(v.x, v.y, bf16), b = narrow2(v.z, v.w, bf16);
+  if (vec && n >= 4) {
+    *reinterpret_cast<uint2*>(p) = make_uint2(a, b);
+    return;
+  }
+  p[0] = (uint16_t)a;
+  if (n > 1) p[1] = (uint16_t)(a >> 16);
+  if (n > 2) p[2] = (uint16_t)b;
+  if (n > 3) p[3] = (uint16_t)(b >> 16);
+}
+__device__ __forceinline__ float4 load4_f32(const float* p, int n, int vec) {
+  if (vec && n >= 4) return *reinterpret_cast<const float4*>(p);
+  return make_float4(p[0], n > 1 ? p[1] : 0.f, n > 2 ? p[2] : 0.f, n > 3 ? p[3] : 0.f);
+}
+__device__ __forceinline__ void store4_f32(float* p, int n, int vec, const float4& v) {
+  if (vec && n >= 4) { *reinterpret_cast<float4*>(p) = v; return; }
+  p[0] = v.x;
+  if (n > 1) p[1] = v.y;
+  if (n > 2) p[2] = v.z;
+  if (n > 3) p[3] = v.w;
+}
+__device__ __forceinline__ float4 add(const float4& a, const float4& b) { return make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w); }
+
+__device__ __forceinline__ float activate(float z, int act) {
+  if (act == PS_ACT_RELU) return z < 0.f ? 0.f : z;                 // NaN stays
+  if (act == PS_ACT_GELU) return 0.5f * z * (1.f + erff(z * 0.70710678f));
+  if (act == PS_ACT_SILU) return __fdividef(z, 1.f + expf(-z));
+  return z;
+}
+// d * act'(z)
+__device__ __forceinline__ float through(float d, float z, int act) {
+  if (act == PS_ACT_RELU) return z > 0.f ? d : 0.f;
+  if (act == PS_ACT_GELU) return d * (0.5f * (1.f + erff(z * 0.70710678f)) + z * 0.39894228f * expf(-0.5f * z * z));
+  if (act == PS_ACT_SILU) {
+    const float e = __fdividef(1.f, 1.f + expf(-z));
+    return d * (e * (1.f + z * (1.f - e)));
+  }
+  return d;
+}
+
+// Everything elementwise for four consecutive columns of a row.  which: the weight matrix (forward) or the worker (weight gradient); bias: in0's
+// four values, loaded by the caller, whose column stays the same over many rows.
+template <int OP>
+__device__ __forceinline__ void finish4(const DenseEpi& e, int64_t row, int col, int n, int which, const float4& bias, float4 v) {
+  if (OP == D_FWD) {
+    v = add(v, bias);
+    if (e.out1) store4(e.out1, row * e.out1_pitch + col, n, e.v_out1, e.bf16, v);
+    if (e.act != PS_ACT_NONE) v = make_float4(activate(v.x, e.act), activate(v.y, e.act), activate(v.z, e.act), activate(v.w, e.act));
+    if (e.in1) v = add(v, load4(e.in1, row * e.in1_pitch + col, n, e.v_in1, e.bf16));
+    if (e.out0_fp32) store4_f32(reinterpret_cast<float*>(e.out0) + row * e.out0_pitch + col, n, e.v_out0, v);
+    else store4(e.out0, row * e.out0_pitch + col, n, e.v_out0, e.bf16, v);
+  } else if (OP == D_DX) {
+    if (e.in1) v = add(v, load4(e.in1, row * e.in1_pitch + col, n, e.v_in1, e.bf16));
+    if (e.out0) store4(e.out0, row * e.out0_pitch + col, n, e.v_out0, e.bf16, v);
+    if (e.out1) {
+      const float4 z = load4(e.in2, row * e.in2_pitch + col, n, e.v_in2, e.bf16);
+      store4(e.out1, row * e.out1_pitch + col, n, e.v_out1, e.bf16,
+             make_float4(through(v.x, z.x, e.act), through(v.y, z.y, e.act), through(v.z, z.z, e.act), through(v.w, z.w, e.act)));
+    }
+  } else {
+    const int64_t at = (int64_t)which * e.out0_stride + row * e.out0_pitch + col;
+    if (e.out0_fp32) {
+      float* p = reinterpret_cast<float*>(e.out0) + at;
+      if (e.accumulate) v = add(v, load4_f32(p, n, e.v_out0));
+      store4_f32(p, n, e.v_out0, v);
+    } else {
+      if (e.accumulate) v = add(v, load4(e.out0, at, n, e.v_out0, e.bf16));
+      store4(e.out0, at, n, e.v_out0, e.bf16, v);
+    }
+  }
+}
+template <int OP>
+__device__ __forceinline__ float4 bias4(const DenseEpi& e, int col, int n, int which) {
+  if (OP != D_FWD || !e.in0 || n <= 0) return make_float4(0.f, 0.f, 0.f, 0.f);
+  return load4(e.in0, (int64_t)which * e.in0_stride + col, n, e.v_in0, e.bf16);
+}
+
+// ---- pairs of CTAs ---------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+// A barrier's address in the pair's first CTA.
+__device__ __forceinline__ uint32_t leaders(const uint64_t* bar) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(smem_u32(bar)));
+  return r;
+}
+__device__ __forceinline__ void arrive_at(uint32_t cluster_addr) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+__device__ __forceinline__ bool cluster_try(uint32_t addr, uint32_t parity) {
+  uint32_t done;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(done) : "r"(addr), "r"(parity) : "memory");
+  return done != 0;
+}
+// The bounded wait of a whole warp for arrivals from both CTAs.
+__device__ __forceinline__ bool pair_wait(uint64_t* bar, uint32_t parity, const volatile uint32_t* abort_flag) {
+  const uint32_t addr = smem_u32(bar);
+  bool done = cluster_try(addr, parity);
+  if (!done) {
+    const long long t0 = clock64();
+    do {
+      done = cluster_try(addr, parity);
+    } while (!done && clock64() - t0 <= WAIT_LIMIT_CYCLES);
+  }
+  return __all_sync(0xffffffffu, done && !*abort_flag);
+}
+// A tile load into this CTA's shared memory that completes on a barrier of the pair's first CTA.
+__device__ __forceinline__ void tma_load_pair(void* smem_dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+      ::"r"(smem_u32(smem_dst)), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2) : "memory");
+}
+__device__ __forceinline__ void umma_f16_pair(uint32_t tmem_d, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t.reg .b64 da, db;\n\t"
+      "elect.sync _|q, 0xffffffff;\n\t"
+      "mov.b64 da, {%1, %2};\n\tmov.b64 db, {%3, %4};\n\t"
+      "setp.ne.b32 p, %6, 0;\n\t"
+      "@q tcgen05.mma.cta_group::2.kind::f16 [%0], da, db, %5, p;\n\t}"
+      ::"r"(tmem_d), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate) : "memory");
+}
+// Arrives on the barrier of both CTAs when the pair's MMAs so far are done.
+__device__ __forceinline__ void umma_commit_pair(uint64_t* bar) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\t.reg .b16 m;\n\telect.sync _|q, 0xffffffff;\n\tmov.b16 m, 3;\n\t"
+      "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], m;\n\t}" ::"r"(smem_u32(bar)) : "memory");
+}
+
+// Shared-memory descriptors.  k contiguous: rows of 128 bytes, groups of eight rows 1,024 apart.  Row index contiguous: one k = 128 bytes
+// (64 rows), groups of eight k 1,024 apart, the next 64 rows 8 KB further.  128-byte swizzle (type 2) in both.
+constexpr uint32_t DESC_HI = (1024 >> 4) | (1u << 14) | (2u << 29);
+template <bool MN> __device__ __forceinline__ uint32_t tile_desc_lo(uint32_t addr) {
+  return ((addr & 0x3FFFF) >> 4) | ((MN ? (BK * 128) >> 4 : 1u) << 16);
+}
+template <bool MN> __host__ __device__ constexpr uint32_t tile_k_step() { return MN ? 16 * 128 / 16 : 32 / 16; }      // sixteen k further, in 16-byte units
+
+struct DenseTile {
+  int grp, w;            // group, its weight matrix
+  int m0, m_end;         // left side: first row of the tile, end of the rows that count
+  int n0, n_end;         // right side
+  int red0, red;         // reduction: first index, length
+};
+
+template <class S>
+__device__ __forceinline__ void decode_tile(const DenseArgs& a, const DenseTab& tab, int t, DenseTile& c) {
+  if (S::OP == D_DW) {
+    const int per = a.m_tiles * a.n_tiles_n, g = t / per, l = t - g * per;
+    c.grp = c.w = g;
+    c.m0 = (l % a.m_tiles) * S::TM; c.m_end = a.m_side;
+    c.n0 = (l / a.m_tiles) * S::BN; c.n_end = a.n_side;
+    c.red0 = tab.row0[g]; c.red = tab.row0[g + 1] - c.red0;
+    return;
+  }
+  int lo = 0, hi = tab.groups;      // the last group that starts at or before t: one with tiles
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (tab.tile0[mid] <= t) lo = mid; else hi = mid;
+  }
+  const int l = t - tab.tile0[lo], first = tab.row0[lo], end = tab.row0[lo + 1];
+  c.grp = lo; c.w = tab.w[lo];
+  c.red0 = 0; c.red = a.red;
+  if (S::FEW) {
+    const int rt = (end - first + S::BN - 1) / S::BN;      // the tiles of one piece of the weights lie together
+    c.m0 = (l / rt) * BM; c.m_end = a.n_side;
+    c.n0 = first + (l % rt) * S::BN; c.n_end = end;
+  } else {
+    // bands of eight tiles along the rows, so that tiles under way together share operands in L2
+    const int mt = (end - first + S::TM - 1) / S::TM, per = 8 * a.n_tiles_n, band = l / per, in = min(8, mt - 8 * band), r = l - band * per;
+    c.m0 = first + (8 * band + r % in) * S::TM; c.m_end = end;
+    c.n0 = (r / in) * S::BN; c.n_end = a.n_side;
+  }
+}
+
+// The first `n` blocks of k are whole; the last may have fewer.
+__device__ __forceinline__ int blocks_of(int red) { return (red + BK - 1) / BK; }
+
+template <class S>
+__global__ void __launch_bounds__(S::THREADS, 1) dense_gemm(const __grid_constant__ DenseMaps maps, const __grid_constant__ DenseArgs a,
+                                                            const __grid_constant__ DenseEpi epi, const __grid_constant__ DenseTab tab) {
+  constexpr int STAGES = S::STAGES, BUFS = S::BUFS, EPI = S::EPI_WARPS;
+  constexpr bool PAIR = S::CTAS == 2, RAGGED = S::OP == D_DW;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  uint8_t* tiles = smem_raw + (base - smem_u32(smem_raw));
+  uint8_t* out_stage = tiles + STAGES * S::STAGE;
+  uint64_t* full = reinterpret_cast<uint64_t*>(out_stage + S::OUT_BYTES);      // [STAGES] copies -> MMA (of the pair's first CTA)
+  uint64_t* empty = full + STAGES;           // [STAGES] MMA -> copies
+  uint64_t* acc_full = empty + STAGES;       // [BUFS] MMA -> epilogue
+  uint64_t* acc_empty = acc_full + BUFS;     // [BUFS] epilogue (of both CTAs) -> MMA
+  uint64_t* tail_full = acc_empty + BUFS;    // [STAGES] copies of a ragged last block -> the warp that zeroes what is not this worker's
+  uint64_t* tail_ready = tail_full + STAGES; // [STAGES] the second CTA's such warp -> MMA
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(tail_ready + STAGES);
+  volatile uint32_t* abort_flag = tmem_slot + 1;
+  const int tid = threadIdx.x, warp = warp_uniform(tid >> 5), lane = tid & 31;
+  const uint32_t rank = PAIR ? cluster_rank() : 0u;
+  const int first_tile = PAIR ? blockIdx.x >> 1 : blockIdx.x, tile_step = S::SPLIT ? a.n_tiles : (PAIR ? gridDim.x >> 1 : gridDim.x);
+  if (tid == 0) {
+    for (int s = 0; s < STAGES; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); mbar_init(&tail_full[s], 1); mbar_init(&tail_ready[s], 1); }
+    for (int i = 0; i < BUFS; ++i) { mbar_init(&acc_full[i], 1); mbar_init(&acc_empty[i], EPI * S::CTAS); }
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    if (PAIR) {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(BUFS * S::ACC) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else {
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(BUFS * S::ACC) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (PAIR) cg::this_cluster().sync();
+  tc_fence_after();
+  const uint32_t tmem = warp_uniform(*tmem_slot);
+  pdl_enter();
+
+  // this CTA's blocks of k of a tile with `n` of them
+  auto block_range = [&](int n, int& b0, int& b1) {
+    b0 = 0; b1 = n;
+    if (S::SPLIT) {
+      b0 = (int)((int64_t)n * (int)blockIdx.z / (int)gridDim.z);
+      b1 = (int)((int64_t)n * ((int)blockIdx.z + 1) / (int)gridDim.z);
+    }
+  };
+
+  if (warp == 0) {
+    // ---------------- copies
+    if (lane == 0) {
+      int s = 0;
+      uint32_t use = 0;
+      bool ok = true;
+      for (int t = first_tile; t < a.n_tiles && ok; t += tile_step) {
+        DenseTile c;
+        decode_tile<S>(a, tab, t, c);
+        int b0, b1;
+        block_range(blocks_of(c.red), b0, b1);
+        const int am = c.m0 + (int)rank * BM, bn = c.n0 + (int)rank * S::B_ROWS;
+        for (int kb = b0; kb < b1; ++kb) {
+          if (use > 0 && !mbar_wait(&empty[s], (use - 1) & 1)) { *abort_flag = 1; ok = false; break; }
+          if (*abort_flag) { ok = false; break; }
+          uint8_t* A = tiles + s * S::STAGE;
+          uint8_t* B = A + S::A_BYTES;
+          const int k0 = kb * BK, r0 = c.red0 + k0;
+          const bool tail = RAGGED && PAIR && c.red - k0 < BK;      // each CTA of a pair cleans up its own
+          uint64_t* local = tail ? &tail_full[s] : &full[s];
+          const uint32_t remote = PAIR ? leaders(&full[s]) : 0u;
+          if (!PAIR || tail) mbar_expect_tx(local, S::STAGE);
+          if (PAIR && rank == 0) {
+            if (tail) mbar_arrive(&full[s]);
+            else mbar_expect_tx(&full[s], 2 * S::STAGE);
+          }
+          auto load = [&](uint8_t* dst, const CUtensorMap* map, int c0, int c1, int c2) {
+            if (PAIR && !tail) tma_load_pair(dst, map, remote, c0, c1, c2);
+            else tma_load_3d(dst, map, local, c0, c1, c2);
+          };
+          if (S::A_MN) {
+#pragma unroll
+            for (int i = 0; i < BM / 64; ++i) load(A + i * BK * 128, &maps.a, am + 64 * i, r0, S::FEW ? c.w : 0);
+          } else {
+            load(A, &maps.a, k0, am, S::FEW ? c.w : 0);
+          }
+          if (S::B_MN) {
+#pragma unroll
+            for (int i = 0; i < S::B_ROWS / 64; ++i) load(B + i * BK * 128, &maps.b, bn + 64 * i, r0, S::OP == D_DX ? c.w : 0);
+          } else {
+            load(B, &maps.b, k0, bn, S::FEW ? 0 : c.w);
+          }
+          if (++s == STAGES) { s = 0; ++use; }
+        }
+      }
+    }
+  } else if (warp == 1) {
+    // ---------------- MMA (a pair's: by its first CTA; the second's warp cleans up its own ragged blocks)
+    // zeroes k rows [valid, next multiple of sixteen) of a stage whose operands both have k as their rows
+    auto clean = [&](int s, int valid) {
+      const int upto = (valid + 15) & ~15;
+      uint8_t* st = tiles + s * S::STAGE;
+      for (int i = lane; i < (upto - valid) * 8; i += 32) {
+        const int at = (valid + (i >> 3)) * 128 + (i & 7) * 16;
+#pragma unroll
+        for (int b = 0; b < S::STAGE / (BK * 128); ++b) *reinterpret_cast<uint4*>(st + b * (BK * 128) + at) = make_uint4(0u, 0u, 0u, 0u);
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+    };
+    int s = 0, lead = 0;
+    uint32_t parity = 0, tails = 0;          // tails: a bit per stage, the parity of its next ragged block
+    bool ok = true;
+    for (int t = first_tile; t < a.n_tiles && ok; t += tile_step) {
+      DenseTile c;
+      decode_tile<S>(a, tab, t, c);
+      int b0, b1;
+      block_range(blocks_of(c.red), b0, b1);
+      if (PAIR && rank != 0) {
+        if (RAGGED && c.red % BK != 0) {
+          const int at = (s + b1 - 1) % STAGES;
+          if (!warp_wait(&tail_full[at], (tails >> at) & 1, abort_flag)) { *abort_flag = 1; break; }
+          tails ^= 1u << at;
+          clean(at, c.red % BK);
+          if (lane == 0) arrive_at(leaders(&tail_ready[at]));
+        }
+        s = (s + b1) % STAGES;
+        continue;
+      }
+      for (int kb = b0; kb < b1; ++kb) {
+        const bool first = (kb - b0) % a.chunk == 0, last = (kb - b0) % a.chunk == a.chunk - 1 || kb + 1 == b1;
+        if (first && lead >= BUFS) {
+          const uint32_t p = ((lead / BUFS) - 1) & 1;
+          if (!(PAIR ? pair_wait(&acc_empty[lead % BUFS], p, abort_flag) : warp_wait(&acc_empty[lead % BUFS], p, abort_flag))) { *abort_flag = 1; ok = false; break; }
+        }
+        if (!(PAIR ? pair_wait(&full[s], parity, abort_flag) : warp_wait(&full[s], parity, abort_flag))) { *abort_flag = 1; ok = false; break; }
+        const int valid = min(BK, c.red - kb * BK);
+        if (RAGGED && valid < BK) {
+          if (PAIR && !warp_wait(&tail_full[s], (tails >> s) & 1, abort_flag)) { *abort_flag = 1; ok = false; break; }
+          clean(s, valid);
+          if (PAIR && !pair_wait(&tail_ready[s], (tails >> s) & 1, abort_flag)) { *abort_flag = 1; ok = false; break; }
+          tails ^= 1u << s;
+        }
+        tc_fence_after();
+        const uint32_t a_lo = tile_desc_lo<S::A_MN>(base + s * S::STAGE), b_lo = tile_desc_lo<S::B_MN>(base + s * S::STAGE + S::A_BYTES);
+        const uint32_t d = tmem + (lead % BUFS) * S::ACC;
+#pragma unroll
+        for (int k = 0; k < BK / 16; ++k)
+          if (k * 16 < valid) {
+            const uint32_t ka = a_lo + k * tile_k_step<S::A_MN>(), kbb = b_lo + k * tile_k_step<S::B_MN>(), acc = k ? 1u : (first ? 0u : 1u);
+            if (PAIR) umma_f16_pair(d, ka, DESC_HI, kbb, DESC_HI, a.idesc, acc);
+            else umma_f16(d, ka, DESC_HI, kbb, DESC_HI, a.idesc, acc);
+          }
+        if (PAIR) umma_commit_pair(&empty[s]); else umma_commit(&empty[s]);
+        if (last) {
+          if (PAIR) umma_commit_pair(&acc_full[lead % BUFS]); else umma_commit(&acc_full[lead % BUFS]);
+          ++lead;
+        }
+        if (++s == STAGES) { s = 0; parity ^= 1; }
+      }
+    }
+  } else {
+    // ---------------- epilogue
+    const int quarter = warp & 3, col0 = S::FEW ? 0 : ((warp - 2) >> 2) * S::COLS;
+    const uint32_t t_lane = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)col0;
+    auto release = [&](int buf) {
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) {
+        if (PAIR) arrive_at(leaders(&acc_empty[buf]));
+        else mbar_arrive(&acc_empty[buf]);
+      }
+    };
+    int lead = 0;
+    for (int t = first_tile; t < a.n_tiles; t += tile_step) {
+      DenseTile c;
+      decode_tile<S>(a, tab, t, c);
+      int b0, b1;
+      block_range(blocks_of(c.red), b0, b1);
+      const int m_base = c.m0 + (int)rank * BM + quarter * 32;
+      // 32 columns of this warp's 32 rows through shared memory: a lane has a row of the accumulator and stores four columns of eight rows
+      float4* stage = reinterpret_cast<float4*>(out_stage + (warp - 2) * 4096);
+      auto write_out = [&](const float* v, int j0) {
+        const int col = c.n0 + col0 + j0 + (lane & 7) * 4, n = c.n_end - col;
+        __syncwarp();
+#pragma unroll
+        for (int q = 0; q < 8; ++q) stage[lane * 8 + (q ^ (lane & 7))] = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+        __syncwarp();
+        const float4 bias = bias4<S::OP>(epi, col, n, c.w);
+#pragma unroll 2
+        for (int i = 0; i < 8; ++i) {
+          const int r = i * 4 + (lane >> 3), m = m_base + r;
+          if (m < c.m_end && n > 0) finish4<S::OP>(epi, m, col, n, c.w, bias, stage[r * 8 + ((lane & 7) ^ (r & 7))]);
+        }
+      };
+      if constexpr (S::DRAIN) {
+        float sum[S::COLS];
+#pragma unroll
+        for (int j = 0; j < S::COLS; ++j) sum[j] = 0.f;
+        bool ok = true;
+        for (int kb = b0; kb < b1; kb += a.chunk) {
+          const int buf = lead % BUFS;
+          if (!warp_wait(&acc_full[buf], (lead / BUFS) & 1, abort_flag)) { ok = false; break; }
+          tc_fence_after();
+#pragma unroll
+          for (int j0 = 0; j0 < S::COLS; j0 += 32) {
+            uint32_t r[2][16];
+            tmem_ld16(t_lane + buf * S::ACC + j0, r[0]);
+            if (j0 + 16 < S::COLS) tmem_ld16(t_lane + buf * S::ACC + j0 + 16, r[1]);
+            tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+              if (j0 + j < S::COLS) sum[j0 + j] += __uint_as_float(r[j / 16][j % 16]);
+          }
+          release(buf);
+          ++lead;
+        }
+        if (!ok) { *abort_flag = 1; break; }
+        if constexpr (S::SPLIT) {      // all copies have landed and been read: the partial tile takes their place
+          float* part = reinterpret_cast<float*>(tiles);
+          if (S::FEW) {
+#pragma unroll
+            for (int j = 0; j < S::COLS; ++j) part[j * S::PART_PITCH + quarter * 32 + lane] = sum[j];
+          } else {
+            float4* d = reinterpret_cast<float4*>(part + (quarter * 32 + lane) * S::PART_PITCH + col0);
+#pragma unroll
+            for (int j = 0; j < S::COLS / 4; ++j) d[j] = make_float4(sum[4 * j], sum[4 * j + 1], sum[4 * j + 2], sum[4 * j + 3]);
+          }
+        } else {
+#pragma unroll
+          for (int j0 = 0; j0 < S::COLS; j0 += 32) write_out(sum + j0, j0);
+        }
+      } else {
+        const int buf = lead % BUFS;
+        const bool empty_sum = b1 == b0;      // a worker without rows: its weight gradient is zero
+        if (!empty_sum) {
+          if (!warp_wait(&acc_full[buf], (lead / BUFS) & 1, abort_flag)) { *abort_flag = 1; break; }
+          tc_fence_after();
+        }
+#pragma unroll 1
+        for (int j0 = 0; j0 < S::COLS; j0 += 32) {
+          uint32_t r[32];
+          if (empty_sum) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) r[j] = 0u;
+          } else {
+            tmem_ld32(t_lane + buf * S::ACC + j0, r);
+          }
+          if (j0 + 32 >= S::COLS && !empty_sum) release(buf);
+          float v[32];
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(r[j]);
+          write_out(v, j0);
+        }
+        if (!empty_sum) ++lead;
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (PAIR) cg::this_cluster().sync();      // no CTA leaves while the other may still arrive at its barriers
+  if (warp == 1) {
+    tc_fence_after();
+    if (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(BUFS * S::ACC) : "memory");
+    else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(BUFS * S::ACC) : "memory");
+  }
+  if constexpr (S::SPLIT) {
+    DenseTile c;
+    decode_tile<S>(a, tab, blockIdx.x, c);
+    cg::cluster_group cl = cg::this_cluster();
+    cl.sync();
+    const int ranks = gridDim.z, me = blockIdx.z;
+    constexpr int QUADS = (S::FEW ? BM : S::BN) / 4;      // of a row of the result
+    const int rows = S::FEW ? min(S::BN, c.n_end - c.n0) : min(BM, c.m_end - c.m0);
+    const int row0 = S::FEW ? c.n0 : c.m0, column0 = S::FEW ? c.m0 : c.n0, end = S::FEW ? c.m_end : c.n_end;
+    float* part = reinterpret_cast<float*>(tiles);
+    for (int e = me * S::THREADS + tid; e < rows * QUADS; e += ranks * S::THREADS) {
+      const int r = e / QUADS, q = e - r * QUADS, col = column0 + 4 * q, n = end - col;
+      if (n <= 0) continue;
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int k = 0; k < ranks; ++k) v = add(v, *reinterpret_cast<const float4*>(cl.map_shared_rank(part, k) + r * S::PART_PITCH + 4 * q));
+      finish4<S::OP>(epi, row0 + r, col, n, c.w, bias4<S::OP>(epi, col, n, c.w), v);
+    }
+    cl.sync();                               // a CTA's shared memory outlives its readers
+  }
+  if (tid == 0 && *abort_flag) {
+    atomicOr(&g_dense_status, STATUS_WAIT_TIMEOUT);
+    for (int i = 0; i < 1000; ++i) __nanosleep(1000);      // let copies already issued land before the CTA ends
+  }
+}
+
+// ---- the bias gradient: column sums of each worker's rows ------------------------------------------------------------------
+// A CTA sums 64 columns (128 bytes of a row) over its share of a worker's rows; the CTAs of a cluster share a worker's rows and add their
+// sums in order.
+constexpr int CSUM_TPB = 256;
+struct ColumnSumArgs {
+  const void* dy; void* db;
+  int64_t pitch, db_stride;
+  int32_t N, bf16, db_fp32, accumulate, vec;
+};
+__global__ void __launch_bounds__(CSUM_TPB) column_sums(const __grid_constant__ ColumnSumArgs a, const __grid_constant__ DenseTab tab) {
+  __shared__ float part[CSUM_TPB / 8][64 + 1];
+  __shared__ float mine[64];
+  pdl_enter();
+  const int g = blockIdx.y, ranks = gridDim.z, me = blockIdx.z, col = blockIdx.x * 64 + (threadIdx.x & 7) * 8, n = a.N - col;
+  const int first = tab.row0[g], rows = tab.row0[g + 1] - first;
+  const int r0 = first + (int)((int64_t)rows * me / ranks), r1 = first + (int)((int64_t)rows * (me + 1) / ranks);
+  float acc[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) acc[j] = 0.f;
+  if (n > 0) {
+#pragma unroll 4
+    for (int r = r0 + (threadIdx.x >> 3); r < r1; r += CSUM_TPB / 8) {
+      const uint16_t* p = reinterpret_cast<const uint16_t*>(a.dy) + (int64_t)r * a.pitch + col;
+      if (a.vec && n >= 8) {
+        const uint4 w = *reinterpret_cast<const uint4*>(p);
+        const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[j] += widen((x[j >> 1] >> (16 * (j & 1))) & 0xFFFFu, a.bf16);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (j < n) acc[j] += widen(p[j], a.bf16);
+      }
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) part[threadIdx.x >> 3][(threadIdx.x & 7) * 8 + j] = acc[j];
+  __syncthreads();
+  if (threadIdx.x < 64) {
+    float s = 0.f;
+#pragma unroll 8
+    for (int i = 0; i < CSUM_TPB / 8; ++i) s += part[i][threadIdx.x];
+    mine[threadIdx.x] = s;
+  }
+  cg::cluster_group cl = cg::this_cluster();
+  cl.sync();
+  const int c = blockIdx.x * 64 + threadIdx.x;
+  if (me == 0 && threadIdx.x < 64 && c < a.N) {
+    float s = 0.f;
+    for (int k = 0; k < ranks; ++k) s += cl.map_shared_rank(mine, k)[threadIdx.x];
+    const int64_t at = (int64_t)g * a.db_stride + c;
+    if (a.db_fp32) {
+      float* p = reinterpret_cast<float*>(a.db) + at;
+      *p = a.accumulate ? *p + s : s;
+    } else {
+      uint16_t* p = reinterpret_cast<uint16_t*>(a.db) + at;
+      if (a.accumulate) s += widen(*p, a.bf16);
+      *p = (uint16_t)narrow2(s, 0.f, a.bf16);
+    }
+  }
+  cl.sync();
+}
+
+// Rows of 16-bit values to a pitch that the tile copies can read.
+__global__ void __launch_bounds__(256) lay_out_rows(const uint16_t* __restrict__ src, uint16_t* __restrict__ dst, int64_t rows, int32_t cols, int64_t pitch, int64_t dst_pitch,
+                                                    int64_t matrix_rows, int64_t matrix_stride) {
+  pdl_enter();
+  for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
+    const int64_t w = r / matrix_rows;
+    const uint16_t* s = src + w * matrix_stride + (r - w * matrix_rows) * pitch;
+    uint16_t* d = dst + r * dst_pitch;
+    for (int c = threadIdx.x; c < cols; c += 256) d[c] = s[c];
+  }
+}
+
+// ---- host ----------------------------------------------------------------------------------------------------------------
+constexpr int32_t MAX_FEATURES = 1 << 20;
+constexpr int64_t MAX_ROWS = (1ll << 31) - (1 << 20);
+
+bool tma_ok(const void* p, int64_t pitch) { return ((uintptr_t)p & 15) == 0 && pitch % 8 == 0; }
+int vec_ok(const void* p, int64_t pitch, int64_t stride, int size) {      // four values at once
+  return p && ((uintptr_t)p & (4 * size - 1)) == 0 && pitch % 4 == 0 && stride % 4 == 0;
+}
+
+// A 16-bit matrix, or a stack of them.
+struct Operand {
+  const void* p;
+  int64_t rows, cols, pitch, count, stride;
+};
+bool operand_ok(const Operand& o) { return tma_ok(o.p, o.pitch) && (o.count == 1 || o.stride % 8 == 0); }
+uint64_t laid_out_bytes(const Operand& o) {
+  return operand_ok(o) ? 0 : (uint64_t)(o.rows * o.count * ((o.cols + 7) / 8 * 8)) * 2 + 256;
+}
+
+bool operand_map(CUtensorMap* m, const Operand& o, uint32_t box_rows) {
+  const uint64_t dims[3] = {(uint64_t)o.cols, (uint64_t)o.rows, (uint64_t)o.count};
+  const uint64_t bytes[2] = {(uint64_t)o.pitch * 2, (uint64_t)(o.count == 1 ? o.rows * o.pitch : o.stride) * 2};
+  const uint32_t box[3] = {BK, box_rows, 1};
+  return encode_tensor_map_bf16(m, reinterpret_cast<const uint16_t*>(o.p), 3, dims, bytes, box, 128);
+}
+
+template <class S> cudaError_t allow() { return allow_smem((const void*)dense_gemm<S>, S::SMEM); }
+
+int32_t setup() {      // once per device
+  static std::mutex mutex;
+  static bool done[64] = {false};
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return fail(PS_ERR_CUDA, "no current device");
+  std::lock_guard<std::mutex> lock(mutex);
+  if (done[dev]) return PS_OK;
+  bool ok = configure_tc5_kernels() == 0;
+  const cudaError_t e[] = {allow<Pair<D_FWD, false>>(), allow<Pair<D_FWD, true>>(), allow<Pair<D_DX, false>>(), allow<Pair<D_DW, false>>(), allow<Pair<D_DW, true>>(),
+                           allow<Single<D_FWD, false>>(), allow<Single<D_FWD, true>>(), allow<Single<D_DX, false>>(), allow<Single<D_DW, false>>(), allow<Single<D_DW, true>>(),
+                           allow<Split<D_FWD>>(), allow<Split<D_DX>>(), allow<Split<D_DW>>(),
+                           allow<Few<D_FWD, 16>>(), allow<Few<D_FWD, 32>>(), allow<Few<D_FWD, 64>>(), allow<Few<D_DX, 16>>(), allow<Few<D_DX, 32>>(), allow<Few<D_DX, 64>>()};
+  for (cudaError_t x : e) ok = ok && x == cudaSuccess;
+  if (!ok) return fail(PS_ERR_CUDA, "kernel configuration failed: %s", cudaGetErrorString(cudaGetLastError()));
+  done[dev] = true;
+  return PS_OK;
+}
+
+struct Problem {
+  DenseTab tab;          // merged groups (forward, input gradient) or workers (weight gradient)
+  DenseArgs args;
+  DenseEpi epi;
+  Operand a, b;          // left and right operand of the plain orientation
+  cudaStream_t st;
+};
+
+template <class S>
+int32_t launch(const Problem& p, int split) {
+  DenseMaps maps;
+  const Operand &l = S::FEW ? p.b : p.a, &r = S::FEW ? p.a : p.b;
+  if (!operand_map(&maps.a, l, S::A_MN ? 64 : BM) || !operand_map(&maps.b, r, S::B_MN ? 64 : S::B_ROWS)) return fail(PS_ERR_CUDA, "tensor map");
+  DenseArgs a = p.args;
+  a.idesc = (1u << 4) | (p.epi.bf16 ? (1u << 7) | (1u << 10) : 0u) | (S::A_MN ? 1u << 15 : 0u) | (S::B_MN ? 1u << 16 : 0u) | ((uint32_t)(S::BN >> 3) << 17) |
+            ((uint32_t)(S::TM >> 4) << 24);
+  a.chunk = S::DRAIN ? DRAIN_BLOCKS : 1 << 30;
+  cudaLaunchConfig_t cfg = {};
+  const int walkers = g_sm_count / S::CTAS;
+  cfg.gridDim = S::SPLIT ? dim3(a.n_tiles, 1, split) : dim3(S::CTAS * std::min(a.n_tiles, walkers));
+  cfg.blockDim = dim3(S::THREADS);
+  cfg.dynamicSmemBytes = S::SMEM;
+  cfg.stream = p.st;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = S::CTAS;
+  at[1].val.clusterDim.y = 1;
+  at[1].val.clusterDim.z = S::SPLIT ? split : 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 2;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, dense_gemm<S>, maps, a, p.epi, p.tab);
+  return e == cudaSuccess ? PS_OK : fail(PS_ERR_CUDA, "dense layer launch: %s", cudaGetErrorString(e));
+}
+
+// Tiles of `tm` rows (of every group) x `bn` columns; fills the prefix sums.
+int64_t count_tiles(DenseTab& tab, int tm, int64_t n_tiles_n) {
+  int64_t t = 0;
+  for (int g = 0; g < tab.groups; ++g) {
+    tab.tile0[g] = (int32_t)std::min<int64_t>(t, 1ll << 30);
+    t += (int64_t)((tab.row0[g + 1] - tab.row0[g] + tm - 1) / tm) * n_tiles_n;
+  }
+  tab.tile0[tab.groups] = (int32_t)std::min<int64_t>(t, 1ll << 30);
+  return t;
+}
+int64_t padded_rows(const DenseTab& tab, int tm) {
+  int64_t t = 0;
+  for (int g = 0; g < tab.groups; ++g) t += (int64_t)((tab.row0[g + 1] - tab.row0[g] + tm - 1) / tm) * tm;
+  return t;
+}
+int div_up(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
+
+// CTAs that share a tile's blocks of k: as many as the chip has room for, at least two blocks each.
+int split_for(int64_t tiles, int blocks, int room) {
+  int split = 1;
+  while (split < 8 && tiles * split * 2 <= room && blocks >= split * 4) split *= 2;
+  return split;
+}
+
+// Forward and input gradient: rows of groups x `features` columns, reduction over `red`.
+template <int OP>
+int32_t run_rows(Problem& p, int features, int red, bool fp32_out) {
+  DenseTab& tab = p.tab;
+  int used = 0, most = 0;
+  for (int g = 0; g < tab.groups; ++g) {
+    const int r = tab.row0[g + 1] - tab.row0[g];
+    used += r > 0;
+    most = std::max(most, r);
+  }
+  const int64_t rows = tab.row0[tab.groups];
+  const int blocks = div_up(red, BK), sms = g_sm_count;
+  DenseArgs& a = p.args;
+  a.n_side = features;
+  a.red = red;
+  auto tiles_fit = [&](int64_t t) { return t < (1 << 30); };
+  if (rows <= 48ll * used) {
+    const int bn = most <= 16 ? 16 : (most <= 32 ? 32 : 64);
+    a.n_tiles_n = div_up(features, BM);
+    const int64_t t = count_tiles(tab, bn, a.n_tiles_n);
+    if (!tiles_fit(t)) return fail(PS_ERR_BAD_ARG, "too many tiles");
+    a.n_tiles = (int)t;
+    const int split = split_for(t, blocks, 2 * sms);
+    if (bn == 16) return launch<Few<OP, 16>>(p, split);
+    if (bn == 32) return launch<Few<OP, 32>>(p, split);
+    return launch<Few<OP, 64>>(p, split);
+  }
+  a.n_tiles_n = div_up(features, 256);
+  const int64_t pairs = count_tiles(tab, 256, a.n_tiles_n);
+  if (!tiles_fit(pairs * 2)) return fail(PS_ERR_BAD_ARG, "too many tiles");
+  if (pairs * 2 >= sms && padded_rows(tab, 256) * 5 <= padded_rows(tab, 128) * 6) {
+    a.n_tiles = (int)pairs;
+    if constexpr (OP == D_FWD) if (fp32_out) return launch<Pair<OP, true>>(p, 1);
+    return launch<Pair<OP, false>>(p, 1);
+  }
+  const int64_t singles = count_tiles(tab, 128, a.n_tiles_n);
+  if (singles * 3 >= sms * 2) {
+    a.n_tiles = (int)singles;
+    if constexpr (OP == D_FWD) if (fp32_out) return launch<Single<OP, true>>(p, 1);
+    return launch<Single<OP, false>>(p, 1);
+  }
+  a.n_tiles_n = div_up(features, 128);
+  a.n_tiles = (int)count_tiles(tab, 128, a.n_tiles_n);
+  return launch<Split<OP>>(p, split_for(a.n_tiles, blocks, sms));
+}
+
+int32_t run_weights(Problem& p, int N, int K, bool fp32_out) {
+  DenseTab& tab = p.tab;
+  DenseArgs& a = p.args;
+  int most = 0;
+  for (int g = 0; g < tab.groups; ++g) most = std::max(most, tab.row0[g + 1] - tab.row0[g]);
+  const int sms = g_sm_count;
+  a.m_side = N; a.n_side = K; a.red = 0;
+  a.n_tiles_n = div_up(K, 256);
+  auto tiles = [&](int tm) { a.m_tiles = div_up(N, tm); return (int64_t)tab.groups * a.m_tiles * a.n_tiles_n; };
+  const int64_t pairs = tiles(256), singles = tiles(128);
+  if (singles >= 1 << 30) return fail(PS_ERR_BAD_ARG, "too many tiles");
+  if (pairs * 2 >= sms && pairs * 2 <= singles + singles / 5) {
+    a.n_tiles = (int)tiles(256);
+    return fp32_out ? launch<Pair<D_DW, true>>(p, 1) : launch<Pair<D_DW, false>>(p, 1);
+  }
+  if (singles * 3 >= sms * 2) {
+    a.n_tiles = (int)tiles(128);
+    return fp32_out ? launch<Single<D_DW, true>>(p, 1) : launch<Single<D_DW, false>>(p, 1);
+  }
+  a.n_tiles_n = div_up(K, 128);
+  a.n_tiles = (int)tiles(128);
+  return launch<Split<D_DW>>(p, split_for(a.n_tiles, div_up(most, BK), sms));
+}
+
+// Groups with the same weights one after another are one group: their rows lie together.
+void merge_groups(const int32_t* rows, const int32_t* weight_of, int groups, DenseTab& tab) {
+  tab.groups = 0;
+  int at = 0;
+  for (int g = 0; g < groups; ++g) {
+    if (rows[g] == 0) continue;
+    const uint16_t w = (uint16_t)(weight_of ? weight_of[g] : g);
+    if (tab.groups == 0 || tab.w[tab.groups - 1] != w) {
+      tab.row0[tab.groups] = at;
+      tab.w[tab.groups++] = w;
+    }
+    at += rows[g];
+    tab.row0[tab.groups] = at;
+  }
+}
+
+int32_t check_layer(const ps_dense_layer* l, int64_t* rows_out) {
+  if (!l) return fail(PS_ERR_BAD_ARG, "NULL argument");
+  if (l->groups < 1 || l->groups > PS_MAX_WORKERS || !l->rows) return fail(PS_ERR_BAD_ARG, "groups must be 1..%d, with rows", PS_MAX_WORKERS);
+  if (l->n_weights < 1 || l->n_weights > 65535) return fail(PS_ERR_BAD_ARG, "n_weights must be 1..65535");
+  if (l->type != PS_TYPE_BF16 && l->type != PS_TYPE_FP16) return fail(PS_ERR_BAD_ARG, "type must be PS_TYPE_BF16 or PS_TYPE_FP16");
+  if (l->in_features < 1 || l->in_features > MAX_FEATURES || l->out_features < 1 || l->out_features > MAX_FEATURES)
+    return fail(PS_ERR_BAD_ARG, "in_features and out_features must be 1..%d", MAX_FEATURES);
+  if (l->activation < PS_ACT_NONE || l->activation > PS_ACT_SILU) return fail(PS_ERR_BAD_ARG, "unknown activation %d", l->activation);
+  int64_t rows = 0;
+  for (int g = 0; g < l->groups; ++g) {
+    if (l->rows[g] < 0) return fail(PS_ERR_BAD_ARG, "group %d has %d rows", g, l->rows[g]);
+    const int32_t w = l->weight_of ? l->weight_of[g] : g;
+    if (w < 0 || w >= l->n_weights) return fail(PS_ERR_BAD_ARG, "group %d holds weights %d of %d", g, w, l->n_weights);
+    rows += l->rows[g];
+  }
+  if (rows > MAX_ROWS) return fail(PS_ERR_BAD_ARG, "%lld rows are too many", (long long)rows);
+  if (!l->weight || l->weight_pitch < l->in_features || (l->n_weights > 1 && l->weight_stride < (int64_t)(l->out_features - 1) * l->weight_pitch + l->in_features))
+    return fail(PS_ERR_BAD_ARG, "weight is NULL, or its pitch or stride is too small");
+  if (rows > 0 && (!l->x || l->x_pitch < l->in_features)) return fail(PS_ERR_BAD_ARG, "x is NULL or its pitch is too small");
+  if (((uintptr_t)l->weight | (uintptr_t)l->x) & 1) return fail(PS_ERR_BAD_ARG, "an operand is not aligned to its type");
+  *rows_out = rows;
+  return PS_OK;
+}
+// An optional matrix of `size`-byte elements.
+int32_t check_matrix(const char* name, const void* p, int64_t pitch, int64_t cols, int size) {
+  if (p && (pitch < cols || ((uintptr_t)p & (size - 1)))) return fail(PS_ERR_BAD_ARG, "%s: its pitch is too small, or it is not aligned to its type", name);
+  return PS_OK;
+}
+
+Operand weight_operand(const ps_dense_layer* l) { return Operand{l->weight, l->out_features, l->in_features, l->weight_pitch, l->n_weights, l->weight_stride}; }
+Operand row_operand(const void* p, int64_t rows, int64_t cols, int64_t pitch) {
+  return Operand{p, rows, cols, rows == 1 ? (cols + 7) / 8 * 8 : pitch, 1, 0};      // one row: there is no pitch to obey
+}
+
+struct Layout {      // hands out the workspace
+  uint8_t* at;
+  uint64_t left;
+};
+int32_t lay_out(Operand& o, Layout& ws, cudaStream_t st) {
+  if (operand_ok(o)) return PS_OK;
+  const uint64_t need = laid_out_bytes(o);
+  if (!ws.at || ws.left < need) return fail(PS_ERR_ARENA_TOO_SMALL, "an operand has to be laid out anew (its base is not on 16 bytes or its pitch no multiple of 8): %llu more bytes of workspace needed", (unsigned long long)need);
+  uint16_t* d = reinterpret_cast<uint16_t*>(((uintptr_t)ws.at + 255) & ~(uintptr_t)255);
+  const int64_t pitch = (o.cols + 7) / 8 * 8, rows = o.rows * o.count;
+  launch_pdl(lay_out_rows, dim3((unsigned)std::min<int64_t>(rows, 148 * 16)), 256, 0, st, reinterpret_cast<const uint16_t*>(o.p), d, rows, (int32_t)o.cols, o.pitch, pitch, o.rows, o.stride);
+  if (cudaGetLastError() != cudaSuccess) return fail(PS_ERR_CUDA, "operand copy launch");
+  ws.at += need;
+  ws.left -= need;
+  o = Operand{d, o.rows, o.cols, pitch, o.count, o.rows * pitch};
+  return PS_OK;
+}
+
+}  // namespace
+
+}  // namespace psk
+
+using namespace psk;
+
+extern "C" {
+
+int32_t workers_dense_workspace(const ps_dense_layer* l, const void* dy, int64_t dy_pitch, uint64_t* bytes) {
+  int64_t rows = 0;
+  int32_t rc = check_layer(l, &rows);
+  if (rc != PS_OK) return rc;
+  if (!bytes) return fail(PS_ERR_BAD_ARG, "NULL argument");
+  *bytes = 0;
+  if (rows == 0) return PS_OK;
+  *bytes = laid_out_bytes(weight_operand(l)) + laid_out_bytes(row_operand(l->x, rows, l->in_features, l->x_pitch));
+  if (dy) *bytes += laid_out_bytes(row_operand(dy, rows, l->out_features, dy_pitch));
+  return PS_OK;
+}
+
+int32_t workers_dense_status(void* stream) {
+  uint32_t word = 0, zero = 0;
+  cudaError_t e = cudaMemcpyFromSymbolAsync(&word, g_dense_status, sizeof(word), 0, cudaMemcpyDeviceToHost, (cudaStream_t)stream);
+  if (e == cudaSuccess) e = cudaMemcpyToSymbolAsync(g_dense_status, &zero, sizeof(zero), 0, cudaMemcpyHostToDevice, (cudaStream_t)stream);
+  if (e == cudaSuccess) e = cudaStreamSynchronize((cudaStream_t)stream);
+  if (e != cudaSuccess) return fail(PS_ERR_CUDA, "workers_dense_status: %s", cudaGetErrorString(e));
+  return word == 0 ? PS_OK : fail(PS_ERR_DEVICE_STATUS, "a bounded wait in a dense-layer kernel gave up: results since the last call are not to be used");
+}
+
+int32_t workers_dense_forward(const ps_dense_layer* l, const ps_dense_output* o) {
+  int64_t rows = 0;
+  int32_t rc = check_layer(l, &rows);
+  if (rc != PS_OK) return rc;
+  if (!o) return fail(PS_ERR_BAD_ARG, "NULL argument");
+  const int N = l->out_features, K = l->in_features;
+  if (o->y_type != l->type && o->y_type != PS_TYPE_FP32) return fail(PS_ERR_BAD_ARG, "y_type must be the operands' type or PS_TYPE_FP32");
+  const int ys = o->y_type == PS_TYPE_FP32 ? 4 : 2;
+  if (rows > 0 && !o->y) return fail(PS_ERR_BAD_ARG, "y is NULL");
+  if ((rc = check_matrix("y", o->y, o->y_pitch, N, ys)) != PS_OK || (rc = check_matrix("pre", o->pre, o->pre_pitch, N, 2)) != PS_OK ||
+      (rc = check_matrix("residual", o->residual, o->residual_pitch, N, 2)) != PS_OK ||
+      (rc = check_matrix("bias", o->bias, l->n_weights > 1 ? o->bias_stride : N, N, 2)) != PS_OK)
+    return rc;
+  if (rows == 0) return PS_OK;
+  if ((rc = setup()) != PS_OK) return rc;
+  Problem p = {};
+  p.st = (cudaStream_t)l->stream;
+  p.a = row_operand(l->x, rows, K, l->x_pitch);
+  p.b = weight_operand(l);
+  Layout ws = {(uint8_t*)l->workspace, l->workspace_bytes};
+  if ((rc = lay_out(p.a, ws, p.st)) != PS_OK || (rc = lay_out(p.b, ws, p.st)) != PS_OK) return rc;
+  merge_groups(l->rows, l->weight_of, l->groups, p.tab);
+  DenseEpi& e = p.epi;
+  e.in0 = o->bias; e.in0_stride = o->bias_stride; e.v_in0 = vec_ok(o->bias, 0, l->n_weights > 1 ? o->bias_stride : 0, 2);
+  e.in1 = o->residual; e.in1_pitch = o->residual_pitch; e.v_in1 = vec_ok(o->residual, o->residual_pitch, 0, 2);
+  e.out0 = o->y; e.out0_pitch = o->y_pitch; e.v_out0 = vec_ok(o->y, o->y_pitch, 0, ys); e.out0_fp32 = ys == 4;
+  e.out1 = o->pre; e.out1_pitch = o->pre_pitch; e.v_out1 = vec_ok(o->pre, o->pre_pitch, 0, 2);
+  e.act = l->activation; e.bf16 = l->type == PS_TYPE_BF16;
+  return run_rows<D_FWD>(p, N, K, ys == 4);
+}
+
+int32_t workers_dense_backward(const ps_dense_layer* l, const ps_dense_gradients* o) {
+  int64_t rows = 0;
+  int32_t rc = check_layer(l, &rows);
+  if (rc != PS_OK) return rc;
+  if (!o) return fail(PS_ERR_BAD_ARG, "NULL argument");
+  const int N = l->out_features, K = l->in_features;
+  if (o->dw_type != l->type && o->dw_type != PS_TYPE_FP32) return fail(PS_ERR_BAD_ARG, "dw_type must be the operands' type or PS_TYPE_FP32");
+  if (o->accumulate != 0 && o->accumulate != 1) return fail(PS_ERR_BAD_ARG, "accumulate must be 0 or 1");
+  const int ds = o->dw_type == PS_TYPE_FP32 ? 4 : 2;
+  if (rows > 0 && !o->dy) return fail(PS_ERR_BAD_ARG, "dy is NULL");
+  if (o->dx_pre && !o->x_pre && rows > 0) return fail(PS_ERR_BAD_ARG, "dx_pre needs x_pre");
+  if ((rc = check_matrix("dy", o->dy, o->dy_pitch, N, 2)) != PS_OK || (rc = check_matrix("x_pre", o->x_pre, o->x_pre_pitch, K, 2)) != PS_OK ||
+      (rc = check_matrix("dx_add", o->dx_add, o->dx_add_pitch, K, 2)) != PS_OK || (rc = check_matrix("dx", o->dx, o->dx_pitch, K, 2)) != PS_OK ||
+      (rc = check_matrix("dx_pre", o->dx_pre, o->dx_pre_pitch, K, 2)) != PS_OK || (rc = check_matrix("dw", o->dw, o->dw_pitch, K, ds)) != PS_OK ||
+      (rc = check_matrix("dw", o->dw, l->groups > 1 ? o->dw_stride : (int64_t)N * o->dw_pitch, (int64_t)(N - 1) * o->dw_pitch + K, ds)) != PS_OK ||
+      (rc = check_matrix("db", o->db, l->groups > 1 ? o->db_stride : N, N, ds)) != PS_OK)
+    return rc;
+  if ((rc = setup()) != PS_OK) return rc;
+  cudaStream_t st = (cudaStream_t)l->stream;
+  Operand x = row_operand(l->x, rows, K, l->x_pitch), dy = row_operand(o->dy, rows, N, o->dy_pitch), w = weight_operand(l);
+  Layout ws = {(uint8_t*)l->workspace, l->workspace_bytes};
+  if (rows > 0) {
+    const bool want_x = o->dw != nullptr, want_w = o->dx || o->dx_pre;
+    if ((want_x || want_w) && (rc = lay_out(dy, ws, st)) != PS_OK) return rc;
+    if (want_x && (rc = lay_out(x, ws, st)) != PS_OK) return rc;
+    if (want_w && (rc = lay_out(w, ws, st)) != PS_OK) return rc;
+  } else {      // nobody has a row: the gradients are zero
+    cudaError_t ce = cudaSuccess;
+    for (int g = 0; g < l->groups && !o->accumulate && ce == cudaSuccess; ++g) {
+      if (o->dw) ce = cudaMemset2DAsync((uint8_t*)o->dw + (int64_t)g * o->dw_stride * ds, (size_t)o->dw_pitch * ds, 0, (size_t)K * ds, (size_t)N, st);
+      if (o->db && ce == cudaSuccess) ce = cudaMemsetAsync((uint8_t*)o->db + (int64_t)g * o->db_stride * ds, 0, (size_t)N * ds, st);
+    }
+    return ce == cudaSuccess ? PS_OK : fail(PS_ERR_CUDA, "clearing gradients: %s", cudaGetErrorString(ce));
+  }
+  DenseTab workers = {};
+  workers.groups = l->groups;
+  for (int g = 0; g < l->groups; ++g) {
+    workers.w[g] = (uint16_t)g;
+    workers.row0[g + 1] = workers.row0[g] + l->rows[g];
+  }
+  if (o->db) {
+    ColumnSumArgs c = {};
+    c.dy = o->dy; c.db = o->db; c.pitch = o->dy_pitch; c.db_stride = o->db_stride;
+    c.N = N; c.bf16 = l->type == PS_TYPE_BF16; c.db_fp32 = ds == 4; c.accumulate = o->accumulate;
+    c.vec = ((uintptr_t)o->dy & 15) == 0 && o->dy_pitch % 8 == 0;
+    const int blocks = div_up(N, 64) * l->groups;
+    int split = 1;
+    while (split < 8 && blocks * split < 4 * g_sm_count && rows / l->groups >= 64 * split) split *= 2;
+    launch_cluster(column_sums, dim3((unsigned)div_up(N, 64), (unsigned)l->groups, (unsigned)split), CSUM_TPB, 0, split, st, c, workers);
+    if (cudaGetLastError() != cudaSuccess) return fail(PS_ERR_CUDA, "column sum launch");
+  }
+  if (o->dx || o->dx_pre) {
+    Problem p = {};
+    p.st = st;
+    p.a = dy;
+    p.b = w;
+    merge_groups(l->rows, l->weight_of, l->groups, p.tab);
+    DenseEpi& e = p.epi;
+    e.in1 = o->dx_add; e.in1_pitch = o->dx_add_pitch; e.v_in1 = vec_ok(o->dx_add, o->dx_add_pitch, 0, 2);
+    e.in2 = o->x_pre; e.in2_pitch = o->x_pre_pitch; e.v_in2 = vec_ok(o->x_pre, o->x_pre_pitch, 0, 2);
+    e.out0 = o->dx; e.out0_pitch = o->dx_pitch; e.v_out0 = vec_ok(o->dx, o->dx_pitch, 0, 2);
+    e.out1 = o->dx_pre; e.out1_pitch = o->dx_pre_pitch; e.v_out1 = vec_ok(o->dx_pre, o->dx_pre_pitch, 0, 2);
+    e.act = l->activation; e.bf16 = l->type == PS_TYPE_BF16;
+      if ((rc = run_rows<D_DX>(p, K, N, false)) != PS_OK) return rc;
+  }
+  if (o->dw) {
+    Problem p = {};
+    p.st = st;
+    p.a = dy;
+    p.b = x;
+    p.tab = workers;
+    DenseEpi& e = p.epi;
+    e.out0 = o->dw; e.out0_pitch = o->dw_pitch; e.out0_stride = o->dw_stride; e.out0_fp32 = ds == 4; e.accumulate = o->accumulate;
+    e.v_out0 = vec_ok(o->dw, o->dw_pitch, l->groups > 1 ? o->dw_stride : 0, ds);
+    e.bf16 = l->type == PS_TYPE_BF16;
+      if ((rc = run_weights(p, N, K, ds == 4)) != PS_OK) return rc;
+  }
+  return PS_OK;
+}
+
+}  // extern "C"

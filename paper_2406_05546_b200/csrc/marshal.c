@@ -24,6 +24,8 @@ static int32_t (*f_apply_stale)(ps_ctx*, ps_mode, float, float, const int32_t*, 
 static int32_t (*f_apply_summed)(ps_ctx*, const float*, int32_t, float, float, ps_apply_result*);
 static int32_t (*f_apply_adamw)(ps_ctx*, ps_mode, const ps_adamw_hyper*, double, float*, float*, float, const int32_t*, float, ps_apply_result*);
 static int32_t (*f_adamw_step)(ps_adamw*, const ps_adamw_hyper*);
+static int32_t (*f_dense_forward)(const ps_dense_layer*, const ps_dense_output*);
+static int32_t (*f_dense_backward)(const ps_dense_layer*, const ps_dense_gradients*);
 static const char* (*f_error)(ps_ctx*);
 static PyObject *snapshot_type, *error_type;
 static PyObject *as_array;       /* as_array(object, kind): numpy's conversion to a contiguous array */
@@ -159,7 +161,8 @@ static PyObject* bind(PyObject* m, PyObject* const* a, Py_ssize_t nargs) {
       {"ps_pull_snapshot", (void**)&f_pull}, {"ps_queue_reserve", (void**)&f_reserve}, {"workers_grad_step", (void**)&f_grad},
       {"workers_grad_step_summed", (void**)&f_summed}, {"workers_eval", (void**)&f_eval}, {"ps_enqueue", (void**)&f_enqueue},
       {"ps_apply", (void**)&f_apply}, {"ps_apply_stale", (void**)&f_apply_stale}, {"ps_apply_summed", (void**)&f_apply_summed}, {"ps_last_error", (void**)&f_error},
-      {"ps_apply_adamw", (void**)&f_apply_adamw}, {"ps_adamw_step", (void**)&f_adamw_step}};
+      {"ps_apply_adamw", (void**)&f_apply_adamw}, {"ps_adamw_step", (void**)&f_adamw_step},
+      {"workers_dense_forward", (void**)&f_dense_forward}, {"workers_dense_backward", (void**)&f_dense_backward}};
   for (size_t i = 0; i < sizeof(table) / sizeof(table[0]); ++i) {
     PyObject* addr = PyDict_GetItemString(a[0], table[i].name);
     if (!addr) { PyErr_SetString(PyExc_KeyError, table[i].name); return NULL; }
@@ -385,9 +388,100 @@ static PyObject* adamw_step(PyObject* m, PyObject* const* a, Py_ssize_t nargs) {
   Py_RETURN_NONE;
 }
 
+/* A list or tuple of integers, or anything else that holds int32, one per group. */
+static int group_ints(PyObject* o, int32_t* out, Py_ssize_t* n) {
+  if (PyList_CheckExact(o) || PyTuple_CheckExact(o)) {
+    const Py_ssize_t len = PySequence_Fast_GET_SIZE(o);
+    Py_ssize_t i = 0;
+    for (; i < len && i < PS_MAX_WORKERS; ++i) {
+      const long v = PyLong_AsLong(PySequence_Fast_GET_ITEM(o, i));
+      if (v == -1 && PyErr_Occurred()) return -1;
+      if (v != (int32_t)v) { PyErr_SetString(PyExc_OverflowError, "an int32 is wanted"); return -1; }
+      out[i] = (int32_t)v;
+    }
+    *n = len;
+    return 0;
+  }
+  Py_buffer b;
+  if (array(o, &b, I32)) return -1;
+  *n = b.len / 4;
+  memcpy(out, b.buf, (size_t)(*n < PS_MAX_WORKERS ? *n : PS_MAX_WORKERS) * 4);
+  done(&b);
+  return 0;
+}
+static int as_i64(PyObject* o, int64_t* v) { return as_u64(o, (uint64_t*)v); }
+
+/* rows, weight_of | None, n_weights, in_features, out_features, type, activation, x, x_pitch, weight, weight_pitch, weight_stride, workspace | None,
+ * workspace_bytes, stream: a[0] .. a[14] */
+#define LAYER_ARGS 15
+static int layer(PyObject* const* a, ps_dense_layer* l, int32_t* rows, int32_t* weights) {
+  Py_ssize_t n, nw;
+  memset(l, 0, sizeof(*l));
+  if (a[0] == Py_None) { PyErr_SetString(PyExc_TypeError, "rows are wanted"); return -1; }
+  if (group_ints(a[0], rows, &n)) return -1;
+  l->groups = n > PS_MAX_WORKERS ? PS_MAX_WORKERS + 1 : (int32_t)n;      /* more than that the library refuses */
+  l->rows = rows;
+  if (a[1] != Py_None) {
+    if (group_ints(a[1], weights, &nw)) return -1;
+    if (nw != n) { PyErr_SetString(PyExc_ValueError, "weight_of: one snapshot per group is wanted"); return -1; }
+    l->weight_of = weights;
+  }
+  void *x, *w, *ws, *st;
+  if (i32(a[2], &l->n_weights) || i32(a[3], &l->in_features) || i32(a[4], &l->out_features) || i32(a[5], &l->type) || i32(a[6], &l->activation) ||
+      as_ptr(a[7], &x) || as_i64(a[8], &l->x_pitch) || as_ptr(a[9], &w) || as_i64(a[10], &l->weight_pitch) || as_i64(a[11], &l->weight_stride) ||
+      as_ptr(a[12], &ws) || as_u64(a[13], &l->workspace_bytes) || as_ptr(a[14], &st))
+    return -1;
+  l->x = x; l->weight = w; l->workspace = ws; l->stream = st;
+  return 0;
+}
+
+/* (layer..., bias, bias_stride, residual, residual_pitch, y, y_pitch, y_type, pre, pre_pitch) */
+static PyObject* dense_forward(PyObject* m, PyObject* const* a, Py_ssize_t nargs) {
+  WANT(LAYER_ARGS + 9)
+  ps_dense_layer l;
+  ps_dense_output o;
+  int32_t rows[PS_MAX_WORKERS], weights[PS_MAX_WORKERS];
+  if (layer(a, &l, rows, weights)) return NULL;
+  a += LAYER_ARGS;
+  memset(&o, 0, sizeof(o));
+  void *bias, *residual;
+  if (as_ptr(a[0], &bias) || as_i64(a[1], &o.bias_stride) || as_ptr(a[2], &residual) || as_i64(a[3], &o.residual_pitch) || as_ptr(a[4], &o.y) ||
+      as_i64(a[5], &o.y_pitch) || i32(a[6], &o.y_type) || as_ptr(a[7], &o.pre) || as_i64(a[8], &o.pre_pitch))
+    return NULL;
+  o.bias = bias; o.residual = residual;
+  int32_t rc;
+  CALL(f_dense_forward(&l, &o))
+  if (rc) return raise(rc);
+  Py_RETURN_NONE;
+}
+
+/* (layer..., dy, dy_pitch, dx_add, dx_add_pitch, x_pre, x_pre_pitch, dx, dx_pitch, dx_pre, dx_pre_pitch, dw, dw_pitch, dw_stride, db, db_stride, dw_type,
+ * accumulate) */
+static PyObject* dense_backward(PyObject* m, PyObject* const* a, Py_ssize_t nargs) {
+  WANT(LAYER_ARGS + 17)
+  ps_dense_layer l;
+  ps_dense_gradients o;
+  int32_t rows[PS_MAX_WORKERS], weights[PS_MAX_WORKERS];
+  if (layer(a, &l, rows, weights)) return NULL;
+  a += LAYER_ARGS;
+  memset(&o, 0, sizeof(o));
+  void *dy, *add, *pre;
+  if (as_ptr(a[0], &dy) || as_i64(a[1], &o.dy_pitch) || as_ptr(a[2], &add) || as_i64(a[3], &o.dx_add_pitch) || as_ptr(a[4], &pre) ||
+      as_i64(a[5], &o.x_pre_pitch) || as_ptr(a[6], &o.dx) || as_i64(a[7], &o.dx_pitch) || as_ptr(a[8], &o.dx_pre) || as_i64(a[9], &o.dx_pre_pitch) ||
+      as_ptr(a[10], &o.dw) || as_i64(a[11], &o.dw_pitch) || as_i64(a[12], &o.dw_stride) || as_ptr(a[13], &o.db) || as_i64(a[14], &o.db_stride) ||
+      i32(a[15], &o.dw_type) || i32(a[16], &o.accumulate))
+    return NULL;
+  o.dy = dy; o.dx_add = add; o.x_pre = pre;
+  int32_t rc;
+  CALL(f_dense_backward(&l, &o))
+  if (rc) return raise(rc);
+  Py_RETURN_NONE;
+}
+
 #define FAST(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, NULL}
 static PyMethodDef methods[] = {FAST(bind), FAST(pull), FAST(reserve), FAST(grad_step), FAST(grad_step_summed), FAST(eval),
-                                FAST(enqueue), FAST(apply), FAST(apply_stale), FAST(apply_summed), FAST(apply_adamw), FAST(adamw_step), {NULL, NULL, 0, NULL}};
+                                FAST(enqueue), FAST(apply), FAST(apply_stale), FAST(apply_summed), FAST(apply_adamw), FAST(adamw_step),
+                                FAST(dense_forward), FAST(dense_backward), {NULL, NULL, 0, NULL}};
 static struct PyModuleDef def = {PyModuleDef_HEAD_INIT, "_marshal", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
 PyMODINIT_FUNC PyInit__marshal(void) {

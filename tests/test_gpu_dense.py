@@ -1,0 +1,439 @@
+"""The workers' dense layer, forward and backward, against float64: ragged groups, shared and own weights, every tile shape, strides, odd sizes,
+values that are not finite, and what must be left alone."""
+import ctypes as C
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2406_05546_b200 import ps
+from paper_2406_05546_b200.ps import AdamW, workers_dense_backward, workers_dense_forward, workers_dense_status
+
+gpu = pytest.mark.gpu
+TYPES = {"bf16": torch.bfloat16, "fp16": torch.float16}
+
+
+def act(z, kind):
+    if kind == "relu":
+        return torch.where(z < 0, 0.0, z)
+    if kind == "gelu":
+        return z * 0.5 * torch.special.erfc(-z / math.sqrt(2))
+    if kind == "silu":
+        return z / (1 + torch.exp(-z))
+    return z
+
+
+def slope(z, kind):
+    if kind == "relu":
+        return (z > 0).double()
+    if kind == "gelu":
+        return 0.5 * torch.special.erfc(-z / math.sqrt(2)) + z * torch.exp(-z * z / 2) / math.sqrt(2 * math.pi)
+    if kind == "silu":
+        s = 1 / (1 + torch.exp(-z))
+        return s * (1 + z * (1 - s))
+    return torch.ones_like(z)
+
+
+def matrix(gen, rows, cols, kind, pad=0, scale=1.0, extra=0):
+    """[rows + extra, cols] inside a wider buffer whose other values are 77 (extra rows too)."""
+    buf = torch.full((rows + extra, cols + pad), 77, dtype=kind, device="cuda")
+    buf[:rows, :cols] = (torch.randn(rows, cols, generator=gen, device="cuda") * scale).to(kind)
+    return buf, buf[:, :cols]
+
+
+def untouched(buf, rows, cols):
+    return bool((buf[rows:] == 77).all() and (buf[:, cols:] == 77).all())
+
+
+def spans(rows):
+    at = 0
+    for g, n in enumerate(rows):
+        yield g, slice(at, at + n)
+        at += n
+
+
+def sum_error(terms, length, drained):
+    """Largest error of a sum of `length` exact products with absolute sum `terms`: an accumulator takes sixteen products at a time and drops less than
+    2^-22 of what it holds each time (FP32 results: 32 times at most, then one rounded addition per 512 and per CTA of a cluster)."""
+    n = length / 16 + 2
+    if drained:
+        n = min(n, 34) + length / 512 + 10
+    return n * 2.0 ** -22 * terms
+
+
+def half_step(v, kind):
+    """Half the distance of neighbouring values, subnormal ones included."""
+    f = torch.finfo(kind)
+    return v.abs() * f.eps / 2 + f.smallest_normal * f.eps / 2
+
+
+# one row each; few rows; ragged with empty groups; one large batch; many single tiles; rows past every tile border
+SHAPES = [
+    ([1], 1, None, 40, 24),
+    ([3, 0, 1, 2], 4, None, 1568, 512),
+    ([16, 17, 1, 30], 2, [0, 1, 1, 0], 200, 136),
+    ([33, 64, 40], 3, None, 328, 264),
+    ([100, 0, 129, 65, 0], 5, None, 136, 200),
+    ([128, 129], 1, [0, 0], 520, 128),
+    ([300, 257, 511, 90, 700], 2, [0, 0, 1, 1, 0], 96, 1040),
+    ([128] * 40, 8, [g % 8 for g in range(40)], 72, 520),
+    ([2600], 1, None, 136, 2056),
+    ([1000, 0, 1800], 2, [1, 0, 0], 648, 2048),
+]
+
+
+def one_forward(shape, kind, activation, bias, residual, pre, out32, seed=0, pad=(8, 8, 8, 8), extra=0, scale=1.0):
+    rows, n_weights, weight_of, K, N = shape
+    t, M = TYPES[kind], sum(rows)
+    gen = torch.Generator("cuda").manual_seed(seed)
+    _, x = matrix(gen, M, K, t, pad[0], scale, extra)
+    wbuf = torch.full((n_weights, N, K + pad[1]), 77, dtype=t, device="cuda")
+    wbuf[:, :, :K] = (torch.randn(n_weights, N, K, generator=gen, device="cuda") / math.sqrt(K)).to(t)
+    w = wbuf[:, :, :K]
+    b = torch.randn(n_weights, N, generator=gen, device="cuda").to(t) if bias else None
+    _, r = matrix(gen, M, N, t, pad[2]) if residual else (None, None)
+    ybuf, y = matrix(gen, M, N, torch.float32 if out32 else t, pad[3], extra=extra)
+    pbuf, p = matrix(gen, M, N, t, pad[3], extra=extra) if pre else (None, None)
+    assert workers_dense_forward(x, w, rows, weight_of, b, r, activation, y, p) is y
+    workers_dense_status()
+    assert untouched(ybuf, M, N) and (pbuf is None or untouched(pbuf, M, N))
+    for g, s in spans(rows):
+        k = weight_of[g] if weight_of else g
+        z = x[s].double() @ w[k].double().T
+        e = sum_error(x[s].double().abs() @ w[k].double().abs().T, K, out32)
+        if bias:
+            z = z + b[k].double()
+        e = e + z.abs() * 2.0 ** -23
+        if pre:
+            assert ((p[s].double() - z).abs() <= e + half_step(z.abs() + e, t)).all(), (g, "pre")
+        v = act(z, activation)
+        e = e * 1.2 + v.abs() * 2.0 ** -20 + 2.0 ** -24 * z.abs()      # |act'| <= 1.13; erf and exp within a few units in the last place
+        if residual:
+            v = v + r[s].double()
+            e = e + v.abs() * 2.0 ** -23
+        limit = e + (half_step(v.abs() + e, t) if not out32 else v.abs() * 2.0 ** -23)
+        assert ((y[s].double() - v).abs() <= limit).all(), (g, float(((y[s].double() - v).abs() / limit).max()))
+
+
+@gpu
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: f"{len(s[0])}x{sum(s[0])}-{s[3]}-{s[4]}")
+@pytest.mark.parametrize("kind,activation,bias,residual,pre,out32", [
+    ("bf16", "none", False, False, False, False), ("bf16", "relu", True, False, True, False), ("fp16", "gelu", True, True, True, False),
+    ("bf16", "silu", False, True, False, True), ("fp16", "none", True, False, False, True)])
+def test_forward(shape, kind, activation, bias, residual, pre, out32):
+    one_forward(shape, kind, activation, bias, residual, pre, out32)
+
+
+@gpu
+@pytest.mark.parametrize("shape", [([5, 1, 9], 3, None, 37, 51), ([130, 70], 1, [0, 0], 1, 3), ([2600], 1, None, 129, 2051), ([1], 1, None, 7, 1), ([300, 1], 2, None, 65, 9)],
+                         ids=lambda s: f"{len(s[0])}x{sum(s[0])}-{s[3]}-{s[4]}")
+@pytest.mark.parametrize("pad", [(0, 0, 0, 0), (1, 2, 3, 5)])
+@pytest.mark.parametrize("out32", [False, True])
+def test_forward_odd_sizes_and_pitches(shape, pad, out32):
+    one_forward(shape, "bf16", "gelu", True, True, True, out32, pad=pad, extra=3)
+
+
+@gpu
+@pytest.mark.parametrize("K", [4096, 16000])
+@pytest.mark.parametrize("rows", [[2], [70], [2600]])
+def test_forward_long_sums(K, rows):
+    one_forward((rows, 1, None, K, 2048), "bf16", "none", True, False, True, True)
+
+
+def one_backward(shape, kind, activation, add, raw, through, dw32, accumulate=0, pad=(8, 8, 8, 8), extra=0, seed=1, spoil=None):
+    rows, n_weights, weight_of, K, N = shape
+    t, M, G = TYPES[kind], sum(rows), len(rows)
+    d = torch.float32 if dw32 else t
+    gen = torch.Generator("cuda").manual_seed(seed)
+    _, x = matrix(gen, M, K, t, pad[0], extra=extra)
+    _, dy = matrix(gen, M, N, t, pad[1], extra=extra)
+    w = (torch.randn(n_weights, N, K + pad[2], generator=gen, device="cuda") / math.sqrt(N)).to(t)[:, :, :K]
+    _, da = matrix(gen, M, K, t, pad[3]) if add else (None, None)
+    _, xp = matrix(gen, M, K, t, pad[3]) if through else (None, None)
+    xbuf, dx = matrix(gen, M, K, t, pad[3], extra=extra) if raw else (None, None)
+    pbuf, dp = matrix(gen, M, K, t, pad[0], extra=extra) if through else (None, None)
+    wbuf = torch.full((G, N * (K + pad[2]) + 8), 77, dtype=d, device="cuda")
+    dw = torch.as_strided(wbuf, (G, N, K), (wbuf.shape[1], K + pad[2], 1))
+    bbuf = torch.full((G, N + 8), 77, dtype=d, device="cuda")
+    db = bbuf[:, :N]
+    if accumulate:
+        dw.copy_(torch.randn(G, N, K, generator=gen, device="cuda"))
+        db.copy_(torch.randn(G, N, generator=gen, device="cuda"))
+    dw0, db0 = dw.double(), db.double()
+    if spoil is not None:
+        spoil(x, dy, rows)
+    workers_dense_backward(dy, x, w, rows, weight_of, xp, activation, da, dx, dp, dw, db, accumulate)
+    workers_dense_status()
+    for buf in (xbuf, pbuf):
+        assert buf is None or untouched(buf, M, K)
+    assert (bbuf[:, N:] == 77).all() and (wbuf[:, N * (K + pad[2]):] == 77).all()
+    if pad[2]:
+        gap = torch.as_strided(wbuf, (G, N, pad[2]), (wbuf.shape[1], K + pad[2], 1), K)
+        assert (gap == 77).all()
+    for g, s in spans(rows):
+        k = weight_of[g] if weight_of else g
+        gy, gx = dy[s].double(), x[s].double()
+        if spoil is not None and not (torch.isfinite(gy).all() and torch.isfinite(gx).all()):
+            continue
+        v = gy @ w[k].double()
+        e = sum_error(gy.abs() @ w[k].double().abs(), N, False)
+        if add:
+            v = v + da[s].double()
+            e = e + v.abs() * 2.0 ** -23
+        if raw:
+            assert ((dx[s].double() - v).abs() <= e + half_step(v.abs() + e, t)).all(), (g, "dx")
+        if through:
+            q = slope(xp[s].double(), activation)
+            e2, v2 = e * 1.2 + v.abs() * 2.0 ** -19, v * q      # |act'| <= 1.13, within 2^-20
+            assert ((dp[s].double() - v2).abs() <= e2 + half_step(v2.abs() + e2, t)).all(), (g, "dx_pre")
+        for got, old, want, terms in ((dw[g], dw0[g], gy.T @ gx, gy.abs().T @ gx.abs()), (db[g], db0[g], gy.sum(0), gy.abs().sum(0))):
+            e = sum_error(terms, max(rows[g], 1), dw32)
+            if accumulate:
+                want = want + old
+                e = e + want.abs() * 2.0 ** -23
+            limit = e + (half_step(want.abs() + e, t) if not dw32 else want.abs() * 2.0 ** -23)
+            assert ((got.double() - want).abs() <= limit).all(), (g, "dw/db", float(((got.double() - want).abs() - limit).max()))
+
+
+@gpu
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: f"{len(s[0])}x{sum(s[0])}-{s[3]}-{s[4]}")
+@pytest.mark.parametrize("kind,activation,add,raw,through,dw32", [
+    ("bf16", "none", False, True, False, False), ("fp16", "relu", True, True, True, True), ("bf16", "gelu", False, False, True, True),
+    ("fp16", "silu", True, False, True, False)])
+def test_backward(shape, kind, activation, add, raw, through, dw32):
+    one_backward(shape, kind, activation, add, raw, through, dw32)
+
+
+@gpu
+@pytest.mark.parametrize("shape", [([5, 1, 9], 3, None, 37, 51), ([130, 70], 1, [0, 0], 1, 3), ([1300], 1, None, 2049, 2051), ([1], 1, None, 7, 1), ([300, 1], 2, None, 65, 9),
+                                   ([0, 0], 2, None, 33, 17)], ids=lambda s: f"{len(s[0])}x{sum(s[0])}-{s[3]}-{s[4]}")
+@pytest.mark.parametrize("pad", [(0, 0, 0, 0), (1, 2, 3, 5)])
+@pytest.mark.parametrize("accumulate", [0, 1])
+def test_backward_odd_sizes_and_pitches(shape, pad, accumulate):
+    one_backward(shape, "bf16", "gelu", True, True, True, bool(accumulate), accumulate, pad=pad, extra=3)
+
+
+@gpu
+@pytest.mark.parametrize("rows", [[70, 5, 0, 33, 200], [1000, 1, 77]])
+@pytest.mark.parametrize("N,K", [(136, 200), (2048, 2304)])
+@pytest.mark.parametrize("dw32", [False, True])
+def test_one_workers_infinities_stay_its_own(rows, N, K, dw32):
+    """A worker's NaN and infinities are in none of the other workers' gradients, though their rows share blocks of the reduction."""
+    def spoil(x, dy, rows):
+        for g, s in spans(rows):
+            if g % 2:
+                x[s], dy[s] = math.nan, math.inf
+    one_backward((rows, len(rows), None, K, N), "bf16", "relu", False, True, True, dw32, spoil=spoil)
+
+
+@gpu
+@pytest.mark.parametrize("shape", [([3, 2], 2, None, 64, 64), ([130, 90], 1, [0, 0], 128, 136)])
+def test_values_that_are_not_finite_follow_the_formula(shape):
+    rows, n_weights, weight_of, K, N = shape
+    x = torch.ones(sum(rows), K, device="cuda").bfloat16()
+    w = torch.ones(n_weights, N, K, device="cuda").bfloat16()
+    x[0, 0], x[1, 1] = math.nan, math.inf
+    for activation in ("none", "relu", "gelu", "silu"):
+        y = workers_dense_forward(x, w, rows, weight_of, activation=activation)
+        assert torch.isnan(y[0]).all() and (y[1] == math.inf).all() and torch.isfinite(y[2:]).all()
+    # a gradient masked by the ReLU is zero, whatever it is
+    z = -torch.ones(sum(rows), K, device="cuda").bfloat16()
+    dy, dx = torch.full((sum(rows), N), math.inf, device="cuda").bfloat16(), torch.empty_like(z)
+    workers_dense_backward(dy, x, w, rows, weight_of, x_pre=z, activation="relu", dx_pre=dx)
+    assert not dx.any()
+
+
+@gpu
+def test_empty_call_writes_nothing():
+    x, w, y = torch.empty(0, 16, device="cuda").bfloat16(), torch.ones(2, 8, 16, device="cuda").bfloat16(), torch.full((3, 8), 7.0, device="cuda").bfloat16()
+    workers_dense_forward(x, w, [0, 0], y=y)
+    assert (y == 7).all()
+    dw, db = torch.ones(2, 8, 16, device="cuda"), torch.ones(2, 8, device="cuda")
+    workers_dense_backward(torch.empty(0, 8, device="cuda").bfloat16(), x, w, [0, 0], dw=dw, db=db, accumulate=True)
+    assert (dw == 1).all() and (db == 1).all()
+    workers_dense_backward(torch.empty(0, 8, device="cuda").bfloat16(), x, w, [0, 0], dw=dw, db=db)
+    assert not dw.any() and not db.any()
+
+
+@gpu
+@pytest.mark.parametrize("shape", [SHAPES[2], SHAPES[6], SHAPES[8]], ids=lambda s: f"{len(s[0])}x{sum(s[0])}-{s[3]}-{s[4]}")
+def test_captured_replayed_and_on_two_streams(shape):
+    rows, n_weights, weight_of, K, N = shape
+    gen = torch.Generator("cuda").manual_seed(2)
+    make = lambda *s: torch.randn(*s, generator=gen, device="cuda").bfloat16()
+    M = sum(rows)
+    x, w, dy = make(M, K), make(n_weights, N, K), make(M, N)
+
+    def both(y, dx, dw, db):
+        workers_dense_forward(x, w, rows, weight_of, activation="gelu", y=y)
+        workers_dense_backward(dy, x, w, rows, weight_of, dx=dx, dw=dw, db=db)
+    outs = [(torch.zeros(M, N, device="cuda").bfloat16(), torch.zeros(M, K, device="cuda").bfloat16(), torch.zeros(len(rows), N, K, device="cuda"),
+             torch.zeros(len(rows), N, device="cuda")) for _ in range(4)]
+    both(*outs[0])
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(3):
+        for st, o in zip(streams, outs[1:3]):
+            with torch.cuda.stream(st):
+                both(*o)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both(*outs[3])
+    for t in outs[3]:
+        t.fill_(5)
+    graph.replay()
+    graph.replay()
+    torch.cuda.synchronize()
+    workers_dense_status()
+    for o in outs[1:]:
+        for a, b in zip(o, outs[0]):
+            assert torch.equal(a, b)
+    x.copy_(make(M, K))
+    graph.replay()
+    both(*outs[0])
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(outs[0], outs[3]))
+    del graph
+
+
+@gpu
+def test_gradients_against_differences():
+    """d/dt of sum(c * y(t)) along random directions of x, W and b, y from the forward call in FP32: the differences' error is that of the values
+    (2^-22 of the terms' sums, over the step) and the third derivatives' (the layer is linear: none)."""
+    rows, K, N = [40, 0, 25], 96, 64
+    gen = torch.Generator("cuda").manual_seed(8)
+    grid = lambda *s: torch.randint(-8, 9, s, generator=gen, device="cuda").bfloat16() / 8      # sums and differences are exact in bf16
+    x, w, b, c = grid(65, K), grid(3, N, K), grid(3, N), grid(65, N)
+    dx, dw, db = torch.empty_like(x), torch.empty(3, N, K, device="cuda"), torch.empty(3, N, device="cuda")
+    workers_dense_backward(c, x, w, rows, dx=dx, dw=dw, db=db)
+    value = lambda x, w, b: float((workers_dense_forward(x, w, rows, bias=b, out_dtype=torch.float32).double() * c.double()).sum())
+    ux, uw, ub = grid(65, K), grid(3, N, K), grid(3, N)
+    for args, want in (((ux, 0, 0), (dx.double() * ux.double()).sum()), ((0, uw, 0), (dw.double() * uw.double()).sum()), ((0, 0, ub), (db.double() * ub.double()).sum())):
+        up, down = (value(x + s * args[0], w + s * args[1], b + s * args[2]) for s in (1, -1))
+        size = float((c.double().abs() @ torch.ones(N, 1, device="cuda").double()).sum()) * K * 4
+        tol = size * 2.0 ** -22 + (float(dx.double().abs().sum()) * 2.0 ** -9 if args[0] is ux else 0.0)      # dx is rounded to bf16
+        assert abs((up - down) / 2 - float(want)) <= tol
+
+
+@gpu
+def test_a_training_step_of_two_layers():
+    """Workers with ragged batches and a residual block: forward, backward into one fp32 gradient per worker, their mean, and AdamW with a bf16 copy that the
+    next forward reads; against the same in float64 (by autograd), within the roundings of what passes through bf16."""
+    rows, D, H = [50, 0, 77, 3], 64, 160
+    M, G = sum(rows), 4
+    gen = torch.Generator("cuda").manual_seed(9)
+    normal = lambda *s, scale=1.0: torch.randn(*s, generator=gen, device="cuda") * scale
+    x, target = normal(M, D).bfloat16(), normal(M, D).bfloat16()
+    master = [normal(H, D, scale=0.1), normal(H, scale=0.1), normal(D, H, scale=0.1), normal(D, scale=0.1)]
+    copies = [p.bfloat16() for p in master]
+    per_worker = [torch.empty(G, *p.shape, device="cuda") for p in master]
+    mean = [torch.empty_like(p) for p in master]
+    opt = AdamW(master, mean, copies=copies, weight_decay=0.0)
+    for step in (1, 2):
+        w1, b1, w2, b2 = copies
+        pre, h, y = torch.empty(M, H, device="cuda").bfloat16(), None, None
+        one = [0] * G
+        h = workers_dense_forward(x, w1, rows, one, bias=b1, activation="gelu", pre=pre)
+        y = workers_dense_forward(h, w2, rows, one, bias=b2, residual=x)
+        dy = (y.float() - target.float()).bfloat16()
+        dpre, dx = torch.empty_like(pre), torch.empty_like(x)
+        workers_dense_backward(dy, h, w2, rows, one, x_pre=pre, activation="gelu", dx_pre=dpre, dw=per_worker[2], db=per_worker[3])
+        workers_dense_backward(dpre, x, w1, rows, one, dx_add=dy, dx=dx, dw=per_worker[0], db=per_worker[1])
+        ref = [p.double().requires_grad_() for p in copies] + [x.double().requires_grad_()]
+        z = ref[4] @ ref[0].T + ref[1]
+        out = act(z, "gelu") @ ref[2].T + ref[3] + ref[4]
+        (0.5 * (out - target.double()).square()).sum().backward()
+        got = [t.sum(0).double() for t in per_worker] + [dx.double()]
+        for a, r in zip(got, ref):      # five roundings to bf16 on the way (pre, h, y, dy, dpre), each 2^-9 at most of what it rounds
+            assert float((a - r.grad).norm() / r.grad.norm()) < 5 * 2.0 ** -9
+        for m, t in zip(mean, per_worker):
+            torch.mean(t, 0, out=m)
+        opt.ps_adamw_step(lr=1e-2, step=step)
+        torch.cuda.synchronize()
+        assert all(torch.equal(c, p.bfloat16()) for c, p in zip(copies, master))
+
+
+# ---- refusals --------------------------------------------------------------------------------------------------------------
+def layer(**more):
+    """A layer whose addresses are never read: every refusal comes before any launch."""
+    rows = np.array(more.pop("row_list", [4, 0, 3]), dtype=np.int32)
+    l = ps.DenseLayer(len(rows), 3, rows.ctypes.data, None, 32, 16, ps.TYPE_BF16, 0, 1 << 20, 32, 1 << 21, 32, 512, None, 0, None)
+    l._keep = rows
+    for k, v in more.items():
+        if k == "weight_list":
+            l._w = np.array(v, dtype=np.int32)
+            l.weight_of = l._w.ctypes.data
+        else:
+            setattr(l, k, v)
+    return l
+
+
+BAD_LAYERS = [dict(groups=0), dict(groups=257), dict(rows=None), dict(row_list=[4, -1, 3]), dict(row_list=[2**31 - 1, 2**31 - 1, 1]), dict(n_weights=2), dict(n_weights=0),
+              dict(weight_list=[0, 1, 3]), dict(weight_list=[0, -1, 0]), dict(type=ps.TYPE_FP32), dict(type=7), dict(in_features=0), dict(out_features=-1),
+              dict(in_features=(1 << 20) + 1), dict(activation=4), dict(activation=-1), dict(x=None), dict(x_pitch=31), dict(weight=None), dict(weight_pitch=31),
+              dict(weight_stride=511), dict(x=(1 << 20) + 1)]
+
+
+@pytest.mark.parametrize("bad", BAD_LAYERS, ids=str)
+def test_refused_layers(bad):
+    lib, size = ps.load(), C.c_uint64()
+    out = ps.DenseOutput(y=1 << 22, y_pitch=16, y_type=ps.TYPE_BF16)
+    grads = ps.DenseGradients(dy=1 << 22, dy_pitch=16, dx=1 << 23, dx_pitch=32, dw_type=ps.TYPE_FP32)
+    l = layer(**bad)
+    assert lib.workers_dense_forward(C.byref(l), C.byref(out)) == -1
+    assert lib.workers_dense_backward(C.byref(l), C.byref(grads)) == -1
+    assert lib.workers_dense_workspace(C.byref(l), None, 0, C.byref(size)) == -1
+
+
+@pytest.mark.parametrize("bad", [dict(y=None), dict(y_pitch=15), dict(y_type=ps.TYPE_FP16), dict(y_type=9), dict(y=(1 << 22) + 1), dict(residual=1 << 23, residual_pitch=15),
+                                 dict(pre=1 << 23, pre_pitch=1), dict(bias=1 << 23, bias_stride=15), dict(bias=(1 << 23) + 1, bias_stride=16)], ids=str)
+def test_refused_outputs(bad):
+    out = ps.DenseOutput(y=1 << 22, y_pitch=16, y_type=ps.TYPE_BF16)
+    for k, v in bad.items():
+        setattr(out, k, v)
+    assert ps.load().workers_dense_forward(C.byref(layer()), C.byref(out)) == -1
+
+
+@pytest.mark.parametrize("bad", [dict(dy=None), dict(dy_pitch=15), dict(dx_pitch=31), dict(dx_pre=1 << 23, dx_pre_pitch=32), dict(dw=1 << 23, dw_pitch=31, dw_stride=512),
+                                 dict(dw=1 << 23, dw_pitch=32, dw_stride=511), dict(db=1 << 23, db_stride=15), dict(dw_type=ps.TYPE_FP16), dict(accumulate=2),
+                                 dict(dw=(1 << 23) + 2, dw_pitch=32, dw_stride=512), dict(dx_add=1 << 23, dx_add_pitch=3)], ids=str)
+def test_refused_gradients(bad):
+    grads = ps.DenseGradients(dy=1 << 22, dy_pitch=16, dx=1 << 23, dx_pitch=32, dw_type=ps.TYPE_FP32)
+    for k, v in bad.items():
+        setattr(grads, k, v)
+    assert ps.load().workers_dense_backward(C.byref(layer()), C.byref(grads)) == -1
+
+
+def test_workspace_is_asked_for_where_tile_copies_cannot_read():
+    lib, size = ps.load(), C.c_uint64()
+    ask = lambda l, dy=None, pitch=0: lib.workers_dense_workspace(C.byref(l), dy, pitch, C.byref(size)) == 0 and size.value
+    assert ask(layer()) == 0 and ask(layer(), 1 << 22, 16) == 0
+    assert ask(layer(x_pitch=33)) >= 7 * 32 * 2 and ask(layer(x=(1 << 20) + 8)) >= 7 * 32 * 2
+    assert ask(layer(weight_pitch=33, weight_stride=600)) >= 3 * 16 * 32 * 2 and ask(layer(weight_stride=513)) >= 3 * 16 * 32 * 2
+    assert ask(layer(), 1 << 22, 17) >= 7 * 16 * 2
+    assert ask(layer(row_list=[0, 0, 0], x=None)) == 0
+    assert lib.workers_dense_forward(None, None) == -1 and lib.workers_dense_workspace(C.byref(layer()), None, 0, None) == -1
+
+
+@gpu
+def test_refusals_of_the_binding():
+    x, w = torch.zeros(4, 16, device="cuda").bfloat16(), torch.zeros(2, 8, 16, device="cuda").bfloat16()
+    for bad in (dict(rows=[4]), dict(rows=[3, 2]), dict(weight=w[:, :, :8]), dict(weight=w.half()), dict(weight_of=[0]), dict(activation="tanh"),
+                dict(bias=torch.zeros(2, 9, device="cuda").bfloat16()), dict(y=torch.zeros(4, 8, device="cuda").half()), dict(x=x.cpu()), dict(x=x.T.contiguous().T),
+                dict(residual=torch.zeros(4, 8, device="cuda")), dict(pre=torch.zeros(3, 8, device="cuda").bfloat16())):
+        args = {**dict(x=x, weight=w, rows=[2, 2]), **bad}
+        with pytest.raises((ValueError, ps.PSError)):
+            workers_dense_forward(**args)
+    with pytest.raises(TypeError):
+        workers_dense_forward(x.double(), w.double(), [2, 2])
+    with pytest.raises(ps.PSError):
+        workers_dense_forward(x.float(), w.float(), [2, 2])
+    with pytest.raises(ps.PSError):
+        workers_dense_forward(x, w, [5, -1])
+    dy = torch.zeros(4, 8, device="cuda").bfloat16()
+    with pytest.raises(ValueError):
+        workers_dense_backward(dy, x, w, [2, 2], dx_pre=torch.zeros_like(x))
+    with pytest.raises(ValueError):
+        workers_dense_backward(dy, x, w, [2, 2], dw=torch.zeros(2, 8, 16, device="cuda"), db=torch.zeros(2, 8, device="cuda").bfloat16())
