@@ -29,6 +29,7 @@
 #include <algorithm>
 #include <cmath>
 #include <mutex>
+#include <type_traits>
 
 #include "device_common.cuh"
 #include "error.h"
@@ -67,12 +68,13 @@ template <int OP, bool DRAIN> using Single = DenseShape<OP, 1, 256, 4, false, fa
 template <int OP> using Split = DenseShape<OP, 1, 128, 3, true, false, true>;
 template <int OP, int BN> using Few = DenseShape<OP, 1, BN, BN == 64 ? 4 : 5, true, true, true>;
 
-// Groups of rows [row0[g], row0[g + 1]) with weight matrix w[g]; tile0: prefix sums of their tiles (weight gradient: not used).
+// Forward and input gradient: groups of rows [row0[g], row1[g]), those with the same weights next to each other (a run), cut into blocks of rows;
+// blk0: prefix sums of their blocks.  Weight gradient: the workers' rows.
 struct DenseTab {
-  int32_t groups;
-  int32_t row0[PS_MAX_WORKERS + 1];
-  int32_t tile0[PS_MAX_WORKERS + 1];
-  uint16_t w[PS_MAX_WORKERS];
+  int32_t groups, runs;
+  int32_t row0[PS_MAX_WORKERS], row1[PS_MAX_WORKERS], blk0[PS_MAX_WORKERS + 1];
+  int32_t run_blk0[PS_MAX_WORKERS + 1], run_pair0[PS_MAX_WORKERS + 1];      // a run's first block, and first pair of blocks
+  uint16_t w[PS_MAX_WORKERS], run_w[PS_MAX_WORKERS];
 };
 
 // What the epilogue adds and where it writes (pitches in elements).  forward: in0 bias, in1 residual, out0 y, out1 pre; input gradient: in1
@@ -86,9 +88,10 @@ struct DenseEpi {
 };
 
 struct DenseArgs {
-  int32_t n_tiles, m_tiles, n_side, n_tiles_n;      // tiles; weight gradient: tiles along the left side; length and tiles of the right side (Few: of the left)
+  int32_t n_tiles, m_tiles, n_side, n_tiles_n;      // tiles; along the left side; length and tiles of the right side (Few: of the left)
   int32_t m_side;                                   // weight gradient: length of the left side
   int32_t red;                                      // reduction length (weight gradient: the group's rows)
+  int32_t rows;                                     // of all groups
   int32_t chunk;                                    // blocks of k per accumulator
   uint32_t idesc;
 };
@@ -107,14 +110,18 @@ __device__ __forceinline__ uint32_t narrow2(float lo, float hi, int bf16) {
   const __half2 h = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&h);
 }
-// Four consecutive 16-bit values from element i on, of which n exist.
-__device__ __forceinline__ float4 load4(const void* base, int64_t i, int n, int vec, int bf16) {
+// Four consecutive 16-bit values from element i on, of which n exist, as they lie; and as floats.
+__device__ __forceinline__ uint2 raw4(const void* base, int64_t i, int n, int vec) {
   const uint16_t* p = reinterpret_cast<const uint16_t*>(base) + i;
-  if (vec && n >= 4) {
-    const uint2 w = *reinterpret_cast<const uint2*>(p);
-    return make_float4(widen(w.x & 0xFFFFu, bf16), widen(w.x >> 16, bf16), widen(w.y & 0xFFFFu, bf16), widen(w.y >> 16, bf16));
-  }
-  return make_float4(widen(p[0], bf16), n > 1 ? widen(p[1], bf16) : 0.f, n > 2 ? widen(p[2], bf16) : 0.f, n > 3 ? widen(p[3], bf16) : 0.f);
+  if (vec && n >= 4) return *reinterpret_cast<const uint2*>(p);
+  uint2 w = make_uint2(p[0], 0u);
+  if (n > 1) w.x |= (uint32_t)p[1] << 16;
+  if (n > 2) w.y = p[2];
+  if (n > 3) w.y |= (uint32_t)p[3] << 16;
+  return w;
+}
+__device__ __forceinline__ float4 widen4(const uint2& w, int bf16) {
+  return make_float4(widen(w.x & 0xFFFFu, bf16), widen(w.x >> 16, bf16), widen(w.y & 0xFFFFu, bf16), widen(w.y >> 16, bf16));
 }
 __device__ __forceinline__ void store4(void* base, int64_t i, int n, int vec, int bf16, const float4& v) {
   uint16_t* p = reinterpret_cast<uint16_t*>(base) + i;
@@ -141,58 +148,86 @@ __device__ __forceinline__ void store4_f32(float* p, int n, int vec, const float
 }
 __device__ __forceinline__ float4 add(const float4& a, const float4& b) { return make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w); }
 
+// The normal distribution function, and e = exp(-z^2 / 2): Abramowitz and Stegun 7.1.26 (a polynomial in 1 / (1 + p x) times e; erf within
+// 1.5e-7), which shares the exponential with the density.
+__device__ __forceinline__ float normal_cdf(float z, float& e) {
+  const float t = __fdividef(1.f, fmaf(0.3275911f * 0.70710678f, fabsf(z), 1.f));
+  e = __expf(-0.5f * z * z);
+  const float tail = 0.5f * e * t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+  return z > 0.f ? 1.f - tail : tail;      // NaN: tail is
+}
 __device__ __forceinline__ float activate(float z, int act) {
   if (act == PS_ACT_RELU) return z < 0.f ? 0.f : z;                 // NaN stays
-  if (act == PS_ACT_GELU) return 0.5f * z * (1.f + erff(z * 0.70710678f));
-  if (act == PS_ACT_SILU) return __fdividef(z, 1.f + expf(-z));
+  if (act == PS_ACT_GELU) { float e; return z * normal_cdf(z, e); }
+  if (act == PS_ACT_SILU) return __fdividef(z, 1.f + __expf(-z));
   return z;
 }
 // d * act'(z)
 __device__ __forceinline__ float through(float d, float z, int act) {
   if (act == PS_ACT_RELU) return z > 0.f ? d : 0.f;
-  if (act == PS_ACT_GELU) return d * (0.5f * (1.f + erff(z * 0.70710678f)) + z * 0.39894228f * expf(-0.5f * z * z));
+  if (act == PS_ACT_GELU) {
+    float e;
+    const float c = normal_cdf(z, e);
+    return d * fmaf(z * 0.39894228f, e, c);
+  }
   if (act == PS_ACT_SILU) {
-    const float e = __fdividef(1.f, 1.f + expf(-z));
-    return d * (e * (1.f + z * (1.f - e)));
+    const float e = __fdividef(1.f, 1.f + __expf(-z));
+    return d * (e * fmaf(z, 1.f - e, 1.f));
   }
   return d;
+}
+__device__ __forceinline__ float4 activate4(const float4& z, int act) { return make_float4(activate(z.x, act), activate(z.y, act), activate(z.z, act), activate(z.w, act)); }
+__device__ __forceinline__ float4 through4(const float4& d, const float4& z, int act) {
+  return make_float4(through(d.x, z.x, act), through(d.y, z.y, act), through(d.z, z.z, act), through(d.w, z.w, act));
+}
+
+// What the elementwise part reads for four consecutive columns of a row.  Loaded well before it is used: in a tile's read-out nothing else hides
+// the loads (with loads where they were used, the input gradient of 16,384 x 4096 x 4096 with everything on took 787 us, alone 345).
+template <int OP> struct EpiIn { uint2 a, b; };
+template <> struct EpiIn<D_DW> { float4 a; };
+template <int OP>
+__device__ __forceinline__ EpiIn<OP> load_in(const DenseEpi& e, int64_t row, int col, int n, int which) {
+  EpiIn<OP> x;
+  if constexpr (OP == D_DW) {
+    x.a = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (e.accumulate) {
+      const int64_t at = (int64_t)which * e.out0_stride + row * e.out0_pitch + col;
+      x.a = e.out0_fp32 ? load4_f32(reinterpret_cast<const float*>(e.out0) + at, n, e.v_out0) : widen4(raw4(e.out0, at, n, e.v_out0), e.bf16);
+    }
+  } else {
+    x.a = x.b = make_uint2(0u, 0u);
+    if (e.in1) x.a = raw4(e.in1, row * e.in1_pitch + col, n, e.v_in1);
+    if (OP == D_DX && e.out1) x.b = raw4(e.in2, row * e.in2_pitch + col, n, e.v_in2);
+  }
+  return x;
 }
 
 // Everything elementwise for four consecutive columns of a row.  which: the weight matrix (forward) or the worker (weight gradient); bias: in0's
 // four values, loaded by the caller, whose column stays the same over many rows.
 template <int OP>
-__device__ __forceinline__ void finish4(const DenseEpi& e, int64_t row, int col, int n, int which, const float4& bias, float4 v) {
-  if (OP == D_FWD) {
+__device__ __forceinline__ void finish4(const DenseEpi& e, int64_t row, int col, int n, int which, const float4& bias, const EpiIn<OP>& in, float4 v) {
+  if constexpr (OP == D_FWD) {
     v = add(v, bias);
     if (e.out1) store4(e.out1, row * e.out1_pitch + col, n, e.v_out1, e.bf16, v);
-    if (e.act != PS_ACT_NONE) v = make_float4(activate(v.x, e.act), activate(v.y, e.act), activate(v.z, e.act), activate(v.w, e.act));
-    if (e.in1) v = add(v, load4(e.in1, row * e.in1_pitch + col, n, e.v_in1, e.bf16));
+    if (e.act != PS_ACT_NONE) v = activate4(v, e.act);
+    if (e.in1) v = add(v, widen4(in.a, e.bf16));
     if (e.out0_fp32) store4_f32(reinterpret_cast<float*>(e.out0) + row * e.out0_pitch + col, n, e.v_out0, v);
     else store4(e.out0, row * e.out0_pitch + col, n, e.v_out0, e.bf16, v);
-  } else if (OP == D_DX) {
-    if (e.in1) v = add(v, load4(e.in1, row * e.in1_pitch + col, n, e.v_in1, e.bf16));
+  } else if constexpr (OP == D_DX) {
+    if (e.in1) v = add(v, widen4(in.a, e.bf16));
     if (e.out0) store4(e.out0, row * e.out0_pitch + col, n, e.v_out0, e.bf16, v);
-    if (e.out1) {
-      const float4 z = load4(e.in2, row * e.in2_pitch + col, n, e.v_in2, e.bf16);
-      store4(e.out1, row * e.out1_pitch + col, n, e.v_out1, e.bf16,
-             make_float4(through(v.x, z.x, e.act), through(v.y, z.y, e.act), through(v.z, z.z, e.act), through(v.w, z.w, e.act)));
-    }
+    if (e.out1) store4(e.out1, row * e.out1_pitch + col, n, e.v_out1, e.bf16, through4(v, widen4(in.b, e.bf16), e.act));
   } else {
     const int64_t at = (int64_t)which * e.out0_stride + row * e.out0_pitch + col;
-    if (e.out0_fp32) {
-      float* p = reinterpret_cast<float*>(e.out0) + at;
-      if (e.accumulate) v = add(v, load4_f32(p, n, e.v_out0));
-      store4_f32(p, n, e.v_out0, v);
-    } else {
-      if (e.accumulate) v = add(v, load4(e.out0, at, n, e.v_out0, e.bf16));
-      store4(e.out0, at, n, e.v_out0, e.bf16, v);
-    }
+    if (e.accumulate) v = add(v, in.a);
+    if (e.out0_fp32) store4_f32(reinterpret_cast<float*>(e.out0) + at, n, e.v_out0, v);
+    else store4(e.out0, at, n, e.v_out0, e.bf16, v);
   }
 }
 template <int OP>
 __device__ __forceinline__ float4 bias4(const DenseEpi& e, int col, int n, int which) {
   if (OP != D_FWD || !e.in0 || n <= 0) return make_float4(0.f, 0.f, 0.f, 0.f);
-  return load4(e.in0, (int64_t)which * e.in0_stride + col, n, e.v_in0, e.bf16);
+  return widen4(raw4(e.in0, (int64_t)which * e.in0_stride + col, n, e.v_in0), e.bf16);
 }
 
 // ---- pairs of CTAs ---------------------------------------------------------------------------------------------------------
@@ -231,11 +266,25 @@ __device__ __forceinline__ bool pair_wait(uint64_t* bar, uint32_t parity, const 
   }
   return __all_sync(0xffffffffu, done && !*abort_flag);
 }
-// A tile load into this CTA's shared memory that completes on a barrier of the pair's first CTA.
-__device__ __forceinline__ void tma_load_pair(void* smem_dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2) {
-  asm volatile(
-      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
-      ::"r"(smem_u32(smem_dst)), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2) : "memory");
+// Copies and their byte counts, issued by a whole warp that has stayed together, as the MMAs are: one lane of it issues.  From a single lane's
+// branch every copy's operands went through vector registers, about 150 clocks each, and with four copies to a stage (weight gradient) the producer
+// was what the kernel waited for: 934 clocks per stage; 16,384 x 4096 x 4096 576 -> 382 us.
+// PAIR: into this CTA's shared memory, completing on the barrier of the pair's first CTA.
+template <bool PAIR>
+__device__ __forceinline__ void tma_load_warp(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2) {
+  if (PAIR)
+    asm volatile(
+        "{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\t"
+        "@q cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];\n\t}"
+        ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2) : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\t"
+        "@q cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];\n\t}"
+        ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2) : "memory");
+}
+__device__ __forceinline__ void expect_tx_warp(uint32_t bar, uint32_t bytes) {
+  asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\t@q mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n\t}" ::"r"(bar), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void umma_f16_pair(uint32_t tmem_d, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
@@ -262,43 +311,59 @@ template <bool MN> __device__ __forceinline__ uint32_t tile_desc_lo(uint32_t add
 template <bool MN> __host__ __device__ constexpr uint32_t tile_k_step() { return MN ? 16 * 128 / 16 : 32 / 16; }      // sixteen k further, in 16-byte units
 
 struct DenseTile {
-  int grp, w;            // group, its weight matrix
-  int m0, m_end;         // left side: first row of the tile, end of the rows that count
-  int n0, n_end;         // right side
+  int w;                 // the weight matrix; weight gradient: the worker
+  int m0, m_end;         // left side: first row of this CTA's part, end of the rows that count
+  int n0, n_end;         // right side, of the whole tile
   int red0, red;         // reduction: first index, length
 };
 
-template <class S>
-__device__ __forceinline__ void decode_tile(const DenseArgs& a, const DenseTab& tab, int t, DenseTile& c) {
-  if (S::OP == D_DW) {
-    const int per = a.m_tiles * a.n_tiles_n, g = t / per, l = t - g * per;
-    c.grp = c.w = g;
-    c.m0 = (l % a.m_tiles) * S::TM; c.m_end = a.m_side;
-    c.n0 = (l / a.m_tiles) * S::BN; c.n_end = a.n_side;
-    c.red0 = tab.row0[g]; c.red = tab.row0[g + 1] - c.red0;
-    return;
-  }
-  int lo = 0, hi = tab.groups;      // the last group that starts at or before t: one with tiles
+// The last of `n` ascending starts that is not above `at`: of equal ones, the one that is not empty.
+__device__ __forceinline__ int find_start(const int32_t* start, int n, int at) {
+  int lo = 0, hi = n;
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
-    if (tab.tile0[mid] <= t) lo = mid; else hi = mid;
+    if (start[mid] <= at) lo = mid; else hi = mid;
   }
-  const int l = t - tab.tile0[lo], first = tab.row0[lo], end = tab.row0[lo + 1];
-  c.grp = lo; c.w = tab.w[lo];
-  c.red0 = 0; c.red = a.red;
-  if (S::FEW) {
-    const int rt = (end - first + S::BN - 1) / S::BN;      // the tiles of one piece of the weights lie together
-    c.m0 = (l / rt) * BM; c.m_end = a.n_side;
-    c.n0 = first + (l % rt) * S::BN; c.n_end = end;
-  } else {
-    // bands of eight tiles along the rows, so that tiles under way together share operands in L2
-    const int mt = (end - first + S::TM - 1) / S::TM, per = 8 * a.n_tiles_n, band = l / per, in = min(8, mt - 8 * band), r = l - band * per;
-    c.m0 = first + (8 * band + r % in) * S::TM; c.m_end = end;
-    c.n0 = (r / in) * S::BN; c.n_end = a.n_side;
-  }
+  return lo;
 }
 
-// The first `n` blocks of k are whole; the last may have fewer.
+template <class S>
+__device__ __forceinline__ void decode_tile(const DenseArgs& a, const DenseTab& tab, int t, int rank, DenseTile& c) {
+  if (S::OP == D_DW) {
+    const int per = a.m_tiles * a.n_tiles_n, g = t / per, l = t - g * per;
+    c.w = g;
+    c.m0 = (l % a.m_tiles) * S::TM + rank * BM; c.m_end = a.m_side;
+    c.n0 = (l / a.m_tiles) * S::BN; c.n_end = a.n_side;
+    c.red0 = tab.row0[g]; c.red = tab.row1[g] - c.red0;
+    return;
+  }
+  c.red0 = 0; c.red = a.red;
+  if (S::FEW) {      // the blocks of a run that share a piece of the weights lie together
+    const int r = find_start(tab.run_pair0, tab.runs, t), l = t - tab.run_pair0[r], blocks = tab.run_blk0[r + 1] - tab.run_blk0[r];
+    const int blk = tab.run_blk0[r] + l % blocks, g = find_start(tab.blk0, tab.groups, blk);
+    c.w = tab.run_w[r];
+    c.m0 = (l / blocks) * BM; c.m_end = a.n_side;
+    c.n0 = tab.row0[g] + (blk - tab.blk0[g]) * S::BN; c.n_end = tab.row1[g];
+    return;
+  }
+  // bands of eight (pairs of) blocks, so that tiles under way together share operands in L2
+  const int per = 8 * a.n_tiles_n, band = t / per, in = min(8, a.m_tiles - 8 * band), l = t - band * per, m = 8 * band + l % in;
+  c.n0 = (l / in) * S::BN; c.n_end = a.n_side;
+  int blk = m;
+  if (S::CTAS == 2) {
+    const int r = find_start(tab.run_pair0, tab.runs, m);
+    blk = tab.run_blk0[r] + 2 * (m - tab.run_pair0[r]) + rank;
+    c.w = tab.run_w[r];
+    if (blk >= tab.run_blk0[r + 1]) {      // the run's blocks are odd in number: nothing to bring in but zeros, nothing to write
+      c.m0 = c.m_end = a.rows;
+      return;
+    }
+  }
+  const int g = find_start(tab.blk0, tab.groups, blk);
+  c.w = tab.w[g];
+  c.m0 = tab.row0[g] + (blk - tab.blk0[g]) * BM; c.m_end = tab.row1[g];
+}
+
 __device__ __forceinline__ int blocks_of(int red) { return (red + BK - 1) / BK; }
 
 template <class S>
@@ -354,48 +419,47 @@ __global__ void __launch_bounds__(S::THREADS, 1) dense_gemm(const __grid_constan
 
   if (warp == 0) {
     // ---------------- copies
-    if (lane == 0) {
-      int s = 0;
-      uint32_t use = 0;
-      bool ok = true;
-      for (int t = first_tile; t < a.n_tiles && ok; t += tile_step) {
-        DenseTile c;
-        decode_tile<S>(a, tab, t, c);
-        int b0, b1;
-        block_range(blocks_of(c.red), b0, b1);
-        const int am = c.m0 + (int)rank * BM, bn = c.n0 + (int)rank * S::B_ROWS;
-        for (int kb = b0; kb < b1; ++kb) {
-          if (use > 0 && !mbar_wait(&empty[s], (use - 1) & 1)) { *abort_flag = 1; ok = false; break; }
-          if (*abort_flag) { ok = false; break; }
-          uint8_t* A = tiles + s * S::STAGE;
-          uint8_t* B = A + S::A_BYTES;
-          const int k0 = kb * BK, r0 = c.red0 + k0;
-          const bool tail = RAGGED && PAIR && c.red - k0 < BK;      // each CTA of a pair cleans up its own
-          uint64_t* local = tail ? &tail_full[s] : &full[s];
-          const uint32_t remote = PAIR ? leaders(&full[s]) : 0u;
-          if (!PAIR || tail) mbar_expect_tx(local, S::STAGE);
-          if (PAIR && rank == 0) {
-            if (tail) mbar_arrive(&full[s]);
-            else mbar_expect_tx(&full[s], 2 * S::STAGE);
-          }
-          auto load = [&](uint8_t* dst, const CUtensorMap* map, int c0, int c1, int c2) {
-            if (PAIR && !tail) tma_load_pair(dst, map, remote, c0, c1, c2);
-            else tma_load_3d(dst, map, local, c0, c1, c2);
-          };
+    const uint32_t full0 = smem_u32(full), full_of_pair = PAIR ? leaders(full) : full0, tail0 = smem_u32(tail_full);
+    int s = 0;
+    uint32_t use = 0;
+    bool ok = true;
+    for (int t = first_tile; t < a.n_tiles && ok; t += tile_step) {
+      DenseTile c;
+      decode_tile<S>(a, tab, t, (int)rank, c);
+      int b0, b1;
+      block_range(blocks_of(c.red), b0, b1);
+      const int am = c.m0, bn = c.n0 + (int)rank * S::B_ROWS;
+      for (int kb = b0; kb < b1; ++kb) {
+        if (use > 0 && !warp_wait(&empty[s], (use - 1) & 1, abort_flag)) { *abort_flag = 1; ok = false; break; }
+        const uint32_t A = base + s * S::STAGE, B = A + S::A_BYTES;
+        const int k0 = kb * BK, r0 = c.red0 + k0;
+        auto load = [&](auto remote, uint32_t bar) {
+          constexpr bool R = decltype(remote)::value;
           if (S::A_MN) {
 #pragma unroll
-            for (int i = 0; i < BM / 64; ++i) load(A + i * BK * 128, &maps.a, am + 64 * i, r0, S::FEW ? c.w : 0);
+            for (int i = 0; i < BM / 64; ++i) tma_load_warp<R>(A + i * BK * 128, &maps.a, bar, am + 64 * i, r0, S::FEW ? c.w : 0);
           } else {
-            load(A, &maps.a, k0, am, S::FEW ? c.w : 0);
+            tma_load_warp<R>(A, &maps.a, bar, k0, am, S::FEW ? c.w : 0);
           }
           if (S::B_MN) {
 #pragma unroll
-            for (int i = 0; i < S::B_ROWS / 64; ++i) load(B + i * BK * 128, &maps.b, bn + 64 * i, r0, S::OP == D_DX ? c.w : 0);
+            for (int i = 0; i < S::B_ROWS / 64; ++i) tma_load_warp<R>(B + i * BK * 128, &maps.b, bar, bn + 64 * i, r0, S::OP == D_DX ? c.w : 0);
           } else {
-            load(B, &maps.b, k0, bn, S::FEW ? 0 : c.w);
+            tma_load_warp<R>(B, &maps.b, bar, k0, bn, S::FEW ? 0 : c.w);
           }
-          if (++s == STAGES) { s = 0; ++use; }
+        };
+        if (!PAIR) {
+          expect_tx_warp(full0 + 8 * s, S::STAGE);
+          load(std::false_type(), full0 + 8 * s);
+        } else if (RAGGED && c.red - k0 < BK) {      // each CTA of a pair cleans up its own
+          if (rank == 0) expect_tx_warp(full0 + 8 * s, 0);
+          expect_tx_warp(tail0 + 8 * s, S::STAGE);
+          load(std::false_type(), tail0 + 8 * s);
+        } else {
+          if (rank == 0) expect_tx_warp(full0 + 8 * s, 2 * S::STAGE);
+          load(std::true_type(), full_of_pair + 8 * s);
         }
+        if (++s == STAGES) { s = 0; ++use; }
       }
     }
   } else if (warp == 1) {
@@ -417,7 +481,7 @@ __global__ void __launch_bounds__(S::THREADS, 1) dense_gemm(const __grid_constan
     bool ok = true;
     for (int t = first_tile; t < a.n_tiles && ok; t += tile_step) {
       DenseTile c;
-      decode_tile<S>(a, tab, t, c);
+      decode_tile<S>(a, tab, t, (int)rank, c);
       int b0, b1;
       block_range(blocks_of(c.red), b0, b1);
       if (PAIR && rank != 0) {
@@ -478,23 +542,34 @@ __global__ void __launch_bounds__(S::THREADS, 1) dense_gemm(const __grid_constan
     int lead = 0;
     for (int t = first_tile; t < a.n_tiles; t += tile_step) {
       DenseTile c;
-      decode_tile<S>(a, tab, t, c);
+      decode_tile<S>(a, tab, t, (int)rank, c);
       int b0, b1;
       block_range(blocks_of(c.red), b0, b1);
-      const int m_base = c.m0 + (int)rank * BM + quarter * 32;
+      const int m_base = c.m0 + quarter * 32;
       // 32 columns of this warp's 32 rows through shared memory: a lane has a row of the accumulator and stores four columns of eight rows
       float4* stage = reinterpret_cast<float4*>(out_stage + (warp - 2) * 4096);
-      auto write_out = [&](const float* v, int j0) {
+      constexpr int AHEAD = S::DRAIN ? 4 : 8;      // the sums take the registers
+      struct Ahead { EpiIn<S::OP> in[AHEAD]; float4 bias; };
+      auto read_ahead = [&](Ahead& x, int j0, int i0) {
+        const int col = c.n0 + col0 + j0 + (lane & 7) * 4, n = c.n_end - col;
+        if (i0 == 0) x.bias = bias4<S::OP>(epi, col, n, c.w);
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+          const int m = m_base + (i0 + i) * 4 + (lane >> 3);
+          if (m < c.m_end && n > 0) x.in[i] = load_in<S::OP>(epi, m, col, n, c.w);
+        }
+      };
+      auto write_out = [&](const float* v, int j0, Ahead& x) {
         const int col = c.n0 + col0 + j0 + (lane & 7) * 4, n = c.n_end - col;
         __syncwarp();
 #pragma unroll
         for (int q = 0; q < 8; ++q) stage[lane * 8 + (q ^ (lane & 7))] = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
         __syncwarp();
-        const float4 bias = bias4<S::OP>(epi, col, n, c.w);
-#pragma unroll 2
+#pragma unroll
         for (int i = 0; i < 8; ++i) {
+          if (i > 0 && i % AHEAD == 0) read_ahead(x, j0, i);
           const int r = i * 4 + (lane >> 3), m = m_base + r;
-          if (m < c.m_end && n > 0) finish4<S::OP>(epi, m, col, n, c.w, bias, stage[r * 8 + ((lane & 7) ^ (r & 7))]);
+          if (m < c.m_end && n > 0) finish4<S::OP>(epi, m, col, n, c.w, x.bias, x.in[i % AHEAD], stage[r * 8 + ((lane & 7) ^ (r & 7))]);
         }
       };
       if constexpr (S::DRAIN) {
@@ -532,11 +607,17 @@ __global__ void __launch_bounds__(S::THREADS, 1) dense_gemm(const __grid_constan
           }
         } else {
 #pragma unroll
-          for (int j0 = 0; j0 < S::COLS; j0 += 32) write_out(sum + j0, j0);
+          for (int j0 = 0; j0 < S::COLS; j0 += 32) {
+            Ahead x;
+            read_ahead(x, j0, 0);
+            write_out(sum + j0, j0, x);
+          }
         }
       } else {
         const int buf = lead % BUFS;
         const bool empty_sum = b1 == b0;      // a worker without rows: its weight gradient is zero
+        Ahead now, next;
+        read_ahead(now, 0, 0);
         if (!empty_sum) {
           if (!warp_wait(&acc_full[buf], (lead / BUFS) & 1, abort_flag)) { *abort_flag = 1; break; }
           tc_fence_after();
@@ -544,6 +625,7 @@ __global__ void __launch_bounds__(S::THREADS, 1) dense_gemm(const __grid_constan
 #pragma unroll 1
         for (int j0 = 0; j0 < S::COLS; j0 += 32) {
           uint32_t r[32];
+          if (j0 + 32 < S::COLS) read_ahead(next, j0 + 32, 0);
           if (empty_sum) {
 #pragma unroll
             for (int j = 0; j < 32; ++j) r[j] = 0u;
@@ -554,7 +636,8 @@ __global__ void __launch_bounds__(S::THREADS, 1) dense_gemm(const __grid_constan
           float v[32];
 #pragma unroll
           for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(r[j]);
-          write_out(v, j0);
+          write_out(v, j0, now);
+          now = next;
         }
         if (!empty_sum) ++lead;
       }
@@ -570,7 +653,7 @@ __global__ void __launch_bounds__(S::THREADS, 1) dense_gemm(const __grid_constan
   }
   if constexpr (S::SPLIT) {
     DenseTile c;
-    decode_tile<S>(a, tab, blockIdx.x, c);
+    decode_tile<S>(a, tab, blockIdx.x, 0, c);
     cg::cluster_group cl = cg::this_cluster();
     cl.sync();
     const int ranks = gridDim.z, me = blockIdx.z;
@@ -578,12 +661,22 @@ __global__ void __launch_bounds__(S::THREADS, 1) dense_gemm(const __grid_constan
     const int rows = S::FEW ? min(S::BN, c.n_end - c.n0) : min(BM, c.m_end - c.m0);
     const int row0 = S::FEW ? c.n0 : c.m0, column0 = S::FEW ? c.m0 : c.n0, end = S::FEW ? c.m_end : c.n_end;
     float* part = reinterpret_cast<float*>(tiles);
-    for (int e = me * S::THREADS + tid; e < rows * QUADS; e += ranks * S::THREADS) {
-      const int r = e / QUADS, q = e - r * QUADS, col = column0 + 4 * q, n = end - col;
-      if (n <= 0) continue;
-      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int k = 0; k < ranks; ++k) v = add(v, *reinterpret_cast<const float4*>(cl.map_shared_rank(part, k) + r * S::PART_PITCH + 4 * q));
-      finish4<S::OP>(epi, row0 + r, col, n, c.w, bias4<S::OP>(epi, col, n, c.w), v);
+    constexpr int AT_ONCE = 4;
+    for (int e0 = me * S::THREADS + tid; e0 < rows * QUADS; e0 += AT_ONCE * ranks * S::THREADS) {
+      EpiIn<S::OP> in[AT_ONCE];
+#pragma unroll
+      for (int i = 0; i < AT_ONCE; ++i) {
+        const int e = e0 + i * ranks * S::THREADS, r = e / QUADS, col = column0 + 4 * (e - r * QUADS), n = end - col;
+        if (e < rows * QUADS && n > 0) in[i] = load_in<S::OP>(epi, row0 + r, col, n, c.w);
+      }
+#pragma unroll
+      for (int i = 0; i < AT_ONCE; ++i) {
+        const int e = e0 + i * ranks * S::THREADS, r = e / QUADS, q = e - r * QUADS, col = column0 + 4 * q, n = end - col;
+        if (e >= rows * QUADS || n <= 0) continue;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int k = 0; k < ranks; ++k) v = add(v, *reinterpret_cast<const float4*>(cl.map_shared_rank(part, k) + r * S::PART_PITCH + 4 * q));
+        finish4<S::OP>(epi, row0 + r, col, n, c.w, bias4<S::OP>(epi, col, n, c.w), in[i], v);
+      }
     }
     cl.sync();                               // a CTA's shared memory outlives its readers
   }
@@ -607,13 +700,13 @@ __global__ void __launch_bounds__(CSUM_TPB) column_sums(const __grid_constant__ 
   __shared__ float mine[64];
   pdl_enter();
   const int g = blockIdx.y, ranks = gridDim.z, me = blockIdx.z, col = blockIdx.x * 64 + (threadIdx.x & 7) * 8, n = a.N - col;
-  const int first = tab.row0[g], rows = tab.row0[g + 1] - first;
+  const int first = tab.row0[g], rows = tab.row1[g] - first;
   const int r0 = first + (int)((int64_t)rows * me / ranks), r1 = first + (int)((int64_t)rows * (me + 1) / ranks);
   float acc[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) acc[j] = 0.f;
   if (n > 0) {
-#pragma unroll 4
+#pragma unroll 8
     for (int r = r0 + (threadIdx.x >> 3); r < r1; r += CSUM_TPB / 8) {
       const uint16_t* p = reinterpret_cast<const uint16_t*>(a.dy) + (int64_t)r * a.pitch + col;
       if (a.vec && n >= 8) {
@@ -750,20 +843,25 @@ int32_t launch(const Problem& p, int split) {
   return e == cudaSuccess ? PS_OK : fail(PS_ERR_CUDA, "dense layer launch: %s", cudaGetErrorString(e));
 }
 
-// Tiles of `tm` rows (of every group) x `bn` columns; fills the prefix sums.
-int64_t count_tiles(DenseTab& tab, int tm, int64_t n_tiles_n) {
-  int64_t t = 0;
+// Cuts the groups into blocks of `tm` rows and fills the prefix sums.  Returns the number of pairs of blocks (of the same run), or of blocks; per_block
+// > 0: of tiles, that many to a block.
+int64_t cut_rows(DenseTab& tab, int tm, bool pairs, int per_block = 0) {
+  int64_t blocks = 0, units = 0;
+  tab.runs = 0;
   for (int g = 0; g < tab.groups; ++g) {
-    tab.tile0[g] = (int32_t)std::min<int64_t>(t, 1ll << 30);
-    t += (int64_t)((tab.row0[g + 1] - tab.row0[g] + tm - 1) / tm) * n_tiles_n;
+    if (g == 0 || tab.w[g] != tab.w[g - 1]) {
+      if (tab.runs) units += pairs ? (blocks - tab.run_blk0[tab.runs - 1] + 1) / 2 : (blocks - tab.run_blk0[tab.runs - 1]) * per_block;
+      tab.run_blk0[tab.runs] = (int32_t)blocks;
+      tab.run_pair0[tab.runs] = (int32_t)std::min<int64_t>(units, 1 << 30);
+      tab.run_w[tab.runs++] = tab.w[g];
+    }
+    tab.blk0[g] = (int32_t)blocks;
+    blocks += (tab.row1[g] - tab.row0[g] + tm - 1) / tm;
   }
-  tab.tile0[tab.groups] = (int32_t)std::min<int64_t>(t, 1ll << 30);
-  return t;
-}
-int64_t padded_rows(const DenseTab& tab, int tm) {
-  int64_t t = 0;
-  for (int g = 0; g < tab.groups; ++g) t += (int64_t)((tab.row0[g + 1] - tab.row0[g] + tm - 1) / tm) * tm;
-  return t;
+  units += pairs ? (blocks - tab.run_blk0[tab.runs - 1] + 1) / 2 : (blocks - tab.run_blk0[tab.runs - 1]) * per_block;
+  tab.blk0[tab.groups] = tab.run_blk0[tab.runs] = (int32_t)blocks;
+  tab.run_pair0[tab.runs] = (int32_t)std::min<int64_t>(units, 1 << 30);
+  return pairs || per_block ? units : blocks;
 }
 int div_up(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
@@ -778,23 +876,22 @@ int split_for(int64_t tiles, int blocks, int room) {
 template <int OP>
 int32_t run_rows(Problem& p, int features, int red, bool fp32_out) {
   DenseTab& tab = p.tab;
-  int used = 0, most = 0;
+  int most = 0;
+  int64_t rows = 0;
   for (int g = 0; g < tab.groups; ++g) {
-    const int r = tab.row0[g + 1] - tab.row0[g];
-    used += r > 0;
-    most = std::max(most, r);
+    most = std::max(most, tab.row1[g] - tab.row0[g]);
+    rows += tab.row1[g] - tab.row0[g];
   }
-  const int64_t rows = tab.row0[tab.groups];
   const int blocks = div_up(red, BK), sms = g_sm_count;
   DenseArgs& a = p.args;
   a.n_side = features;
   a.red = red;
-  auto tiles_fit = [&](int64_t t) { return t < (1 << 30); };
-  if (rows <= 48ll * used) {
+  a.rows = (int32_t)rows;
+  if (rows <= 48ll * tab.groups) {
     const int bn = most <= 16 ? 16 : (most <= 32 ? 32 : 64);
     a.n_tiles_n = div_up(features, BM);
-    const int64_t t = count_tiles(tab, bn, a.n_tiles_n);
-    if (!tiles_fit(t)) return fail(PS_ERR_BAD_ARG, "too many tiles");
+    const int64_t t = cut_rows(tab, bn, false, a.n_tiles_n);
+    if (t >= 1 << 30) return fail(PS_ERR_BAD_ARG, "too many tiles");
     a.n_tiles = (int)t;
     const int split = split_for(t, blocks, 2 * sms);
     if (bn == 16) return launch<Few<OP, 16>>(p, split);
@@ -802,21 +899,22 @@ int32_t run_rows(Problem& p, int features, int red, bool fp32_out) {
     return launch<Few<OP, 64>>(p, split);
   }
   a.n_tiles_n = div_up(features, 256);
-  const int64_t pairs = count_tiles(tab, 256, a.n_tiles_n);
-  if (!tiles_fit(pairs * 2)) return fail(PS_ERR_BAD_ARG, "too many tiles");
-  if (pairs * 2 >= sms && padded_rows(tab, 256) * 5 <= padded_rows(tab, 128) * 6) {
-    a.n_tiles = (int)pairs;
+  const int64_t row_blocks = cut_rows(tab, BM, false), pairs = cut_rows(tab, BM, true), singles = row_blocks * a.n_tiles_n;
+  if (singles >= 1 << 30) return fail(PS_ERR_BAD_ARG, "too many tiles");
+  if (pairs * a.n_tiles_n * 2 >= sms && pairs * 10 <= row_blocks * 6) {
+    a.m_tiles = (int)pairs;
+    a.n_tiles = (int)pairs * a.n_tiles_n;
     if constexpr (OP == D_FWD) if (fp32_out) return launch<Pair<OP, true>>(p, 1);
     return launch<Pair<OP, false>>(p, 1);
   }
-  const int64_t singles = count_tiles(tab, 128, a.n_tiles_n);
+  a.m_tiles = (int)row_blocks;
   if (singles * 3 >= sms * 2) {
     a.n_tiles = (int)singles;
     if constexpr (OP == D_FWD) if (fp32_out) return launch<Single<OP, true>>(p, 1);
     return launch<Single<OP, false>>(p, 1);
   }
   a.n_tiles_n = div_up(features, 128);
-  a.n_tiles = (int)count_tiles(tab, 128, a.n_tiles_n);
+  a.n_tiles = (int)row_blocks * a.n_tiles_n;
   return launch<Split<OP>>(p, split_for(a.n_tiles, blocks, sms));
 }
 
@@ -824,7 +922,7 @@ int32_t run_weights(Problem& p, int N, int K, bool fp32_out) {
   DenseTab& tab = p.tab;
   DenseArgs& a = p.args;
   int most = 0;
-  for (int g = 0; g < tab.groups; ++g) most = std::max(most, tab.row0[g + 1] - tab.row0[g]);
+  for (int g = 0; g < tab.groups; ++g) most = std::max(most, tab.row1[g] - tab.row0[g]);
   const int sms = g_sm_count;
   a.m_side = N; a.n_side = K; a.red = 0;
   a.n_tiles_n = div_up(K, 256);
@@ -844,19 +942,27 @@ int32_t run_weights(Problem& p, int N, int K, bool fp32_out) {
   return launch<Split<D_DW>>(p, split_for(a.n_tiles, div_up(most, BK), sms));
 }
 
-// Groups with the same weights one after another are one group: their rows lie together.
-void merge_groups(const int32_t* rows, const int32_t* weight_of, int groups, DenseTab& tab) {
-  tab.groups = 0;
-  int at = 0;
+// The groups that have rows, by their weights; those that follow one another, in that order and in memory, are one.
+void sort_groups(const int32_t* rows, const int32_t* weight_of, int groups, DenseTab& tab) {
+  struct Group { int32_t w, row0, row1; } list[PS_MAX_WORKERS];
+  int n = 0, at = 0;
+  bool sorted = true;
   for (int g = 0; g < groups; ++g) {
     if (rows[g] == 0) continue;
-    const uint16_t w = (uint16_t)(weight_of ? weight_of[g] : g);
-    if (tab.groups == 0 || tab.w[tab.groups - 1] != w) {
-      tab.row0[tab.groups] = at;
-      tab.w[tab.groups++] = w;
+    const int32_t w = weight_of ? weight_of[g] : g;
+    if (n && list[n - 1].w == w) list[n - 1].row1 = at + rows[g];
+    else {
+      sorted = sorted && (n == 0 || list[n - 1].w < w);
+      list[n++] = Group{w, at, at + rows[g]};
     }
     at += rows[g];
-    tab.row0[tab.groups] = at;
+  }
+  if (!sorted) std::stable_sort(list, list + n, [](const Group& a, const Group& b) { return a.w < b.w; });
+  tab.groups = n;
+  for (int g = 0; g < n; ++g) {
+    tab.w[g] = (uint16_t)list[g].w;
+    tab.row0[g] = list[g].row0;
+    tab.row1[g] = list[g].row1;
   }
 }
 
@@ -962,7 +1068,7 @@ int32_t workers_dense_forward(const ps_dense_layer* l, const ps_dense_output* o)
   p.b = weight_operand(l);
   Layout ws = {(uint8_t*)l->workspace, l->workspace_bytes};
   if ((rc = lay_out(p.a, ws, p.st)) != PS_OK || (rc = lay_out(p.b, ws, p.st)) != PS_OK) return rc;
-  merge_groups(l->rows, l->weight_of, l->groups, p.tab);
+  sort_groups(l->rows, l->weight_of, l->groups, p.tab);
   DenseEpi& e = p.epi;
   e.in0 = o->bias; e.in0_stride = o->bias_stride; e.v_in0 = vec_ok(o->bias, 0, l->n_weights > 1 ? o->bias_stride : 0, 2);
   e.in1 = o->residual; e.in1_pitch = o->residual_pitch; e.v_in1 = vec_ok(o->residual, o->residual_pitch, 0, 2);
@@ -1009,8 +1115,8 @@ int32_t workers_dense_backward(const ps_dense_layer* l, const ps_dense_gradients
   DenseTab workers = {};
   workers.groups = l->groups;
   for (int g = 0; g < l->groups; ++g) {
-    workers.w[g] = (uint16_t)g;
-    workers.row0[g + 1] = workers.row0[g] + l->rows[g];
+    workers.row0[g] = g ? workers.row1[g - 1] : 0;
+    workers.row1[g] = workers.row0[g] + l->rows[g];
   }
   if (o->db) {
     ColumnSumArgs c = {};
@@ -1028,7 +1134,7 @@ int32_t workers_dense_backward(const ps_dense_layer* l, const ps_dense_gradients
     p.st = st;
     p.a = dy;
     p.b = w;
-    merge_groups(l->rows, l->weight_of, l->groups, p.tab);
+    sort_groups(l->rows, l->weight_of, l->groups, p.tab);
     DenseEpi& e = p.epi;
     e.in1 = o->dx_add; e.in1_pitch = o->dx_add_pitch; e.v_in1 = vec_ok(o->dx_add, o->dx_add_pitch, 0, 2);
     e.in2 = o->x_pre; e.in2_pitch = o->x_pre_pitch; e.v_in2 = vec_ok(o->x_pre, o->x_pre_pitch, 0, 2);
