@@ -84,7 +84,7 @@ struct DenseEpi {
   void *out0, *out1;
   int64_t in0_stride, in1_pitch, in2_pitch, out0_pitch, out0_stride, out1_pitch;
   int32_t act, bf16, out0_fp32, accumulate;
-  int32_t v_in0, v_in1, v_in2, v_out0, v_out1;      // may four values be moved at once?
+  int32_t v_in0, v_in1, v_in2, v_out0, v_out1, v_all;      // may four values be moved at once? (v_all: in everything there is)
 };
 
 struct DenseArgs {
@@ -111,9 +111,11 @@ __device__ __forceinline__ uint32_t narrow2(float lo, float hi, int bf16) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 // Four consecutive 16-bit values from element i on, of which n exist, as they lie; and as floats.
+// FULL: all four do, and may be moved at once.
+template <bool FULL = false>
 __device__ __forceinline__ uint2 raw4(const void* base, int64_t i, int n, int vec) {
   const uint16_t* p = reinterpret_cast<const uint16_t*>(base) + i;
-  if (vec && n >= 4) return *reinterpret_cast<const uint2*>(p);
+  if (FULL || (vec && n >= 4)) return *reinterpret_cast<const uint2*>(p);
   uint2 w = make_uint2(p[0], 0u);
   if (n > 1) w.x |= (uint32_t)p[1] << 16;
   if (n > 2) w.y = p[2];
@@ -123,10 +125,11 @@ __device__ __forceinline__ uint2 raw4(const void* base, int64_t i, int n, int ve
 __device__ __forceinline__ float4 widen4(const uint2& w, int bf16) {
   return make_float4(widen(w.x & 0xFFFFu, bf16), widen(w.x >> 16, bf16), widen(w.y & 0xFFFFu, bf16), widen(w.y >> 16, bf16));
 }
+template <bool FULL>
 __device__ __forceinline__ void store4(void* base, int64_t i, int n, int vec, int bf16, const float4& v) {
   uint16_t* p = reinterpret_cast<uint16_t*>(base) + i;
   const uint32_t a = narrow2(v.x, v.y, bf16), b = narrow2(v.z, v.w, bf16);
-  if (vec && n >= 4) {
+  if (FULL || (vec && n >= 4)) {
     *reinterpret_cast<uint2*>(p) = make_uint2(a, b);
     return;
   }
@@ -135,12 +138,14 @@ __device__ __forceinline__ void store4(void* base, int64_t i, int n, int vec, in
   if (n > 2) p[2] = (uint16_t)b;
   if (n > 3) p[3] = (uint16_t)(b >> 16);
 }
+template <bool FULL>
 __device__ __forceinline__ float4 load4_f32(const float* p, int n, int vec) {
-  if (vec && n >= 4) return *reinterpret_cast<const float4*>(p);
+  if (FULL || (vec && n >= 4)) return *reinterpret_cast<const float4*>(p);
   return make_float4(p[0], n > 1 ? p[1] : 0.f, n > 2 ? p[2] : 0.f, n > 3 ? p[3] : 0.f);
 }
+template <bool FULL>
 __device__ __forceinline__ void store4_f32(float* p, int n, int vec, const float4& v) {
-  if (vec && n >= 4) { *reinterpret_cast<float4*>(p) = v; return; }
+  if (FULL || (vec && n >= 4)) { *reinterpret_cast<float4*>(p) = v; return; }
   p[0] = v.x;
   if (n > 1) p[1] = v.y;
   if (n > 2) p[2] = v.z;
@@ -156,72 +161,108 @@ __device__ __forceinline__ float normal_cdf(float z, float& e) {
   const float tail = 0.5f * e * t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
   return z > 0.f ? 1.f - tail : tail;      // NaN: tail is
 }
-__device__ __forceinline__ float activate(float z, int act) {
-  if (act == PS_ACT_RELU) return z < 0.f ? 0.f : z;                 // NaN stays
-  if (act == PS_ACT_GELU) { float e; return z * normal_cdf(z, e); }
-  if (act == PS_ACT_SILU) return __fdividef(z, 1.f + __expf(-z));
+template <int ACT>
+__device__ __forceinline__ float activate(float z) {
+  if (ACT == PS_ACT_RELU) return z < 0.f ? 0.f : z;                 // NaN stays
+  if (ACT == PS_ACT_GELU) { float e; return z * normal_cdf(z, e); }
+  if (ACT == PS_ACT_SILU) return __fdividef(z, 1.f + __expf(-z));
   return z;
 }
 // d * act'(z)
-__device__ __forceinline__ float through(float d, float z, int act) {
-  if (act == PS_ACT_RELU) return z > 0.f ? d : 0.f;
-  if (act == PS_ACT_GELU) {
+template <int ACT>
+__device__ __forceinline__ float through(float d, float z) {
+  if (ACT == PS_ACT_RELU) return z > 0.f ? d : 0.f;
+  if (ACT == PS_ACT_GELU) {
     float e;
     const float c = normal_cdf(z, e);
     return d * fmaf(z * 0.39894228f, e, c);
   }
-  if (act == PS_ACT_SILU) {
+  if (ACT == PS_ACT_SILU) {
     const float e = __fdividef(1.f, 1.f + __expf(-z));
     return d * (e * fmaf(z, 1.f - e, 1.f));
   }
   return d;
 }
-__device__ __forceinline__ float4 activate4(const float4& z, int act) { return make_float4(activate(z.x, act), activate(z.y, act), activate(z.z, act), activate(z.w, act)); }
-__device__ __forceinline__ float4 through4(const float4& d, const float4& z, int act) {
-  return make_float4(through(d.x, z.x, act), through(d.y, z.y, act), through(d.z, z.z, act), through(d.w, z.w, act));
+// f(activation as a constant)
+template <typename F> __device__ __forceinline__ void with_activation(int act, F f) {
+  if (act == PS_ACT_RELU) f(std::integral_constant<int, PS_ACT_RELU>());
+  else if (act == PS_ACT_GELU) f(std::integral_constant<int, PS_ACT_GELU>());
+  else if (act == PS_ACT_SILU) f(std::integral_constant<int, PS_ACT_SILU>());
 }
 
 // What the elementwise part reads for four consecutive columns of a row.  Loaded well before it is used: in a tile's read-out nothing else hides
 // the loads (with loads where they were used, the input gradient of 16,384 x 4096 x 4096 with everything on took 787 us, alone 345).
 template <int OP> struct EpiIn { uint2 a, b; };
 template <> struct EpiIn<D_DW> { float4 a; };
-template <int OP>
+template <int OP, bool FULL>
 __device__ __forceinline__ EpiIn<OP> load_in(const DenseEpi& e, int64_t row, int col, int n, int which) {
   EpiIn<OP> x;
   if constexpr (OP == D_DW) {
     x.a = make_float4(0.f, 0.f, 0.f, 0.f);
     if (e.accumulate) {
       const int64_t at = (int64_t)which * e.out0_stride + row * e.out0_pitch + col;
-      x.a = e.out0_fp32 ? load4_f32(reinterpret_cast<const float*>(e.out0) + at, n, e.v_out0) : widen4(raw4(e.out0, at, n, e.v_out0), e.bf16);
+      x.a = e.out0_fp32 ? load4_f32<FULL>(reinterpret_cast<const float*>(e.out0) + at, n, e.v_out0) : widen4(raw4<FULL>(e.out0, at, n, e.v_out0), e.bf16);
     }
   } else {
     x.a = x.b = make_uint2(0u, 0u);
-    if (e.in1) x.a = raw4(e.in1, row * e.in1_pitch + col, n, e.v_in1);
-    if (OP == D_DX && e.out1) x.b = raw4(e.in2, row * e.in2_pitch + col, n, e.v_in2);
+    if (e.in1) x.a = raw4<FULL>(e.in1, row * e.in1_pitch + col, n, e.v_in1);
+    if (OP == D_DX && e.out1) x.b = raw4<FULL>(e.in2, row * e.in2_pitch + col, n, e.v_in2);
   }
   return x;
 }
 
-// Everything elementwise for four consecutive columns of a row.  which: the weight matrix (forward) or the worker (weight gradient); bias: in0's
-// four values, loaded by the caller, whose column stays the same over many rows.
-template <int OP>
-__device__ __forceinline__ void finish4(const DenseEpi& e, int64_t row, int col, int n, int which, const float4& bias, const EpiIn<OP>& in, float4 v) {
+// Everything elementwise for four consecutive columns of R rows, row0 + i * step, of which those below `end` exist.  which: the weight matrix
+// (forward) or the worker (weight gradient); bias: in0's four values.  FULL: nothing is cut off and everything may be moved four values at
+// once.  One kind of work for all rows, then the next: with the rows one after the other, and every choice made for each of them, a tile's read-out was
+// a chain of latencies twice as long as its products (24 workers' rows of 2048 -> 5000 with everything on 317 us -> RAGGED_NOW).
+template <int OP, int R, bool FULL>
+__device__ __forceinline__ void finish_rows(const DenseEpi& e, int64_t row0, int step, int64_t end, int col, int n, int which, const float4& bias, const EpiIn<OP> (&in)[R],
+                                            float4 (&v)[R]) {
+  auto each = [&](auto f) {
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+      if (FULL || row0 + i * step < end) f(i, row0 + i * step);
+  };
   if constexpr (OP == D_FWD) {
-    v = add(v, bias);
-    if (e.out1) store4(e.out1, row * e.out1_pitch + col, n, e.v_out1, e.bf16, v);
-    if (e.act != PS_ACT_NONE) v = activate4(v, e.act);
-    if (e.in1) v = add(v, widen4(in.a, e.bf16));
-    if (e.out0_fp32) store4_f32(reinterpret_cast<float*>(e.out0) + row * e.out0_pitch + col, n, e.v_out0, v);
-    else store4(e.out0, row * e.out0_pitch + col, n, e.v_out0, e.bf16, v);
+#pragma unroll
+    for (int i = 0; i < R; ++i) v[i] = add(v[i], bias);
+    if (e.out1) each([&](int i, int64_t r) { store4<FULL>(e.out1, r * e.out1_pitch + col, n, e.v_out1, e.bf16, v[i]); });
+    with_activation(e.act, [&](auto act) {
+      constexpr int A = decltype(act)::value;
+#pragma unroll
+      for (int i = 0; i < R; ++i) v[i] = make_float4(activate<A>(v[i].x), activate<A>(v[i].y), activate<A>(v[i].z), activate<A>(v[i].w));
+    });
+    if (e.in1) {
+#pragma unroll
+      for (int i = 0; i < R; ++i) v[i] = add(v[i], widen4(in[i].a, e.bf16));
+    }
+    if (e.out0_fp32) each([&](int i, int64_t r) { store4_f32<FULL>(reinterpret_cast<float*>(e.out0) + r * e.out0_pitch + col, n, e.v_out0, v[i]); });
+    else each([&](int i, int64_t r) { store4<FULL>(e.out0, r * e.out0_pitch + col, n, e.v_out0, e.bf16, v[i]); });
   } else if constexpr (OP == D_DX) {
-    if (e.in1) v = add(v, widen4(in.a, e.bf16));
-    if (e.out0) store4(e.out0, row * e.out0_pitch + col, n, e.v_out0, e.bf16, v);
-    if (e.out1) store4(e.out1, row * e.out1_pitch + col, n, e.v_out1, e.bf16, through4(v, widen4(in.b, e.bf16), e.act));
+    if (e.in1) {
+#pragma unroll
+      for (int i = 0; i < R; ++i) v[i] = add(v[i], widen4(in[i].a, e.bf16));
+    }
+    if (e.out0) each([&](int i, int64_t r) { store4<FULL>(e.out0, r * e.out0_pitch + col, n, e.v_out0, e.bf16, v[i]); });
+    if (e.out1) {
+      with_activation(e.act, [&](auto act) {
+        constexpr int A = decltype(act)::value;
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+          const float4 z = widen4(in[i].b, e.bf16);
+          v[i] = make_float4(through<A>(v[i].x, z.x), through<A>(v[i].y, z.y), through<A>(v[i].z, z.z), through<A>(v[i].w, z.w));
+        }
+      });
+      each([&](int i, int64_t r) { store4<FULL>(e.out1, r * e.out1_pitch + col, n, e.v_out1, e.bf16, v[i]); });
+    }
   } else {
-    const int64_t at = (int64_t)which * e.out0_stride + row * e.out0_pitch + col;
-    if (e.accumulate) v = add(v, in.a);
-    if (e.out0_fp32) store4_f32(reinterpret_cast<float*>(e.out0) + at, n, e.v_out0, v);
-    else store4(e.out0, at, n, e.v_out0, e.bf16, v);
+    if (e.accumulate) {
+#pragma unroll
+      for (int i = 0; i < R; ++i) v[i] = add(v[i], in[i].a);
+    }
+    const int64_t at = (int64_t)which * e.out0_stride + col;
+    if (e.out0_fp32) each([&](int i, int64_t r) { store4_f32<FULL>(reinterpret_cast<float*>(e.out0) + at + r * e.out0_pitch, n, e.v_out0, v[i]); });
+    else each([&](int i, int64_t r) { store4<FULL>(e.out0, at + r * e.out0_pitch, n, e.v_out0, e.bf16, v[i]); });
   }
 }
 template <int OP>
@@ -548,15 +589,20 @@ __global__ void __launch_bounds__(S::THREADS, 1) dense_gemm(const __grid_constan
       const int m_base = c.m0 + quarter * 32;
       // 32 columns of this warp's 32 rows through shared memory: a lane has a row of the accumulator and stores four columns of eight rows
       float4* stage = reinterpret_cast<float4*>(out_stage + (warp - 2) * 4096);
-      constexpr int AHEAD = S::DRAIN ? 4 : 8;      // the sums take the registers
+      constexpr int AHEAD = S::DRAIN ? 4 : 8;      // rows of a lane at a time: the sums take the registers
       struct Ahead { EpiIn<S::OP> in[AHEAD]; float4 bias; };
+      const bool rows_full = epi.v_all && m_base + 32 <= c.m_end;
       auto read_ahead = [&](Ahead& x, int j0, int i0) {
         const int col = c.n0 + col0 + j0 + (lane & 7) * 4, n = c.n_end - col;
         if (i0 == 0) x.bias = bias4<S::OP>(epi, col, n, c.w);
+        const int64_t m = m_base + i0 * 4 + (lane >> 3);
+        if (rows_full && n >= 4) {
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) {
-          const int m = m_base + (i0 + i) * 4 + (lane >> 3);
-          if (m < c.m_end && n > 0) x.in[i] = load_in<S::OP>(epi, m, col, n, c.w);
+          for (int i = 0; i < AHEAD; ++i) x.in[i] = load_in<S::OP, true>(epi, m + 4 * i, col, n, c.w);
+        } else {
+#pragma unroll
+          for (int i = 0; i < AHEAD; ++i)
+            if (m + 4 * i < c.m_end && n > 0) x.in[i] = load_in<S::OP, false>(epi, m + 4 * i, col, n, c.w);
         }
       };
       auto write_out = [&](const float* v, int j0, Ahead& x) {
@@ -566,10 +612,17 @@ __global__ void __launch_bounds__(S::THREADS, 1) dense_gemm(const __grid_constan
         for (int q = 0; q < 8; ++q) stage[lane * 8 + (q ^ (lane & 7))] = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
         __syncwarp();
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          if (i > 0 && i % AHEAD == 0) read_ahead(x, j0, i);
-          const int r = i * 4 + (lane >> 3), m = m_base + r;
-          if (m < c.m_end && n > 0) finish4<S::OP>(epi, m, col, n, c.w, x.bias, x.in[i % AHEAD], stage[r * 8 + ((lane & 7) ^ (r & 7))]);
+        for (int i0 = 0; i0 < 8; i0 += AHEAD) {
+          if (i0 > 0) read_ahead(x, j0, i0);
+          float4 u[AHEAD];
+#pragma unroll
+          for (int i = 0; i < AHEAD; ++i) {
+            const int r = (i0 + i) * 4 + (lane >> 3);
+            u[i] = stage[r * 8 + ((lane & 7) ^ (r & 7))];
+          }
+          const int64_t m = m_base + i0 * 4 + (lane >> 3);
+          if (rows_full && n >= 4) finish_rows<S::OP, AHEAD, true>(epi, m, 4, c.m_end, col, n, c.w, x.bias, x.in, u);
+          else if (n > 0) finish_rows<S::OP, AHEAD, false>(epi, m, 4, c.m_end, col, n, c.w, x.bias, x.in, u);
         }
       };
       if constexpr (S::DRAIN) {
@@ -661,21 +714,24 @@ __global__ void __launch_bounds__(S::THREADS, 1) dense_gemm(const __grid_constan
     const int rows = S::FEW ? min(S::BN, c.n_end - c.n0) : min(BM, c.m_end - c.m0);
     const int row0 = S::FEW ? c.n0 : c.m0, column0 = S::FEW ? c.m0 : c.n0, end = S::FEW ? c.m_end : c.n_end;
     float* part = reinterpret_cast<float*>(tiles);
-    constexpr int AT_ONCE = 4;
-    for (int e0 = me * S::THREADS + tid; e0 < rows * QUADS; e0 += AT_ONCE * ranks * S::THREADS) {
-      EpiIn<S::OP> in[AT_ONCE];
+    // a thread keeps its columns and goes down the rows, four at a time
+    constexpr int AT_ONCE = 4, ROWS = S::THREADS / QUADS;      // rows that a CTA covers at once
+    const int q = tid % QUADS, col = column0 + 4 * q, n = end - col, step = ranks * ROWS;
+    if (tid < ROWS * QUADS && n > 0) {
+      const float4 bias = bias4<S::OP>(epi, col, n, c.w);
+      for (int r0 = me * ROWS + tid / QUADS; r0 < rows; r0 += AT_ONCE * step) {
+        EpiIn<S::OP> in[AT_ONCE];
+        float4 v[AT_ONCE];
 #pragma unroll
-      for (int i = 0; i < AT_ONCE; ++i) {
-        const int e = e0 + i * ranks * S::THREADS, r = e / QUADS, col = column0 + 4 * (e - r * QUADS), n = end - col;
-        if (e < rows * QUADS && n > 0) in[i] = load_in<S::OP>(epi, row0 + r, col, n, c.w);
-      }
+        for (int i = 0; i < AT_ONCE; ++i)
+          if (r0 + i * step < rows) in[i] = load_in<S::OP, false>(epi, row0 + r0 + i * step, col, n, c.w);
 #pragma unroll
-      for (int i = 0; i < AT_ONCE; ++i) {
-        const int e = e0 + i * ranks * S::THREADS, r = e / QUADS, q = e - r * QUADS, col = column0 + 4 * q, n = end - col;
-        if (e >= rows * QUADS || n <= 0) continue;
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int k = 0; k < ranks; ++k) v = add(v, *reinterpret_cast<const float4*>(cl.map_shared_rank(part, k) + r * S::PART_PITCH + 4 * q));
-        finish4<S::OP>(epi, row0 + r, col, n, c.w, bias4<S::OP>(epi, col, n, c.w), in[i], v);
+        for (int i = 0; i < AT_ONCE; ++i) {
+          v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (r0 + i * step < rows)
+            for (int k = 0; k < ranks; ++k) v[i] = add(v[i], *reinterpret_cast<const float4*>(cl.map_shared_rank(part, k) + (r0 + i * step) * S::PART_PITCH + 4 * q));
+        }
+        finish_rows<S::OP, AT_ONCE, false>(epi, row0 + r0, step, row0 + rows, col, n, c.w, bias, in, v);
       }
     }
     cl.sync();                               // a CTA's shared memory outlives its readers
@@ -687,34 +743,47 @@ __global__ void __launch_bounds__(S::THREADS, 1) dense_gemm(const __grid_constan
 }
 
 // ---- the bias gradient: column sums of each worker's rows ------------------------------------------------------------------
-// A CTA sums 64 columns (128 bytes of a row) over its share of a worker's rows; the CTAs of a cluster share a worker's rows and add their
-// sums in order.
-constexpr int CSUM_TPB = 256;
+// A CTA sums 64 columns (128 bytes of a row) over its share of a worker's rows, eight rows' loads of a thread under way at once; the CTAs of a
+// cluster share a worker's rows and add their sums in order.
+constexpr int CSUM_TPB = 256, CSUM_COLS = 64, CSUM_ROWS = CSUM_TPB / (CSUM_COLS / 8);      // rows that a CTA reads at once
 struct ColumnSumArgs {
   const void* dy; void* db;
   int64_t pitch, db_stride;
   int32_t N, bf16, db_fp32, accumulate, vec;
 };
 __global__ void __launch_bounds__(CSUM_TPB) column_sums(const __grid_constant__ ColumnSumArgs a, const __grid_constant__ DenseTab tab) {
-  __shared__ float part[CSUM_TPB / 8][64 + 1];
-  __shared__ float mine[64];
+  __shared__ float part[CSUM_ROWS][CSUM_COLS + 4];
+  __shared__ float mine[CSUM_COLS];
   pdl_enter();
-  const int g = blockIdx.y, ranks = gridDim.z, me = blockIdx.z, col = blockIdx.x * 64 + (threadIdx.x & 7) * 8, n = a.N - col;
+  const int slot = threadIdx.x >> 3, place = (threadIdx.x & 7) * 8;
+  const int g = blockIdx.y, ranks = gridDim.z, me = blockIdx.z, col = blockIdx.x * CSUM_COLS + place, n = a.N - col;
   const int first = tab.row0[g], rows = tab.row1[g] - first;
   const int r0 = first + (int)((int64_t)rows * me / ranks), r1 = first + (int)((int64_t)rows * (me + 1) / ranks);
   float acc[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) acc[j] = 0.f;
   if (n > 0) {
-#pragma unroll 8
-    for (int r = r0 + (threadIdx.x >> 3); r < r1; r += CSUM_TPB / 8) {
-      const uint16_t* p = reinterpret_cast<const uint16_t*>(a.dy) + (int64_t)r * a.pitch + col;
-      if (a.vec && n >= 8) {
-        const uint4 w = *reinterpret_cast<const uint4*>(p);
+    const uint16_t* p = reinterpret_cast<const uint16_t*>(a.dy) + (int64_t)(r0 + slot) * a.pitch + col;
+    const int64_t step = (int64_t)CSUM_ROWS * a.pitch;
+    int r = r0 + slot;
+    if (a.vec && n >= 8) {
+      constexpr int U = 8;
+      auto take = [&](const uint4& w) {
         const uint32_t x[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
         for (int j = 0; j < 8; ++j) acc[j] += widen((x[j >> 1] >> (16 * (j & 1))) & 0xFFFFu, a.bf16);
-      } else {
+      };
+      for (; r + (U - 1) * CSUM_ROWS < r1; r += U * CSUM_ROWS) {
+        uint4 w[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) w[u] = *reinterpret_cast<const uint4*>(p + u * step);
+        p += U * step;
+#pragma unroll
+        for (int u = 0; u < U; ++u) take(w[u]);
+      }
+      for (; r < r1; r += CSUM_ROWS, p += step) take(*reinterpret_cast<const uint4*>(p));
+    } else {
+      for (; r < r1; r += CSUM_ROWS, p += step) {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
           if (j < n) acc[j] += widen(p[j], a.bf16);
@@ -722,18 +791,18 @@ __global__ void __launch_bounds__(CSUM_TPB) column_sums(const __grid_constant__ 
     }
   }
 #pragma unroll
-  for (int j = 0; j < 8; ++j) part[threadIdx.x >> 3][(threadIdx.x & 7) * 8 + j] = acc[j];
+  for (int j = 0; j < 8; j += 4) *reinterpret_cast<float4*>(&part[slot][place + j]) = make_float4(acc[j], acc[j + 1], acc[j + 2], acc[j + 3]);
   __syncthreads();
-  if (threadIdx.x < 64) {
+  if (threadIdx.x < CSUM_COLS) {
     float s = 0.f;
-#pragma unroll 8
-    for (int i = 0; i < CSUM_TPB / 8; ++i) s += part[i][threadIdx.x];
+#pragma unroll
+    for (int i = 0; i < CSUM_ROWS; ++i) s += part[i][threadIdx.x];
     mine[threadIdx.x] = s;
   }
   cg::cluster_group cl = cg::this_cluster();
   cl.sync();
-  const int c = blockIdx.x * 64 + threadIdx.x;
-  if (me == 0 && threadIdx.x < 64 && c < a.N) {
+  const int c = blockIdx.x * CSUM_COLS + threadIdx.x;
+  if (me == 0 && threadIdx.x < CSUM_COLS && c < a.N) {
     float s = 0.f;
     for (int k = 0; k < ranks; ++k) s += cl.map_shared_rank(mine, k)[threadIdx.x];
     const int64_t at = (int64_t)g * a.db_stride + c;
@@ -887,6 +956,7 @@ int32_t run_rows(Problem& p, int features, int red, bool fp32_out) {
   a.n_side = features;
   a.red = red;
   a.rows = (int32_t)rows;
+  fp32_out = fp32_out && red > DRAIN_BLOCKS * BK;      // a shorter sum takes one accumulator either way
   if (rows <= 48ll * tab.groups) {
     const int bn = most <= 16 ? 16 : (most <= 32 ? 32 : 64);
     a.n_tiles_n = div_up(features, BM);
@@ -923,6 +993,7 @@ int32_t run_weights(Problem& p, int N, int K, bool fp32_out) {
   DenseArgs& a = p.args;
   int most = 0;
   for (int g = 0; g < tab.groups; ++g) most = std::max(most, tab.row1[g] - tab.row0[g]);
+  fp32_out = fp32_out && most > DRAIN_BLOCKS * BK;
   const int sms = g_sm_count;
   a.m_side = N; a.n_side = K; a.red = 0;
   a.n_tiles_n = div_up(K, 256);
@@ -1075,6 +1146,7 @@ int32_t workers_dense_forward(const ps_dense_layer* l, const ps_dense_output* o)
   e.out0 = o->y; e.out0_pitch = o->y_pitch; e.v_out0 = vec_ok(o->y, o->y_pitch, 0, ys); e.out0_fp32 = ys == 4;
   e.out1 = o->pre; e.out1_pitch = o->pre_pitch; e.v_out1 = vec_ok(o->pre, o->pre_pitch, 0, 2);
   e.act = l->activation; e.bf16 = l->type == PS_TYPE_BF16;
+  e.v_all = e.v_out0 && (!o->pre || e.v_out1) && (!o->residual || e.v_in1);
   return run_rows<D_FWD>(p, N, K, ys == 4);
 }
 
@@ -1123,10 +1195,10 @@ int32_t workers_dense_backward(const ps_dense_layer* l, const ps_dense_gradients
     c.dy = o->dy; c.db = o->db; c.pitch = o->dy_pitch; c.db_stride = o->db_stride;
     c.N = N; c.bf16 = l->type == PS_TYPE_BF16; c.db_fp32 = ds == 4; c.accumulate = o->accumulate;
     c.vec = ((uintptr_t)o->dy & 15) == 0 && o->dy_pitch % 8 == 0;
-    const int blocks = div_up(N, 64) * l->groups;
+    const int blocks = div_up(N, CSUM_COLS) * l->groups;
     int split = 1;
-    while (split < 8 && blocks * split < 4 * g_sm_count && rows / l->groups >= 64 * split) split *= 2;
-    launch_cluster(column_sums, dim3((unsigned)div_up(N, 64), (unsigned)l->groups, (unsigned)split), CSUM_TPB, 0, split, st, c, workers);
+    while (split < 8 && blocks * split < 4 * g_sm_count && rows / l->groups >= CSUM_ROWS * split) split *= 2;
+    launch_cluster(column_sums, dim3((unsigned)div_up(N, CSUM_COLS), (unsigned)l->groups, (unsigned)split), CSUM_TPB, 0, split, st, c, workers);
     if (cudaGetLastError() != cudaSuccess) return fail(PS_ERR_CUDA, "column sum launch");
   }
   if (o->dx || o->dx_pre) {
@@ -1141,7 +1213,8 @@ int32_t workers_dense_backward(const ps_dense_layer* l, const ps_dense_gradients
     e.out0 = o->dx; e.out0_pitch = o->dx_pitch; e.v_out0 = vec_ok(o->dx, o->dx_pitch, 0, 2);
     e.out1 = o->dx_pre; e.out1_pitch = o->dx_pre_pitch; e.v_out1 = vec_ok(o->dx_pre, o->dx_pre_pitch, 0, 2);
     e.act = l->activation; e.bf16 = l->type == PS_TYPE_BF16;
-      if ((rc = run_rows<D_DX>(p, K, N, false)) != PS_OK) return rc;
+    e.v_all = (!o->dx || e.v_out0) && (!o->dx_pre || (e.v_out1 && e.v_in2)) && (!o->dx_add || e.v_in1);
+    if ((rc = run_rows<D_DX>(p, K, N, false)) != PS_OK) return rc;
   }
   if (o->dw) {
     Problem p = {};
@@ -1153,7 +1226,8 @@ int32_t workers_dense_backward(const ps_dense_layer* l, const ps_dense_gradients
     e.out0 = o->dw; e.out0_pitch = o->dw_pitch; e.out0_stride = o->dw_stride; e.out0_fp32 = ds == 4; e.accumulate = o->accumulate;
     e.v_out0 = vec_ok(o->dw, o->dw_pitch, l->groups > 1 ? o->dw_stride : 0, ds);
     e.bf16 = l->type == PS_TYPE_BF16;
-      if ((rc = run_weights(p, N, K, ds == 4)) != PS_OK) return rc;
+    e.v_all = e.v_out0;
+    if ((rc = run_weights(p, N, K, ds == 4)) != PS_OK) return rc;
   }
   return PS_OK;
 }

@@ -25,6 +25,7 @@ static int32_t (*f_apply_summed)(ps_ctx*, const float*, int32_t, float, float, p
 static int32_t (*f_apply_adamw)(ps_ctx*, ps_mode, const ps_adamw_hyper*, double, float*, float*, float, const int32_t*, float, ps_apply_result*);
 static int32_t (*f_adamw_step)(ps_adamw*, const ps_adamw_hyper*);
 static int32_t (*f_dense_forward)(const ps_dense_layer*, const ps_dense_output*);
+static int32_t (*f_dense_workspace)(const ps_dense_layer*, const void*, int64_t, uint64_t*);
 static int32_t (*f_dense_backward)(const ps_dense_layer*, const ps_dense_gradients*);
 static const char* (*f_error)(ps_ctx*);
 static PyObject *snapshot_type, *error_type;
@@ -162,7 +163,8 @@ static PyObject* bind(PyObject* m, PyObject* const* a, Py_ssize_t nargs) {
       {"workers_grad_step_summed", (void**)&f_summed}, {"workers_eval", (void**)&f_eval}, {"ps_enqueue", (void**)&f_enqueue},
       {"ps_apply", (void**)&f_apply}, {"ps_apply_stale", (void**)&f_apply_stale}, {"ps_apply_summed", (void**)&f_apply_summed}, {"ps_last_error", (void**)&f_error},
       {"ps_apply_adamw", (void**)&f_apply_adamw}, {"ps_adamw_step", (void**)&f_adamw_step},
-      {"workers_dense_forward", (void**)&f_dense_forward}, {"workers_dense_backward", (void**)&f_dense_backward}};
+      {"workers_dense_forward", (void**)&f_dense_forward}, {"workers_dense_backward", (void**)&f_dense_backward},
+      {"workers_dense_workspace", (void**)&f_dense_workspace}};
   for (size_t i = 0; i < sizeof(table) / sizeof(table[0]); ++i) {
     PyObject* addr = PyDict_GetItemString(a[0], table[i].name);
     if (!addr) { PyErr_SetString(PyExc_KeyError, table[i].name); return NULL; }
@@ -409,79 +411,225 @@ static int group_ints(PyObject* o, int32_t* out, Py_ssize_t* n) {
   done(&b);
   return 0;
 }
-static int as_i64(PyObject* o, int64_t* v) { return as_u64(o, (uint64_t*)v); }
 
-/* rows, weight_of | None, n_weights, in_features, out_features, type, activation, x, x_pitch, weight, weight_pitch, weight_stride, workspace | None,
- * workspace_bytes, stream: a[0] .. a[14] */
-#define LAYER_ARGS 15
-static int layer(PyObject* const* a, ps_dense_layer* l, int32_t* rows, int32_t* weights) {
-  Py_ssize_t n, nw;
-  memset(l, 0, sizeof(*l));
-  if (a[0] == Py_None) { PyErr_SetString(PyExc_TypeError, "rows are wanted"); return -1; }
-  if (group_ints(a[0], rows, &n)) return -1;
-  l->groups = n > PS_MAX_WORKERS ? PS_MAX_WORKERS + 1 : (int32_t)n;      /* more than that the library refuses */
-  l->rows = rows;
-  if (a[1] != Py_None) {
-    if (group_ints(a[1], weights, &nw)) return -1;
-    if (nw != n) { PyErr_SetString(PyExc_ValueError, "weight_of: one snapshot per group is wanted"); return -1; }
-    l->weight_of = weights;
+/* ---- torch tensors, by their Python attributes (a call's tensors cost 0.5 us each here, 1.1 in Python) ---- */
+typedef struct {
+  char* p;
+  Py_ssize_t dims, size[3];
+  int64_t stride[3];
+  PyObject* dtype;                /* borrowed: dtypes are singletons that live as long as torch */
+} View;
+
+static PyObject *n_shape, *n_stride, *n_data_ptr, *n_dtype, *n_get_device, *t_float32;
+static PyObject* allocate;        /* allocate(bytes, device) -> a tensor */
+
+static int view(PyObject* t, const char* name, View* v) {
+  PyObject *shape = NULL, *stride = NULL, *ptr = NULL;
+  int rc = -1;
+  if (!(shape = PyObject_GetAttr(t, n_shape)) || !(stride = PyObject_CallMethodNoArgs(t, n_stride)) || !(ptr = PyObject_CallMethodNoArgs(t, n_data_ptr)) ||
+      !(v->dtype = PyObject_GetAttr(t, n_dtype)))
+    goto end;
+  Py_DECREF(v->dtype);
+  if (!PyTuple_Check(shape) || !PyTuple_Check(stride) || (v->dims = PyTuple_GET_SIZE(shape)) < 1 || v->dims > 3 || PyTuple_GET_SIZE(stride) != v->dims) {
+    PyErr_Format(PyExc_ValueError, "%s: a tensor of one to three dimensions is wanted", name);
+    goto end;
   }
-  void *x, *w, *ws, *st;
-  if (i32(a[2], &l->n_weights) || i32(a[3], &l->in_features) || i32(a[4], &l->out_features) || i32(a[5], &l->type) || i32(a[6], &l->activation) ||
-      as_ptr(a[7], &x) || as_i64(a[8], &l->x_pitch) || as_ptr(a[9], &w) || as_i64(a[10], &l->weight_pitch) || as_i64(a[11], &l->weight_stride) ||
-      as_ptr(a[12], &ws) || as_u64(a[13], &l->workspace_bytes) || as_ptr(a[14], &st))
+  for (Py_ssize_t i = 0; i < v->dims; ++i) {
+    v->size[i] = PyLong_AsSsize_t(PyTuple_GET_ITEM(shape, i));
+    v->stride[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(stride, i));
+  }
+  v->p = (char*)PyLong_AsVoidPtr(ptr);
+  rc = PyErr_Occurred() ? -1 : 0;
+end:
+  Py_XDECREF(shape);
+  Py_XDECREF(stride);
+  Py_XDECREF(ptr);
+  return rc;
+}
+static int on_device(PyObject* t, const char* name, long device) {
+  PyObject* d = PyObject_CallMethodNoArgs(t, n_get_device);
+  if (!d) return -1;
+  const long is = PyLong_AsLong(d);
+  Py_DECREF(d);
+  if (is == device && !PyErr_Occurred()) return 0;
+  if (!PyErr_Occurred()) PyErr_Format(PyExc_ValueError, "%s: a tensor on cuda device %ld is wanted", name, device);
+  return -1;
+}
+
+/* A matrix of at least `rows` rows with its columns next to each other; of None: nothing.  Another dtype is refused unless `or_float32`. */
+static int rows_of(PyObject* t, const char* name, int64_t rows, int64_t cols, PyObject* dtype, int or_float32, long device, void** p, int64_t* pitch, PyObject** got) {
+  *p = NULL;
+  *pitch = 0;
+  if (t == Py_None) return 0;
+  View v;
+  if (view(t, name, &v) || on_device(t, name, device)) return -1;
+  if (v.dims != 2 || v.size[0] < rows || v.size[1] != cols || (v.stride[1] != 1 && cols > 1) || (v.dtype != dtype && !(or_float32 && v.dtype == t_float32))) {
+    PyErr_Format(PyExc_ValueError, "%s: at least [%lld, %lld] of %R, columns next to each other, is wanted", name, (long long)rows, (long long)cols, dtype);
     return -1;
-  l->x = x; l->weight = w; l->workspace = ws; l->stream = st;
+  }
+  *p = v.p;
+  *pitch = v.size[0] <= 1 && v.stride[0] < cols ? cols : v.stride[0];
+  if (got) *got = v.dtype;
+  return 0;
+}
+/* A stack of `count` matrices [d1][d2], or of vectors [d2] (d1 < 0); a single one may lack its first dimension. */
+static int stack_of(PyObject* t, const char* name, int64_t count, int64_t d1, int64_t d2, PyObject* dtype, int or_float32, long device, void** p, int64_t* pitch, int64_t* stride,
+                    PyObject** got) {
+  *p = NULL;
+  *pitch = *stride = 0;
+  if (t == Py_None) return 0;
+  View v;
+  if (view(t, name, &v) || on_device(t, name, device)) return -1;
+  const Py_ssize_t inner = d1 < 0 ? 1 : 2;
+  const int single = count == 1 && v.dims == inner;
+  const Py_ssize_t o = single ? 0 : 1;
+  if (v.dims != inner + o || (!single && v.size[0] != count) || (d1 >= 0 && v.size[o] != d1) || v.size[v.dims - 1] != d2 || (v.stride[v.dims - 1] != 1 && d2 > 1) ||
+      (v.dtype != dtype && !(or_float32 && v.dtype == t_float32))) {
+    if (d1 < 0) PyErr_Format(PyExc_ValueError, "%s: [%lld, %lld] of %R, columns next to each other, is wanted", name, (long long)count, (long long)d2, dtype);
+    else PyErr_Format(PyExc_ValueError, "%s: [%lld, %lld, %lld] of %R, columns next to each other, is wanted", name, (long long)count, (long long)d1, (long long)d2, dtype);
+    return -1;
+  }
+  *p = v.p;
+  *stride = single ? 0 : v.stride[0];
+  if (d1 >= 0) *pitch = d1 <= 1 && v.stride[o] < d2 ? d2 : v.stride[o];
+  if (got) *got = v.dtype;
   return 0;
 }
 
-/* (layer..., bias, bias_stride, residual, residual_pitch, y, y_pitch, y_type, pre, pre_pitch) */
-static PyObject* dense_forward(PyObject* m, PyObject* const* a, Py_ssize_t nargs) {
-  WANT(LAYER_ARGS + 9)
+/* A layer's arguments: a[0] x, a[1] weight, a[2] rows, a[3] weight_of | None, a[4] activation, a[5] the operands' type, a[6] device, a[7] stream. */
+#define LAYER_ARGS 8
+typedef struct {
   ps_dense_layer l;
-  ps_dense_output o;
   int32_t rows[PS_MAX_WORKERS], weights[PS_MAX_WORKERS];
-  if (layer(a, &l, rows, weights)) return NULL;
-  a += LAYER_ARGS;
-  memset(&o, 0, sizeof(o));
+  int64_t total, groups;
+  long device;
+  PyObject *dtype, *space;        /* space: the workspace's tensor, or NULL */
+} Layer;
+
+static int layer(PyObject* const* a, Layer* y) {
+  ps_dense_layer* l = &y->l;
+  Py_ssize_t n, nw;
+  void *st, *p;
+  View w;
+  memset(l, 0, sizeof(*l));
+  y->space = NULL;
+  y->device = PyLong_AsLong(a[6]);
+  if (a[2] == Py_None) PyErr_SetString(PyExc_TypeError, "rows are wanted");
+  if (PyErr_Occurred() || group_ints(a[2], y->rows, &n) || i32(a[4], &l->activation) || i32(a[5], &l->type) || as_ptr(a[7], &st)) return -1;
+  y->groups = n;
+  l->groups = n > PS_MAX_WORKERS ? PS_MAX_WORKERS + 1 : (int32_t)n;      /* more than that the library refuses */
+  l->rows = y->rows;
+  y->total = 0;
+  for (Py_ssize_t i = 0; i < n && i < PS_MAX_WORKERS; ++i) y->total += y->rows[i];
+  if (view(a[1], "weight", &w)) return -1;
+  if (w.dims < 2) { PyErr_SetString(PyExc_ValueError, "weight: [n_weights, out_features, in_features] is wanted"); return -1; }
+  const Py_ssize_t count = w.dims == 3 ? w.size[0] : 1, N = w.size[w.dims - 2], K = w.size[w.dims - 1];
+  if (count > INT32_MAX || N > INT32_MAX || K > INT32_MAX) { PyErr_SetString(PyExc_ValueError, "weight is too large"); return -1; }
+  l->n_weights = (int32_t)count;
+  l->out_features = (int32_t)N;
+  l->in_features = (int32_t)K;
+  if (a[3] != Py_None) {
+    if (group_ints(a[3], y->weights, &nw)) return -1;
+    if (nw != n) { PyErr_SetString(PyExc_ValueError, "weight_of: one snapshot per group is wanted"); return -1; }
+    l->weight_of = y->weights;
+  } else if (n != count) {
+    PyErr_SetString(PyExc_ValueError, "weight_of is wanted where the groups are not as many as the weights");
+    return -1;
+  }
+  if (!(y->dtype = PyObject_GetAttr(a[0], n_dtype))) return -1;
+  Py_DECREF(y->dtype);
+  if (rows_of(a[0], "x", y->total < 0 ? 0 : y->total, K, y->dtype, 0, y->device, &p, &l->x_pitch, NULL)) return -1;
+  l->x = p;
+  if (stack_of(a[1], "weight", count, N, K, y->dtype, 0, y->device, &p, &l->weight_pitch, &l->weight_stride, NULL)) return -1;
+  l->weight = p;
+  l->stream = st;
+  return 0;
+}
+/* The workspace, where the tile copies cannot read an operand as it lies. */
+static int workspace(PyObject* device, Layer* y, const void* dy, int64_t dy_pitch) {
+  ps_dense_layer* l = &y->l;
+  if (!((((uintptr_t)l->x | (uintptr_t)l->weight | (uintptr_t)dy) & 15) | ((l->x_pitch | l->weight_pitch | l->weight_stride | dy_pitch) & 7))) return 0;
+  uint64_t need = 0;
+  if (f_dense_workspace(l, dy, dy_pitch, &need) || !need) return 0;      /* a call that is refused here is refused again where it is made */
+  if (!(y->space = PyObject_CallFunction(allocate, "KO", (unsigned long long)need, device))) return -1;
+  PyObject* ptr = PyObject_CallMethodNoArgs(y->space, n_data_ptr);
+  if (!ptr) { Py_CLEAR(y->space); return -1; }
+  l->workspace = PyLong_AsVoidPtr(ptr);
+  l->workspace_bytes = need;
+  Py_DECREF(ptr);
+  return 0;
+}
+
+/* (layer..., bias, residual, y, y_type, pre) */
+static PyObject* dense_forward(PyObject* m, PyObject* const* a, Py_ssize_t nargs) {
+  WANT(LAYER_ARGS + 5)
+  Layer y;
+  ps_dense_output o;
   void *bias, *residual;
-  if (as_ptr(a[0], &bias) || as_i64(a[1], &o.bias_stride) || as_ptr(a[2], &residual) || as_i64(a[3], &o.residual_pitch) || as_ptr(a[4], &o.y) ||
-      as_i64(a[5], &o.y_pitch) || i32(a[6], &o.y_type) || as_ptr(a[7], &o.pre) || as_i64(a[8], &o.pre_pitch))
+  int64_t unused;
+  if (layer(a, &y)) return NULL;
+  PyObject* const* b = a + LAYER_ARGS;
+  const int64_t M = y.total, N = y.l.out_features;
+  memset(&o, 0, sizeof(o));
+  if (stack_of(b[0], "bias", y.l.n_weights, -1, N, y.dtype, 0, y.device, &bias, &unused, &o.bias_stride, NULL) ||
+      rows_of(b[1], "residual", M, N, y.dtype, 0, y.device, &residual, &o.residual_pitch, NULL) ||
+      rows_of(b[2], "y", M, N, y.dtype, 1, y.device, &o.y, &o.y_pitch, NULL) || i32(b[3], &o.y_type) ||
+      rows_of(b[4], "pre", M, N, y.dtype, 0, y.device, &o.pre, &o.pre_pitch, NULL) || workspace(a[6], &y, NULL, 0))
     return NULL;
-  o.bias = bias; o.residual = residual;
+  o.bias = bias;
+  o.residual = residual;
   int32_t rc;
-  CALL(f_dense_forward(&l, &o))
+  CALL(f_dense_forward(&y.l, &o))
+  Py_XDECREF(y.space);
   if (rc) return raise(rc);
   Py_RETURN_NONE;
 }
 
-/* (layer..., dy, dy_pitch, dx_add, dx_add_pitch, x_pre, x_pre_pitch, dx, dx_pitch, dx_pre, dx_pre_pitch, dw, dw_pitch, dw_stride, db, db_stride, dw_type,
- * accumulate) */
+/* (layer..., dy, dx_add, x_pre, dx, dx_pre, dw, db, accumulate) */
 static PyObject* dense_backward(PyObject* m, PyObject* const* a, Py_ssize_t nargs) {
-  WANT(LAYER_ARGS + 17)
-  ps_dense_layer l;
+  WANT(LAYER_ARGS + 8)
+  Layer y;
   ps_dense_gradients o;
-  int32_t rows[PS_MAX_WORKERS], weights[PS_MAX_WORKERS];
-  if (layer(a, &l, rows, weights)) return NULL;
-  a += LAYER_ARGS;
-  memset(&o, 0, sizeof(o));
   void *dy, *add, *pre;
-  if (as_ptr(a[0], &dy) || as_i64(a[1], &o.dy_pitch) || as_ptr(a[2], &add) || as_i64(a[3], &o.dx_add_pitch) || as_ptr(a[4], &pre) ||
-      as_i64(a[5], &o.x_pre_pitch) || as_ptr(a[6], &o.dx) || as_i64(a[7], &o.dx_pitch) || as_ptr(a[8], &o.dx_pre) || as_i64(a[9], &o.dx_pre_pitch) ||
-      as_ptr(a[10], &o.dw) || as_i64(a[11], &o.dw_pitch) || as_i64(a[12], &o.dw_stride) || as_ptr(a[13], &o.db) || as_i64(a[14], &o.db_stride) ||
-      i32(a[15], &o.dw_type) || i32(a[16], &o.accumulate))
+  int64_t unused;
+  PyObject *dw_type = NULL, *db_type = NULL;
+  if (layer(a, &y)) return NULL;
+  PyObject* const* b = a + LAYER_ARGS;
+  const int64_t M = y.total, N = y.l.out_features, K = y.l.in_features;
+  memset(&o, 0, sizeof(o));
+  if (rows_of(b[0], "dy", M, N, y.dtype, 0, y.device, &dy, &o.dy_pitch, NULL) || rows_of(b[1], "dx_add", M, K, y.dtype, 0, y.device, &add, &o.dx_add_pitch, NULL) ||
+      rows_of(b[2], "x_pre", M, K, y.dtype, 0, y.device, &pre, &o.x_pre_pitch, NULL) || rows_of(b[3], "dx", M, K, y.dtype, 0, y.device, &o.dx, &o.dx_pitch, NULL) ||
+      rows_of(b[4], "dx_pre", M, K, y.dtype, 0, y.device, &o.dx_pre, &o.dx_pre_pitch, NULL) ||
+      stack_of(b[5], "dw", y.groups, N, K, y.dtype, 1, y.device, &o.dw, &o.dw_pitch, &o.dw_stride, &dw_type) ||
+      stack_of(b[6], "db", y.groups, -1, N, y.dtype, 1, y.device, &o.db, &unused, &o.db_stride, &db_type) || i32(b[7], &o.accumulate))
     return NULL;
-  o.dy = dy; o.dx_add = add; o.x_pre = pre;
+  if (dw_type && db_type && dw_type != db_type) { PyErr_SetString(PyExc_ValueError, "dw and db of one type are wanted"); return NULL; }
+  if (workspace(a[6], &y, dy, o.dy_pitch)) return NULL;
+  o.dy = dy;
+  o.dx_add = add;
+  o.x_pre = pre;
+  o.dw_type = (dw_type ? dw_type : db_type) == t_float32 ? PS_TYPE_FP32 : y.l.type;
   int32_t rc;
-  CALL(f_dense_backward(&l, &o))
+  CALL(f_dense_backward(&y.l, &o))
+  Py_XDECREF(y.space);
   if (rc) return raise(rc);
+  Py_RETURN_NONE;
+}
+
+/* (torch.float32, allocate) */
+static PyObject* bind_torch(PyObject* m, PyObject* const* a, Py_ssize_t nargs) {
+  WANT(2)
+  Py_INCREF(a[0]);
+  Py_XSETREF(t_float32, a[0]);
+  Py_INCREF(a[1]);
+  Py_XSETREF(allocate, a[1]);
   Py_RETURN_NONE;
 }
 
 #define FAST(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, NULL}
 static PyMethodDef methods[] = {FAST(bind), FAST(pull), FAST(reserve), FAST(grad_step), FAST(grad_step_summed), FAST(eval),
                                 FAST(enqueue), FAST(apply), FAST(apply_stale), FAST(apply_summed), FAST(apply_adamw), FAST(adamw_step),
-                                FAST(dense_forward), FAST(dense_backward), {NULL, NULL, 0, NULL}};
+                                FAST(dense_forward), FAST(dense_backward), FAST(bind_torch), {NULL, NULL, 0, NULL}};
 static struct PyModuleDef def = {PyModuleDef_HEAD_INIT, "_marshal", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
 PyMODINIT_FUNC PyInit__marshal(void) {
@@ -489,5 +637,10 @@ PyMODINIT_FUNC PyInit__marshal(void) {
   k_version = PyUnicode_InternFromString("new_version");
   k_checkpointed = PyUnicode_InternFromString("checkpointed");
   k_replicated = PyUnicode_InternFromString("replicated");
+  n_shape = PyUnicode_InternFromString("shape");
+  n_stride = PyUnicode_InternFromString("stride");
+  n_data_ptr = PyUnicode_InternFromString("data_ptr");
+  n_dtype = PyUnicode_InternFromString("dtype");
+  n_get_device = PyUnicode_InternFromString("get_device");
   return PyModule_Create(&def);
 }

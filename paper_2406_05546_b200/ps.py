@@ -4,7 +4,6 @@ Every step of the hot path runs in the library's CUDA kernels; torch is used for
 pinned memory and for the stream.  There is no CPU fallback: if the library is missing or no
 CUDA device is present, constructing a ParameterServer raises.
 """
-import contextlib
 import ctypes as C
 import os
 
@@ -105,7 +104,6 @@ class DenseGradients(C.Structure):
                 ("dw_type", C.c_int32), ("accumulate", C.c_int32)]
 
 
-_SAME = contextlib.nullcontext()      # the device is current already
 _lib = None
 _marshal = None      # the extension that passes the arguments of the per-tick calls
 
@@ -174,7 +172,7 @@ def load(path=None):
         m.bind({n: C.cast(getattr(L, n), C.c_void_p).value for n in
                 ("ps_pull_snapshot", "ps_queue_reserve", "workers_grad_step", "workers_grad_step_summed", "workers_eval",
                  "ps_enqueue", "ps_apply", "ps_apply_stale", "ps_apply_summed", "ps_apply_adamw",
-                 "ps_adamw_step", "workers_dense_forward", "workers_dense_backward", "ps_last_error")}, Snapshot, PSError,
+                 "ps_adamw_step", "workers_dense_forward", "workers_dense_backward", "workers_dense_workspace", "ps_last_error")}, Snapshot, PSError,
                lambda o, kind: np.ascontiguousarray(o, dtype=(np.int32, np.int64, np.uint64)[kind]),
                lambda snaps, n: (Snapshot * n)(*snaps))
         _lib, _marshal = L, m
@@ -203,67 +201,40 @@ def _np_ptr(a):
     return a.ctypes.data if a is not None else None
 
 
+_TYPES = {}
+
+
 def _type(t):
-    import torch
-    kinds = {torch.float32: TYPE_FP32, torch.bfloat16: TYPE_BF16, torch.float16: TYPE_FP16}
-    if t.dtype not in kinds:
+    if not _TYPES:
+        import torch
+        _TYPES.update({torch.float32: TYPE_FP32, torch.bfloat16: TYPE_BF16, torch.float16: TYPE_FP16})
+    kind = _TYPES.get(t.dtype)
+    if kind is None:
         raise TypeError(f"float32, bfloat16 or float16 is wanted, not {t.dtype}")
-    return kinds[t.dtype]
+    return kind
 
 
-def _rows_of(t, name, rows, cols, like, dtype=None):
-    """(address, pitch) of a matrix with at least `rows` rows; (None, 0) of None."""
-    if t is None:
-        return None, 0
-    if t.dim() != 2 or t.shape[0] < rows or t.shape[1] != cols or t.dtype != (dtype or like.dtype) or t.device != like.device or (t.stride(1) != 1 and cols > 1):
-        raise ValueError(f"{name}: [{rows}, {cols}] of {dtype or like.dtype} on {like.device}, columns next to each other, is wanted")
-    return t.data_ptr(), max(t.stride(0), cols) if t.shape[0] <= 1 else t.stride(0)
+_cuda = None      # torch._C, once the binding knows torch
 
 
-def _stack_of(t, name, shape, like, dtype=None):
-    """(address, pitch, stride) of a stack of matrices (or of vectors: pitch 0), or of a single one; Nones of None."""
-    if t is None:
-        return None, 0, 0
-    if t.dim() == len(shape) - 1:
-        t = t.unsqueeze(0)
-    if tuple(t.shape) != shape or t.dtype != (dtype or like.dtype) or t.device != like.device or (t.stride(-1) != 1 and shape[-1] > 1):
-        raise ValueError(f"{name}: {list(shape)} of {dtype or like.dtype} on {like.device}, columns next to each other, is wanted")
-    pitch = 0 if len(shape) == 2 else (t.stride(1) if shape[1] > 1 else max(t.stride(1), shape[2]))
-    return t.data_ptr(), pitch, t.stride(0)
-
-
-def _dense_layer(x, weight, rows, weight_of, activation, dy):
-    """The marshalled layer (without workspace and stream), its row count and weight count, and what keeps its workspace alive."""
+def _bind_torch():
     import torch
-    if x.device.type != "cuda":
+    global _cuda
+    load()
+    _marshal.bind_torch(torch.float32, lambda size, device: torch.empty(size, dtype=torch.uint8, device=f"cuda:{device}"))
+    _cuda = torch._C
+
+
+def _dense(x, activation):
+    """(activation's number, x's type, its device's number); makes sure that the binding knows torch."""
+    if _cuda is None:
+        _bind_torch()
+    if not x.is_cuda:
         raise ValueError("cuda tensors are wanted")
-    if weight.dim() not in (2, 3):
-        raise ValueError("weight: [n_weights, out_features, in_features] is wanted")
-    n_weights, N, K = (1, *weight.shape) if weight.dim() == 2 else weight.shape
-    if weight_of is None and len(rows) != n_weights:
-        raise ValueError("weight_of is wanted where the groups are not as many as the weights")
-    M = int(sum(rows))
     act = ACTIVATIONS.get(activation, activation)
     if not isinstance(act, int):
         raise ValueError(f"activation {activation!r}: one of {sorted(ACTIVATIONS)} is wanted")
-    xp, x_pitch = _rows_of(x, "x", M, K, x)
-    wp, w_pitch, w_stride = _stack_of(weight, "weight", (n_weights, N, K), x)
-    dp, d_pitch = _rows_of(dy, "dy", M, N, x)
-    kind = _type(x)
-    space, size = None, 0
-    if (xp | wp | (dp or 0) | 2 * (x_pitch | w_pitch | w_stride | d_pitch)) & 15 and M > 0:
-        r = np.ascontiguousarray(rows, dtype=np.int32)
-        w = None if weight_of is None else np.ascontiguousarray(weight_of, dtype=np.int32)
-        l = DenseLayer(len(r), n_weights, r.ctypes.data, _np_ptr(w), K, N, kind, act, xp, x_pitch, wp, w_pitch, w_stride, None, 0, None)
-        need = C.c_uint64()
-        rc = load().workers_dense_workspace(C.byref(l), dp, d_pitch, C.byref(need))
-        if rc != 0:
-            raise PSError(rc, _lib.ps_last_error(None).decode())
-        if need.value:
-            space = torch.empty(need.value, dtype=torch.uint8, device=x.device)
-            size = need.value
-    args = (rows, weight_of, n_weights, K, N, kind, act, xp, x_pitch, wp, w_pitch, w_stride, space.data_ptr() if size else None, size)
-    return args, M, n_weights, N, K, dp, d_pitch, space
+    return act, _type(x), x.get_device()
 
 
 def workers_dense_forward(x, weight, rows, weight_of=None, bias=None, residual=None, activation="none", y=None, pre=None, out_dtype=None):
@@ -271,19 +242,17 @@ def workers_dense_forward(x, weight, rows, weight_of=None, bias=None, residual=N
     [n_weights, N, K] (or [N, K]), bias [n_weights, N], residual [M, N]: bfloat16 or float16 cuda tensors; rows: the groups' rows (their sum may
     be below M: what lies behind is left alone); weight_of: which weights a group uses (default: its own number).  y (allocated if not given; of
     out_dtype, float32 or the operands') and pre (x W^T + bias, if given) are written.  Runs on torch's current stream of x's device.  Returns y."""
-    import torch
-    load()
-    with torch.cuda.device(x.device) if x.device.type == "cuda" and torch.cuda.current_device() != x.device.index else _SAME:
-        args, M, n_weights, N, K, _, _, space = _dense_layer(x, weight, rows, weight_of, activation, None)
-        if y is None:
-            y = torch.empty((x.shape[0], N), dtype=out_dtype or x.dtype, device=x.device)
-        elif out_dtype is not None and y.dtype != out_dtype:
-            raise ValueError(f"y is {y.dtype}, not {out_dtype}")
-        bp, _, b_stride = _stack_of(bias, "bias", (n_weights, N), x)
-        rp, r_pitch = _rows_of(residual, "residual", M, N, x)
-        yp, y_pitch = _rows_of(y, "y", M, N, x, torch.float32 if y.dtype == torch.float32 else x.dtype)
-        pp, p_pitch = _rows_of(pre, "pre", M, N, x)
-        _marshal.dense_forward(*args, torch.cuda.current_stream().cuda_stream, bp, b_stride, rp, r_pitch, yp, y_pitch, _type(y), pp, p_pitch)
+    act, kind, device = _dense(x, activation)
+    if _cuda._cuda_getDevice() != device:
+        import torch
+        with torch.cuda.device(device):
+            return workers_dense_forward(x, weight, rows, weight_of, bias, residual, activation, y, pre, out_dtype)
+    if y is None:
+        import torch
+        y = torch.empty((x.shape[0], weight.shape[-2]), dtype=out_dtype or x.dtype, device=x.device)
+    elif out_dtype is not None and y.dtype != out_dtype:
+        raise ValueError(f"y is {y.dtype}, not {out_dtype}")
+    _marshal.dense_forward(x, weight, rows, weight_of, act, kind, device, _cuda._cuda_getCurrentRawStream(device), bias, residual, y, _type(y), pre)
     return y
 
 
@@ -292,25 +261,14 @@ def workers_dense_backward(dy, x, weight, rows, weight_of=None, x_pre=None, acti
     """The gradients of x W^T + bias (include/ps.h), into those of dx [M, K], dx_pre [M, K], dw [groups, N, K] and db [groups, N] that are given:
     dx = dy W + dx_add, dx_pre = dx * activation'(x_pre), and for every group dw = dy^T x and db = the column sums of dy, which are added to with
     accumulate.  dw and db: float32, or the operands' type.  Otherwise as workers_dense_forward."""
-    import torch
-    load()
-    with torch.cuda.device(x.device) if x.device.type == "cuda" and torch.cuda.current_device() != x.device.index else _SAME:
-        if dy is None:
-            raise ValueError("dy is wanted")
-        args, M, n_weights, N, K, dp, d_pitch, space = _dense_layer(x, weight, rows, weight_of, activation, dy)
-        G = len(rows)
-        grad = dw if dw is not None else db
-        kind = torch.float32 if grad is not None and grad.dtype == torch.float32 else x.dtype
-        ap, a_pitch = _rows_of(dx_add, "dx_add", M, K, x)
-        zp, z_pitch = _rows_of(x_pre, "x_pre", M, K, x)
-        xp, x_pitch = _rows_of(dx, "dx", M, K, x)
-        pp, p_pitch = _rows_of(dx_pre, "dx_pre", M, K, x)
-        wp, w_pitch, w_stride = _stack_of(dw, "dw", (G, N, K), x, kind)
-        bp, _, b_stride = _stack_of(db, "db", (G, N), x, kind)
-        if dx_pre is not None and x_pre is None:
-            raise ValueError("dx_pre needs x_pre")
-        _marshal.dense_backward(*args, torch.cuda.current_stream().cuda_stream, dp, d_pitch, ap, a_pitch, zp, z_pitch, xp, x_pitch, pp, p_pitch, wp, w_pitch,
-                                w_stride, bp, b_stride, TYPE_FP32 if kind == torch.float32 else args[5], accumulate)
+    act, kind, device = _dense(x, activation)
+    if _cuda._cuda_getDevice() != device:
+        import torch
+        with torch.cuda.device(device):
+            return workers_dense_backward(dy, x, weight, rows, weight_of, x_pre, activation, dx_add, dx, dx_pre, dw, db, accumulate)
+    if dy is None or (dx_pre is not None and x_pre is None):
+        raise ValueError("dy, and x_pre for dx_pre, are wanted")
+    _marshal.dense_backward(x, weight, rows, weight_of, act, kind, device, _cuda._cuda_getCurrentRawStream(device), dy, dx_add, x_pre, dx, dx_pre, dw, db, bool(accumulate))
 
 
 def workers_dense_status():
