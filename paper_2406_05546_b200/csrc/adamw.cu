@@ -129,39 +129,55 @@ __device__ __forceinline__ void decode_e4m3(uint2 codes, float scale, float (&x)
 }
 __device__ __forceinline__ void decode_e5m2(uint2 codes, float scale, float (&x)[PER]) {      // a half whose low byte is zero
 #pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const uint32_t c = ((i < 4 ? codes.x : codes.y) >> (8 * (i & 3))) & 0xFFu;
-    x[i] = __half2float(__ushort_as_half((unsigned short)(c << 8))) * scale;
+  for (int i = 0; i < PER / 2; ++i) {
+    const uint32_t h2 = prmt(i < 2 ? codes.x : codes.y, 0u, i & 1 ? 0x3424u : 0x1404u);
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h2));
+    x[2 * i] = f.x * scale;
+    x[2 * i + 1] = f.y * scale;
   }
 }
 __device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & 0x7F800000u) != 0x7F800000u; }
-// The scale that puts the block's largest finite value at 1.75 * 2^top at most (the types' largest values), one warp per block.
-__device__ __forceinline__ uint32_t block_scale(const float (&x)[PER], int top) {
+// The bits of a block's largest magnitude (one warp per block); CHECK: of its finite ones, otherwise at or above those of infinity where one is not.
+template <bool CHECK>
+__device__ __forceinline__ uint32_t block_most(const float (&x)[PER]) {
   uint32_t most = 0;
 #pragma unroll
-  for (int i = 0; i < PER; ++i) most = max(most, finite(x[i]) ? __float_as_uint(x[i]) & 0x7FFFFFFFu : 0u);
-  most = __reduce_max_sync(0xffffffffu, most);
-  return (uint32_t)min(max((int)((most + 0x1FFFFFu) >> 23) - top, 1), 254);
+  for (int i = 0; i < PER; ++i) most = max(most, !CHECK || finite(x[i]) ? __float_as_uint(x[i]) & 0x7FFFFFFFu : 0u);
+  return __reduce_max_sync(0xffffffffu, most);
 }
+// The scale that puts the largest at 1.75 * 2^top at most (the types' largest values).
+__device__ __forceinline__ uint32_t scale_byte(uint32_t most, int top) { return (uint32_t)min(max((int)((most + 0x1FFFFFu) >> 23) - top, 1), 254); }
+template <bool CHECK>
 __device__ __forceinline__ uint2 encode_e4m3(const float (&x)[PER], float inv) {
   uint32_t w[2] = {0u, 0u};
 #pragma unroll
   for (int i = 0; i < PER / 2; ++i) {
-    const float lo = finite(x[2 * i]) ? x[2 * i] * inv : __uint_as_float(0x7FFFFFFFu), hi = finite(x[2 * i + 1]) ? x[2 * i + 1] * inv : __uint_as_float(0x7FFFFFFFu);
+    const float nan = __uint_as_float(0x7FFFFFFFu);
+    const float lo = !CHECK || finite(x[2 * i]) ? x[2 * i] * inv : nan, hi = !CHECK || finite(x[2 * i + 1]) ? x[2 * i + 1] * inv : nan;
     uint16_t two;
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(two) : "f"(hi), "f"(lo));
     w[i >> 1] |= (uint32_t)two << (16 * (i & 1));
   }
   return make_uint2(w[0], w[1]);
 }
-__device__ __forceinline__ uint32_t encode_e5m2(float x, float inv, uint32_t random16) {
-  if (!finite(x)) return 0x7Fu;
+// random21: the random bits, in bits 5 .. 20 (of the 21 that are dropped)
+template <bool CHECK>
+__device__ __forceinline__ uint32_t encode_e5m2(float x, float inv, uint32_t random21) {
+  if (CHECK && !finite(x)) return 0x7Fu;
   const float u = x * inv;      // 0 .. 57,344
   // below 2^-14 the codes are evenly spaced: adding 2^-14 brings them to the places of one binade
   const bool low = u < 6.103515625e-05f;
-  const uint32_t bits = __float_as_uint(low ? __fadd_rn(u, 6.103515625e-05f) : u) + (random16 << 5);
-  const uint32_t c = (bits >> 21) - (low ? 113u * 4u : 112u * 4u);
-  return u > 0.f ? max(c, 1u) : c;
+  const uint32_t bits = __float_as_uint(low ? __fadd_rn(u, 6.103515625e-05f) : u) + random21;
+  return max((bits >> 21) - (low ? 113u * 4u : 112u * 4u), min(__float_as_uint(u), 1u));      // a positive value is not rounded to zero
+}
+template <bool CHECK>
+__device__ __forceinline__ void encode_block(const float (&m)[PER], const float (&v)[PER], float inv_m, float inv_v, const uint4& r, uint2& cm, uint2& cv) {
+  cm = encode_e4m3<CHECK>(m, inv_m);
+  const uint32_t words[4] = {r.x, r.y, r.z, r.w};
+  uint32_t w[2] = {0u, 0u};
+#pragma unroll
+  for (int i = 0; i < PER; ++i) w[i >> 2] |= encode_e5m2<CHECK>(v[i], inv_v, (i & 1 ? words[i >> 1] >> 11 : words[i >> 1] << 5) & 0x1FFFE0u) << (8 * (i & 3));
+  cv = make_uint2(w[0], w[1]);
 }
 
 // ---- one step
@@ -222,7 +238,7 @@ __global__ void __launch_bounds__(TPB) adamw_step(const DevTensor* __restrict__ 
     decode_e5m2(cv, scale_of(t.v_scale[block]), v);
   }
 #pragma unroll
-  for (int i = 0; i < PER; ++i) adam_update(p[i], __fmul_rn(g[i], s.factor), m[i], v[i], s, decay);
+  for (int i = 0; i < PER; i += 2) adam_update2(p[i], p[i + 1], __fmul_rn(g[i], s.factor), __fmul_rn(g[i + 1], s.factor), m[i], m[i + 1], v[i], v[i + 1], s, decay);
   if (vec) store8(reinterpret_cast<P*>(t.p) + i0, p);
   else store_some(reinterpret_cast<P*>(t.p), i0, n, p);
   if constexpr (HAS_COPY) {
@@ -239,27 +255,30 @@ __global__ void __launch_bounds__(TPB) adamw_step(const DevTensor* __restrict__ 
     }
   } else {
     // lanes past the tensor's end hold zero moments: they had zero gradients and moments
-    sm = block_scale(m, 8);
-    sv = block_scale(v, 15);
     const uint64_t j = (uint64_t)(i0 / PER);
     const uint4 r = philox4x32_10(make_uint4((uint32_t)j, (uint32_t)(j >> 32), (uint32_t)ref.tensor, step),
                                   make_uint2((uint32_t)call.seed, (uint32_t)(call.seed >> 32)));
-    const uint32_t words[4] = {r.x, r.y, r.z, r.w};
-    const uint2 cm = encode_e4m3(m, inverse_scale_of(sm));
-    const float inv = inverse_scale_of(sv);
-    uint32_t cv[2] = {0u, 0u};
-#pragma unroll
-    for (int i = 0; i < PER; ++i) cv[i >> 2] |= encode_e5m2(v[i], inv, (words[i >> 1] >> (16 * (i & 1))) & 0xFFFFu) << (8 * (i & 3));
+    uint32_t most_m = block_most<false>(m), most_v = block_most<false>(v);
+    uint2 cm, cv;
+    if (max(most_m, most_v) < 0x7F800000u) {
+      sm = scale_byte(most_m, 8);
+      sv = scale_byte(most_v, 15);
+      encode_block<false>(m, v, inverse_scale_of(sm), inverse_scale_of(sv), r, cm, cv);
+    } else {      // something is not finite
+      sm = scale_byte(block_most<true>(m), 8);
+      sv = scale_byte(block_most<true>(v), 15);
+      encode_block<true>(m, v, inverse_scale_of(sm), inverse_scale_of(sv), r, cm, cv);
+    }
     uint8_t *pm = reinterpret_cast<uint8_t*>(t.m) + i0, *pv = reinterpret_cast<uint8_t*>(t.v) + i0;
     if (vec) {
       *reinterpret_cast<uint2*>(pm) = cm;
-      *reinterpret_cast<uint2*>(pv) = make_uint2(cv[0], cv[1]);
+      *reinterpret_cast<uint2*>(pv) = cv;
     } else {
 #pragma unroll
       for (int i = 0; i < PER; ++i)
         if (i < n) {
           pm[i] = (uint8_t)((i < 4 ? cm.x : cm.y) >> (8 * (i & 3)));
-          pv[i] = (uint8_t)(cv[i >> 2] >> (8 * (i & 3)));
+          pv[i] = (uint8_t)((i < 4 ? cv.x : cv.y) >> (8 * (i & 3)));
         }
     }
     if ((threadIdx.x & 31) == 0) {

@@ -67,10 +67,8 @@ struct AdamW {
   AdamColumns a;
   __device__ __forceinline__ float4 operator()(int col, float4 t, float c, const float4& s) const {
     float4 m = reinterpret_cast<const float4*>(a.m)[col], v = reinterpret_cast<const float4*>(a.v)[col];
-    adam_update(t.x, __fmul_rn(c, s.x), m.x, v.x, a.s, a.decay);
-    adam_update(t.y, __fmul_rn(c, s.y), m.y, v.y, a.s, a.decay);
-    adam_update(t.z, __fmul_rn(c, s.z), m.z, v.z, a.s, a.decay);
-    adam_update(t.w, __fmul_rn(c, s.w), m.w, v.w, a.s, a.decay);
+    adam_update2(t.x, t.y, __fmul_rn(c, s.x), __fmul_rn(c, s.y), m.x, m.y, v.x, v.y, a.s, a.decay);
+    adam_update2(t.z, t.w, __fmul_rn(c, s.z), __fmul_rn(c, s.w), m.z, m.w, v.z, v.w, a.s, a.decay);
     reinterpret_cast<float4*>(a.m)[col] = without_padding(col, m);
     reinterpret_cast<float4*>(a.v)[col] = without_padding(col, v);
     return without_padding(col, t);
@@ -211,10 +209,8 @@ __global__ void __launch_bounds__(TPB) async_adamw(const __grid_constant__ Async
         const float c = a.coef_k ? a.coef_k[ord.slot[k]] : a.coef;
         s.step_size = adam.step_size[k];
         s.rs2 = adam.rs2[k];
-        adam_update(t.x, __fmul_rn(c, g[u].x), m.x, v.x, s, adam.col.decay);
-        adam_update(t.y, __fmul_rn(c, g[u].y), m.y, v.y, s, adam.col.decay);
-        adam_update(t.z, __fmul_rn(c, g[u].z), m.z, v.z, s, adam.col.decay);
-        adam_update(t.w, __fmul_rn(c, g[u].w), m.w, v.w, s, adam.col.decay);
+        adam_update2(t.x, t.y, __fmul_rn(c, g[u].x), __fmul_rn(c, g[u].y), m.x, m.y, v.x, v.y, s, adam.col.decay);
+        adam_update2(t.z, t.w, __fmul_rn(c, g[u].z), __fmul_rn(c, g[u].w), m.z, m.w, v.z, v.w, s, adam.col.decay);
         if (k >= a.first_stored) {
           int slot = (int)((a.v0 + (uint64_t)k + 1) % (uint64_t)a.ring_depth);
           reinterpret_cast<float4*>(a.ring[slot])[col] = without_padding(col, t);
