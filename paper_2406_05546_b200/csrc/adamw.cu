@@ -69,10 +69,8 @@ struct Call {
   int32_t skip_nonfinite;
 };
 
-template <typename T> __device__ __forceinline__ float as_float(T x);
-template <> __device__ __forceinline__ float as_float(float x) { return x; }
-template <> __device__ __forceinline__ float as_float(__nv_bfloat16 x) { return __bfloat162float(x); }
-template <> __device__ __forceinline__ float as_float(__half x) { return __half2float(x); }
+__device__ __forceinline__ float as_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ float as_float(__half x) { return __half2float(x); }
 template <typename T> __device__ __forceinline__ T from_float(float x);
 template <> __device__ __forceinline__ float from_float(float x) { return x; }
 template <> __device__ __forceinline__ __nv_bfloat16 from_float(float x) { return __float2bfloat16_rn(x); }
@@ -87,12 +85,20 @@ __device__ __forceinline__ void store8(float* p, const float (&x)[PER]) {
   asm volatile("st.global.v8.f32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
                ::"l"(p), "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7]) : "memory");
 }
-template <typename T> __device__ __forceinline__ void load8(const T* p, float (&x)[PER]) {
-  const uint4 w = __ldcs(reinterpret_cast<const uint4*>(p));
-  T t[PER];
-  memcpy(t, &w, 16);
+// Eight values as they are loaded.
+template <typename T> struct Raw8 { uint4 w; };
+template <> struct Raw8<float> { float x[PER]; };
+__device__ __forceinline__ void load8(const float* p, Raw8<float>& r) { load8(p, r.x); }
+template <typename T> __device__ __forceinline__ void load8(const T* p, Raw8<T>& r) { r.w = __ldcs(reinterpret_cast<const uint4*>(p)); }
+__device__ __forceinline__ void widen8(const Raw8<float>& r, float (&x)[PER]) {
 #pragma unroll
-  for (int i = 0; i < PER; ++i) x[i] = as_float<T>(t[i]);
+  for (int i = 0; i < PER; ++i) x[i] = r.x[i];
+}
+template <typename T> __device__ __forceinline__ void widen8(const Raw8<T>& r, float (&x)[PER]) {
+  T t[PER];
+  memcpy(t, &r.w, 16);
+#pragma unroll
+  for (int i = 0; i < PER; ++i) x[i] = as_float(t[i]);
 }
 template <typename T> __device__ __forceinline__ void store8(T* p, const float (&x)[PER]) {
   T t[PER];
@@ -103,9 +109,15 @@ template <typename T> __device__ __forceinline__ void store8(T* p, const float (
   *reinterpret_cast<uint4*>(p) = w;
 }
 // n of eight values from i0 on, the others zero / left alone
-template <typename T> __device__ __forceinline__ void load_some(const T* p, int64_t i0, int n, float (&x)[PER]) {
+__device__ __forceinline__ void load_some(const float* p, int64_t i0, int n, Raw8<float>& r) {
 #pragma unroll
-  for (int i = 0; i < PER; ++i) x[i] = i < n ? as_float<T>(p[i0 + i]) : 0.f;
+  for (int i = 0; i < PER; ++i) r.x[i] = i < n ? p[i0 + i] : 0.f;
+}
+template <typename T> __device__ __forceinline__ void load_some(const T* p, int64_t i0, int n, Raw8<T>& r) {
+  T t[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) t[i] = i < n ? p[i0 + i] : from_float<T>(0.f);
+  memcpy(&r.w, t, 16);
 }
 template <typename T> __device__ __forceinline__ void store_some(T* p, int64_t i0, int n, const float (&x)[PER]) {
 #pragma unroll
@@ -137,15 +149,20 @@ __device__ __forceinline__ void decode_e5m2(uint2 codes, float scale, float (&x)
   }
 }
 __device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & 0x7F800000u) != 0x7F800000u; }
-// The bits of a block's largest magnitude (one warp per block); CHECK: of its finite ones, otherwise at or above those of infinity where one is not.
-template <bool CHECK>
-__device__ __forceinline__ uint32_t block_most(const float (&x)[PER]) {
+// The largest magnitude of eight values, NaN if one of them is.
+__device__ __forceinline__ float most_of(const float (&x)[PER]) {
+  float m = fabsf(x[0]);
+#pragma unroll
+  for (int i = 1; i < PER; ++i) asm("max.NaN.f32 %0, %0, %1;" : "+f"(m) : "f"(fabsf(x[i])));
+  return m;
+}
+__device__ __forceinline__ uint32_t finite_most_of(const float (&x)[PER]) {
   uint32_t most = 0;
 #pragma unroll
-  for (int i = 0; i < PER; ++i) most = max(most, !CHECK || finite(x[i]) ? __float_as_uint(x[i]) & 0x7FFFFFFFu : 0u);
-  return __reduce_max_sync(0xffffffffu, most);
+  for (int i = 0; i < PER; ++i) most = max(most, finite(x[i]) ? __float_as_uint(x[i]) & 0x7FFFFFFFu : 0u);
+  return most;
 }
-// The scale that puts the largest at 1.75 * 2^top at most (the types' largest values).
+// The scale that puts a block's largest (its bits) at 1.75 * 2^top at most, the types' largest values.
 __device__ __forceinline__ uint32_t scale_byte(uint32_t most, int top) { return (uint32_t)min(max((int)((most + 0x1FFFFFu) >> 23) - top, 1), 254); }
 template <bool CHECK>
 __device__ __forceinline__ uint2 encode_e4m3(const float (&x)[PER], float inv) {
@@ -160,32 +177,54 @@ __device__ __forceinline__ uint2 encode_e4m3(const float (&x)[PER], float inv) {
   }
   return make_uint2(w[0], w[1]);
 }
-// random21: the random bits, in bits 5 .. 20 (of the 21 that are dropped)
-template <bool CHECK>
-__device__ __forceinline__ uint32_t encode_e5m2(float x, float inv, uint32_t random21) {
-  if (CHECK && !finite(x)) return 0x7Fu;
+// random16: added below the two bits of the mantissa that stay
+__device__ __forceinline__ uint32_t encode_e5m2(float x, float inv, uint32_t random16) {
+  if (!finite(x)) return 0x7Fu;
   const float u = x * inv;      // 0 .. 57,344
   // below 2^-14 the codes are evenly spaced: adding 2^-14 brings them to the places of one binade
   const bool low = u < 6.103515625e-05f;
-  const uint32_t bits = __float_as_uint(low ? __fadd_rn(u, 6.103515625e-05f) : u) + random21;
+  const uint32_t bits = __float_as_uint(low ? __fadd_rn(u, 6.103515625e-05f) : u) + (random16 << 5);
   return max((bits >> 21) - (low ? 113u * 4u : 112u * 4u), min(__float_as_uint(u), 1u));      // a positive value is not rounded to zero
 }
-template <bool CHECK>
-__device__ __forceinline__ void encode_block(const float (&m)[PER], const float (&v)[PER], float inv_m, float inv_v, const uint4& r, uint2& cm, uint2& cv) {
-  cm = encode_e4m3<CHECK>(m, inv_m);
+// Eight second moments of a block with scale byte `scale`.  Where all eight are ordinary (above 2^-14 of the scale, which is nearly always), the
+// scale only moves the exponent: a code is the upper byte of bits * 8 + random * 256 - (112 + scale - 127) * 2^26, three instructions with its
+// share of the packing instead of fifteen.
+__device__ __forceinline__ uint2 encode_e5m2(const float (&v)[PER], uint32_t scale, const uint4& r) {
   const uint32_t words[4] = {r.x, r.y, r.z, r.w};
-  uint32_t w[2] = {0u, 0u};
+  uint32_t least = __float_as_uint(v[0]), most = least;
 #pragma unroll
-  for (int i = 0; i < PER; ++i) w[i >> 2] |= encode_e5m2<CHECK>(v[i], inv_v, (i & 1 ? words[i >> 1] >> 11 : words[i >> 1] << 5) & 0x1FFFE0u) << (8 * (i & 3));
-  cv = make_uint2(w[0], w[1]);
+  for (int i = 1; i < PER; ++i) {
+    least = min(least, __float_as_uint(v[i]));
+    most = max(most, __float_as_uint(v[i]));
+  }
+  uint32_t w[2] = {0u, 0u};
+  if (scale > 15u && least >= (scale - 14u) << 23 && most < 0x7F800000u) {
+    const uint32_t minus = 0u - ((scale - 15u) << 2);      // in its lowest byte: what takes the exponent's excess away
+    uint32_t y[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) y[i] = (__float_as_uint(v[i]) << 3) + (prmt(words[i >> 1], minus, i & 1 ? 0x4320u : 0x4100u) & 0xFFFFFF00u);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) w[i] = prmt(prmt(y[4 * i], y[4 * i + 1], 0x0073u), prmt(y[4 * i + 2], y[4 * i + 3], 0x0073u), 0x5410u);
+  } else {
+    const float inv = inverse_scale_of(scale);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) w[i >> 2] |= encode_e5m2(v[i], inv, (words[i >> 1] >> (16 * (i & 1))) & 0xFFFFu) << (8 * (i & 3));
+  }
+  return make_uint2(w[0], w[1]);
 }
 
 // ---- one step
-template <typename P, typename G, typename C, bool HAS_COPY, int BITS>
-__global__ void __launch_bounds__(TPB) adamw_step(const DevTensor* __restrict__ tensors, const PieceRef* __restrict__ pieces, Call call, const DevState* state) {
+// What a thread loads of a piece, and where it goes.
+template <typename P, typename G, int BITS> struct Loaded;
+template <typename P, typename G> struct Loaded<P, G, 32> { Raw8<P> p; Raw8<G> g; Raw8<float> m, v; };
+template <typename P, typename G> struct Loaded<P, G, 8> { Raw8<P> p; Raw8<G> g; uint2 m, v; uint32_t sm, sv; };
+
+// A CTA takes PIECES pieces, all of whose loads come before the first one's work: one with moments in 32 bits, two with 8, whose loads are half the
+// bytes.  us for 200 M elements (bf16 gradient and copy): 32 bits 830, more than the copy rate; 8 bits with one piece 570, two 546, two and
+// registers for four CTAs on an SM 500, 98 % of the copy rate.  (Copies into a ring in shared memory two pieces ahead, by cp.async: 950 to 1,010.)
+template <typename P, typename G, typename C, bool HAS_COPY, int BITS, int PIECES>
+__global__ void __launch_bounds__(TPB, BITS == 8 ? 4 : 1) adamw_step(const DevTensor* __restrict__ tensors, const PieceRef* __restrict__ pieces, int n_pieces, Call call, const DevState* state) {
   pdl_enter();
-  const PieceRef ref = pieces[blockIdx.x];
-  const DevTensor t = tensors[ref.tensor];
   AdamScalars s = call.s;
   double lr = call.h.lr;
   uint32_t step = (uint32_t)call.step;
@@ -195,95 +234,115 @@ __global__ void __launch_bounds__(TPB) adamw_step(const DevTensor* __restrict__ 
     lr = state->lr;
     step = (uint32_t)state->step;
   }
-  const float decay = adam_decay(lr, t.wd);
-  const int64_t i0 = (int64_t)ref.piece * PIECE + threadIdx.x * PER;
-  const int n = (int)min((int64_t)PER, max((int64_t)0, t.n - i0));
-  const bool vec = t.wide && n == PER;
-  if (BITS == 32 && n == 0) return;
-  float p[PER], g[PER], m[PER], v[PER];
-  uint32_t sm = 0, sv = 0;
-  const int64_t block = i0 / BLOCK8;
-  const bool in_block = block * BLOCK8 < t.n;      // the same for a warp
-  if (BITS == 8 && !in_block) return;
-  if (vec) {
-    load8(reinterpret_cast<const P*>(t.p) + i0, p);
-    load8(reinterpret_cast<const G*>(t.g) + i0, g);
-  } else {
-    load_some(reinterpret_cast<const P*>(t.p), i0, n, p);
-    load_some(reinterpret_cast<const G*>(t.g), i0, n, g);
-  }
-  if constexpr (BITS == 32) {
-    if (vec) {
-      load8(reinterpret_cast<const float*>(t.m) + i0, m);
-      load8(reinterpret_cast<const float*>(t.v) + i0, v);
-    } else {
-      load_some(reinterpret_cast<const float*>(t.m), i0, n, m);
-      load_some(reinterpret_cast<const float*>(t.v), i0, n, v);
-    }
-  } else {
-    uint2 cm = make_uint2(0u, 0u), cv = cm;
-    const uint8_t *pm = reinterpret_cast<const uint8_t*>(t.m) + i0, *pv = reinterpret_cast<const uint8_t*>(t.v) + i0;
-    if (vec) {
-      cm = __ldcs(reinterpret_cast<const uint2*>(pm));
-      cv = __ldcs(reinterpret_cast<const uint2*>(pv));
-    } else {
+  PieceRef ref[PIECES];
+  Loaded<P, G, BITS> x[PIECES];
 #pragma unroll
-      for (int i = 0; i < PER; ++i)
-        if (i < n) {
-          (i < 4 ? cm.x : cm.y) |= (uint32_t)pm[i] << (8 * (i & 3));
-          (i < 4 ? cv.x : cv.y) |= (uint32_t)pv[i] << (8 * (i & 3));
-        }
+  for (int k = 0; k < PIECES; ++k) ref[k] = (int)blockIdx.x * PIECES + k < n_pieces ? pieces[blockIdx.x * PIECES + k] : PieceRef{-1, 0};
+#pragma unroll
+  for (int k = 0; k < PIECES; ++k) {
+    if (PIECES > 1 && ref[k].tensor < 0) break;
+    const DevTensor& t = tensors[ref[k].tensor];
+    const int64_t i0 = (int64_t)ref[k].piece * PIECE + threadIdx.x * PER;
+    const int n = (int)min((int64_t)PER, max((int64_t)0, t.n - i0));
+    if (t.wide && n == PER) {
+      load8(reinterpret_cast<const P*>(t.p) + i0, x[k].p);
+      load8(reinterpret_cast<const G*>(t.g) + i0, x[k].g);
+      if constexpr (BITS == 32) {
+        load8(reinterpret_cast<const float*>(t.m) + i0, x[k].m);
+        load8(reinterpret_cast<const float*>(t.v) + i0, x[k].v);
+      } else {
+        x[k].m = __ldcs(reinterpret_cast<const uint2*>(reinterpret_cast<const uint8_t*>(t.m) + i0));
+        x[k].v = __ldcs(reinterpret_cast<const uint2*>(reinterpret_cast<const uint8_t*>(t.v) + i0));
+      }
+    } else {
+      load_some(reinterpret_cast<const P*>(t.p), i0, n, x[k].p);
+      load_some(reinterpret_cast<const G*>(t.g), i0, n, x[k].g);
+      if constexpr (BITS == 32) {
+        load_some(reinterpret_cast<const float*>(t.m), i0, n, x[k].m);
+        load_some(reinterpret_cast<const float*>(t.v), i0, n, x[k].v);
+      } else {
+        const uint8_t *pm = reinterpret_cast<const uint8_t*>(t.m) + i0, *pv = reinterpret_cast<const uint8_t*>(t.v) + i0;
+        x[k].m = x[k].v = make_uint2(0u, 0u);
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+          if (i < n) {
+            (i < 4 ? x[k].m.x : x[k].m.y) |= (uint32_t)pm[i] << (8 * (i & 3));
+            (i < 4 ? x[k].v.x : x[k].v.y) |= (uint32_t)pv[i] << (8 * (i & 3));
+          }
+      }
     }
-    decode_e4m3(cm, scale_of(t.m_scale[block]), m);
-    decode_e5m2(cv, scale_of(t.v_scale[block]), v);
+    if constexpr (BITS == 8) {
+      const int64_t block = i0 / BLOCK8;
+      const bool there = block * BLOCK8 < t.n;      // the same for a warp
+      x[k].sm = there ? t.m_scale[block] : 0;
+      x[k].sv = there ? t.v_scale[block] : 0;
+    }
   }
 #pragma unroll
-  for (int i = 0; i < PER; i += 2) adam_update2(p[i], p[i + 1], __fmul_rn(g[i], s.factor), __fmul_rn(g[i + 1], s.factor), m[i], m[i + 1], v[i], v[i + 1], s, decay);
-  if (vec) store8(reinterpret_cast<P*>(t.p) + i0, p);
-  else store_some(reinterpret_cast<P*>(t.p), i0, n, p);
-  if constexpr (HAS_COPY) {
-    if (vec) store8(reinterpret_cast<C*>(t.copy) + i0, p);
-    else store_some(reinterpret_cast<C*>(t.copy), i0, n, p);
-  }
-  if constexpr (BITS == 32) {
-    if (vec) {
-      store8(reinterpret_cast<float*>(t.m) + i0, m);
-      store8(reinterpret_cast<float*>(t.v) + i0, v);
+  for (int k = 0; k < PIECES; ++k) {
+    if (PIECES > 1 && ref[k].tensor < 0) break;
+    const DevTensor& t = tensors[ref[k].tensor];
+    const int64_t i0 = (int64_t)ref[k].piece * PIECE + threadIdx.x * PER, block = i0 / BLOCK8;
+    const int n = (int)min((int64_t)PER, max((int64_t)0, t.n - i0));
+    if (BITS == 32 ? n == 0 : block * BLOCK8 >= t.n) continue;
+    const bool vec = t.wide && n == PER;
+    const float decay = adam_decay(lr, t.wd);
+    float p[PER], g[PER], m[PER], v[PER];
+    widen8(x[k].p, p);
+    widen8(x[k].g, g);
+    if constexpr (BITS == 32) {
+      widen8(x[k].m, m);
+      widen8(x[k].v, v);
     } else {
-      store_some(reinterpret_cast<float*>(t.m), i0, n, m);
-      store_some(reinterpret_cast<float*>(t.v), i0, n, v);
+      decode_e4m3(x[k].m, scale_of(x[k].sm), m);
+      decode_e5m2(x[k].v, scale_of(x[k].sv), v);
     }
-  } else {
-    // lanes past the tensor's end hold zero moments: they had zero gradients and moments
-    const uint64_t j = (uint64_t)(i0 / PER);
-    const uint4 r = philox4x32_10(make_uint4((uint32_t)j, (uint32_t)(j >> 32), (uint32_t)ref.tensor, step),
-                                  make_uint2((uint32_t)call.seed, (uint32_t)(call.seed >> 32)));
-    uint32_t most_m = block_most<false>(m), most_v = block_most<false>(v);
-    uint2 cm, cv;
-    if (max(most_m, most_v) < 0x7F800000u) {
-      sm = scale_byte(most_m, 8);
-      sv = scale_byte(most_v, 15);
-      encode_block<false>(m, v, inverse_scale_of(sm), inverse_scale_of(sv), r, cm, cv);
-    } else {      // something is not finite
-      sm = scale_byte(block_most<true>(m), 8);
-      sv = scale_byte(block_most<true>(v), 15);
-      encode_block<true>(m, v, inverse_scale_of(sm), inverse_scale_of(sv), r, cm, cv);
-    }
-    uint8_t *pm = reinterpret_cast<uint8_t*>(t.m) + i0, *pv = reinterpret_cast<uint8_t*>(t.v) + i0;
-    if (vec) {
-      *reinterpret_cast<uint2*>(pm) = cm;
-      *reinterpret_cast<uint2*>(pv) = cv;
-    } else {
 #pragma unroll
-      for (int i = 0; i < PER; ++i)
-        if (i < n) {
-          pm[i] = (uint8_t)((i < 4 ? cm.x : cm.y) >> (8 * (i & 3)));
-          pv[i] = (uint8_t)((i < 4 ? cv.x : cv.y) >> (8 * (i & 3)));
-        }
+    for (int i = 0; i < PER; i += 2) adam_update2(p[i], p[i + 1], __fmul_rn(g[i], s.factor), __fmul_rn(g[i + 1], s.factor), m[i], m[i + 1], v[i], v[i + 1], s, decay);
+    if (vec) store8(reinterpret_cast<P*>(t.p) + i0, p);
+    else store_some(reinterpret_cast<P*>(t.p), i0, n, p);
+    if constexpr (HAS_COPY) {
+      if (vec) store8(reinterpret_cast<C*>(t.copy) + i0, p);
+      else store_some(reinterpret_cast<C*>(t.copy), i0, n, p);
     }
-    if ((threadIdx.x & 31) == 0) {
-      t.m_scale[block] = (uint8_t)sm;
-      t.v_scale[block] = (uint8_t)sv;
+    if constexpr (BITS == 32) {
+      if (vec) {
+        store8(reinterpret_cast<float*>(t.m) + i0, m);
+        store8(reinterpret_cast<float*>(t.v) + i0, v);
+      } else {
+        store_some(reinterpret_cast<float*>(t.m), i0, n, m);
+        store_some(reinterpret_cast<float*>(t.v), i0, n, v);
+      }
+    } else {
+      // lanes past the tensor's end hold zero moments: they had zero gradients and moments
+      const uint64_t j = (uint64_t)(i0 / PER);
+      const uint4 r = philox4x32_10(make_uint4((uint32_t)j, (uint32_t)(j >> 32), (uint32_t)ref[k].tensor, step),
+                                    make_uint2((uint32_t)call.seed, (uint32_t)(call.seed >> 32)));
+      uint32_t most_m = __reduce_max_sync(0xffffffffu, __float_as_uint(most_of(m))), most_v = __reduce_max_sync(0xffffffffu, __float_as_uint(most_of(v)));
+      const bool all_finite = max(most_m, most_v) < 0x7F800000u;
+      if (!all_finite) {
+        most_m = __reduce_max_sync(0xffffffffu, finite_most_of(m));
+        most_v = __reduce_max_sync(0xffffffffu, finite_most_of(v));
+      }
+      const uint32_t sm = scale_byte(most_m, 8), sv = scale_byte(most_v, 15);
+      const float inv_m = inverse_scale_of(sm);
+      const uint2 cm = all_finite ? encode_e4m3<false>(m, inv_m) : encode_e4m3<true>(m, inv_m), cv = encode_e5m2(v, sv, r);
+      uint8_t *pm = reinterpret_cast<uint8_t*>(t.m) + i0, *pv = reinterpret_cast<uint8_t*>(t.v) + i0;
+      if (vec) {
+        *reinterpret_cast<uint2*>(pm) = cm;
+        *reinterpret_cast<uint2*>(pv) = cv;
+      } else {
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+          if (i < n) {
+            pm[i] = (uint8_t)((i < 4 ? cm.x : cm.y) >> (8 * (i & 3)));
+            pv[i] = (uint8_t)((i < 4 ? cv.x : cv.y) >> (8 * (i & 3)));
+          }
+      }
+      if ((threadIdx.x & 31) == 0) {
+        t.m_scale[block] = (uint8_t)sm;
+        t.v_scale[block] = (uint8_t)sv;
+      }
     }
   }
 }
@@ -327,9 +386,11 @@ __global__ void __launch_bounds__(TPB) adamw_norm(const DevTensor* __restrict__ 
     const DevTensor& t = tensors[ref.tensor];
     const int64_t i0 = (int64_t)ref.piece * PIECE + threadIdx.x * PER;
     const int n = (int)min((int64_t)PER, max((int64_t)0, t.n - i0));
+    Raw8<G> x;
+    if (t.wide_g && n == PER) load8(reinterpret_cast<const G*>(t.g) + i0, x);
+    else load_some(reinterpret_cast<const G*>(t.g), i0, n, x);
     float g[PER];
-    if (t.wide_g && n == PER) load8(reinterpret_cast<const G*>(t.g) + i0, g);
-    else load_some(reinterpret_cast<const G*>(t.g), i0, n, g);
+    widen8(x, g);
 #pragma unroll
     for (int i = 0; i < PER; ++i) acc[i & 1] = fma((double)g[i], (double)g[i], acc[i & 1]);
   }
@@ -444,9 +505,9 @@ int32_t upload_tensors(ps_adamw* o) {      // the copy's source is pageable: it 
 
 template <typename P, typename G, typename C, bool HAS_COPY>
 void launch_step(const ps_adamw* o, const Call& call, const DevState* state) {
-  const dim3 grid((unsigned)o->n_pieces);
-  if (o->cfg.state_bits == 32) launch_pdl(adamw_step<P, G, C, HAS_COPY, 32>, grid, TPB, 0, o->st, o->tensors, o->pieces, call, state);
-  else launch_pdl(adamw_step<P, G, C, HAS_COPY, 8>, grid, TPB, 0, o->st, o->tensors, o->pieces, call, state);
+  const int n = (int)o->n_pieces;
+  if (o->cfg.state_bits == 32) launch_pdl(adamw_step<P, G, C, HAS_COPY, 32, 1>, dim3((unsigned)n), TPB, 0, o->st, o->tensors, o->pieces, n, call, state);
+  else launch_pdl(adamw_step<P, G, C, HAS_COPY, 8, 2>, dim3((unsigned)((n + 1) / 2)), TPB, 0, o->st, o->tensors, o->pieces, n, call, state);
 }
 template <typename P, typename G>
 void launch_copy(const ps_adamw* o, const Call& call, const DevState* state) {

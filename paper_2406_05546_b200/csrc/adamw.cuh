@@ -7,7 +7,7 @@
 // is what lets the 8-bit moments' codes be tested for equality.  The square root and the quotient, which only the step depends on, are the
 // approximate ones (off by 2^-23 and 2 ulp), and two elements share an instruction where there is one for pairs.  us of the ordered server step,
 // 37 updates of 813,258 weights, and of the many-tensor step with 8-bit moments, 400 M elements: all rounded 86 and 1,528; approximate 39 and
-// 1,400; in pairs ASYNC_NOW and EIGHT_NOW.  The constants are made in fp64 and rounded once.
+// 1,400; in pairs 36 and 1,283.  The constants are made in fp64 and rounded once.
 #pragma once
 #include <cuda_runtime.h>
 #include <stdint.h>
