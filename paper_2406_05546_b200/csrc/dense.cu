@@ -28,6 +28,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <initializer_list>
 #include <mutex>
 #include <type_traits>
 
@@ -84,7 +85,7 @@ struct DenseEpi {
   void *out0, *out1;
   int64_t in0_stride, in1_pitch, in2_pitch, out0_pitch, out0_stride, out1_pitch;
   int32_t act, bf16, out0_fp32, accumulate;
-  int32_t v_in0, v_in1, v_in2, v_out0, v_out1, v_all;      // may four values be moved at once? (v_all: in everything there is)
+  int32_t quads, rows, wide;      // may four values be moved at once, 16 bytes, 32 bytes, in every matrix there is?
 };
 
 struct DenseArgs {
@@ -110,78 +111,79 @@ __device__ __forceinline__ uint32_t narrow2(float lo, float hi, int bf16) {
   const __half2 h = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&h);
 }
-// Four consecutive 16-bit values from element i on, of which n exist, as they lie; and as floats.
-// FULL: all four do, and may be moved at once.
-template <bool FULL = false>
-__device__ __forceinline__ uint2 raw4(const void* base, int64_t i, int n, int vec) {
-  const uint16_t* p = reinterpret_cast<const uint16_t*>(base) + i;
-  if (FULL || (vec && n >= 4)) return *reinterpret_cast<const uint2*>(p);
-  uint2 w = make_uint2(p[0], 0u);
-  if (n > 1) w.x |= (uint32_t)p[1] << 16;
-  if (n > 2) w.y = p[2];
-  if (n > 3) w.y |= (uint32_t)p[3] << 16;
-  return w;
+// ---- elementwise, two values at a time ---------------------------------------------------------------------------------------
+__device__ __forceinline__ u64 mul2(u64 a, u64 b) {
+  u64 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
 }
-__device__ __forceinline__ float4 widen4(const uint2& w, int bf16) {
-  return make_float4(widen(w.x & 0xFFFFu, bf16), widen(w.x >> 16, bf16), widen(w.y & 0xFFFFu, bf16), widen(w.y >> 16, bf16));
+__device__ __forceinline__ u64 add2(u64 a, u64 b) {
+  u64 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
 }
-template <bool FULL>
-__device__ __forceinline__ void store4(void* base, int64_t i, int n, int vec, int bf16, const float4& v) {
-  uint16_t* p = reinterpret_cast<uint16_t*>(base) + i;
-  const uint32_t a = narrow2(v.x, v.y, bf16), b = narrow2(v.z, v.w, bf16);
-  if (FULL || (vec && n >= 4)) {
-    *reinterpret_cast<uint2*>(p) = make_uint2(a, b);
-    return;
-  }
-  p[0] = (uint16_t)a;
-  if (n > 1) p[1] = (uint16_t)(a >> 16);
-  if (n > 2) p[2] = (uint16_t)b;
-  if (n > 3) p[3] = (uint16_t)(b >> 16);
+__device__ __forceinline__ u64 both(float v) { return pack2(v, v); }
+__device__ __forceinline__ float exp2_fast(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
 }
-template <bool FULL>
-__device__ __forceinline__ float4 load4_f32(const float* p, int n, int vec) {
-  if (FULL || (vec && n >= 4)) return *reinterpret_cast<const float4*>(p);
-  return make_float4(p[0], n > 1 ? p[1] : 0.f, n > 2 ? p[2] : 0.f, n > 3 ? p[3] : 0.f);
+__device__ __forceinline__ float reciprocal_fast(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
 }
-template <bool FULL>
-__device__ __forceinline__ void store4_f32(float* p, int n, int vec, const float4& v) {
-  if (FULL || (vec && n >= 4)) { *reinterpret_cast<float4*>(p) = v; return; }
-  p[0] = v.x;
-  if (n > 1) p[1] = v.y;
-  if (n > 2) p[2] = v.z;
-  if (n > 3) p[3] = v.w;
+// The normal distribution function of two values, and e = exp(-z^2 / 2): Abramowitz and Stegun 7.1.26 (a polynomial in 1 / (1 + p x) times e, erf
+// within 1.5e-7), which shares the exponential with the density.  NaN stays.
+__device__ __forceinline__ u64 normal_cdf2(u64 z, u64& e) {
+  float z0, z1, a0, a1;
+  unpack2(z, z0, z1);
+  const u64 t = pack2(reciprocal_fast(fmaf(0.3275911f * 0.70710678f, fabsf(z0), 1.f)), reciprocal_fast(fmaf(0.3275911f * 0.70710678f, fabsf(z1), 1.f)));
+  unpack2(mul2(mul2(z, z), both(-0.72134752f)), a0, a1);      // -log2(e) / 2
+  e = pack2(exp2_fast(a0), exp2_fast(a1));
+  u64 q = ffma2(t, both(0.5307027145f), both(-0.7265760135f));      // the published coefficients, halved
+  q = ffma2(t, q, both(0.7107068705f));
+  q = ffma2(t, q, both(-0.142248368f));
+  q = ffma2(t, q, both(0.127414796f));
+  unpack2(ffma2(mul2(mul2(q, t), e), both(-1.f), both(0.5f)), a0, a1);      // 1/2 minus the tail
+  return add2(pack2(copysignf(a0, z0), copysignf(a1, z1)), both(0.5f));
 }
-__device__ __forceinline__ float4 add(const float4& a, const float4& b) { return make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w); }
-
-// The normal distribution function, and e = exp(-z^2 / 2): Abramowitz and Stegun 7.1.26 (a polynomial in 1 / (1 + p x) times e; erf within
-// 1.5e-7), which shares the exponential with the density.
-__device__ __forceinline__ float normal_cdf(float z, float& e) {
-  const float t = __fdividef(1.f, fmaf(0.3275911f * 0.70710678f, fabsf(z), 1.f));
-  e = __expf(-0.5f * z * z);
-  const float tail = 0.5f * e * t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
-  return z > 0.f ? 1.f - tail : tail;      // NaN: tail is
+__device__ __forceinline__ u64 logistic2(u64 z) {
+  float a0, a1;
+  unpack2(mul2(z, both(-1.44269504f)), a0, a1);
+  unpack2(add2(pack2(exp2_fast(a0), exp2_fast(a1)), both(1.f)), a0, a1);
+  return pack2(reciprocal_fast(a0), reciprocal_fast(a1));
 }
 template <int ACT>
-__device__ __forceinline__ float activate(float z) {
-  if (ACT == PS_ACT_RELU) return z < 0.f ? 0.f : z;                 // NaN stays
-  if (ACT == PS_ACT_GELU) { float e; return z * normal_cdf(z, e); }
-  if (ACT == PS_ACT_SILU) return __fdividef(z, 1.f + __expf(-z));
-  return z;
+__device__ __forceinline__ u64 activate2(u64 z) {
+  if (ACT == PS_ACT_RELU) {      // NaN stays
+    float z0, z1;
+    unpack2(z, z0, z1);
+    return pack2(z0 < 0.f ? 0.f : z0, z1 < 0.f ? 0.f : z1);
+  }
+  if (ACT == PS_ACT_GELU) {
+    u64 e;
+    const u64 c = normal_cdf2(z, e);
+    return mul2(z, c);
+  }
+  return mul2(z, logistic2(z));      // SiLU
 }
 // d * act'(z)
 template <int ACT>
-__device__ __forceinline__ float through(float d, float z) {
-  if (ACT == PS_ACT_RELU) return z > 0.f ? d : 0.f;
+__device__ __forceinline__ u64 through2(u64 d, u64 z) {
+  if (ACT == PS_ACT_RELU) {
+    float z0, z1, d0, d1;
+    unpack2(z, z0, z1);
+    unpack2(d, d0, d1);
+    return pack2(z0 > 0.f ? d0 : 0.f, z1 > 0.f ? d1 : 0.f);
+  }
   if (ACT == PS_ACT_GELU) {
-    float e;
-    const float c = normal_cdf(z, e);
-    return d * fmaf(z * 0.39894228f, e, c);
+    u64 e;
+    const u64 c = normal_cdf2(z, e);
+    return mul2(d, ffma2(mul2(z, both(0.39894228f)), e, c));
   }
-  if (ACT == PS_ACT_SILU) {
-    const float e = __fdividef(1.f, 1.f + __expf(-z));
-    return d * (e * fmaf(z, 1.f - e, 1.f));
-  }
-  return d;
+  const u64 q = logistic2(z);
+  return mul2(mul2(d, q), ffma2(z, ffma2(q, both(-1.f), both(1.f)), both(1.f)));
 }
 // f(activation as a constant)
 template <typename F> __device__ __forceinline__ void with_activation(int act, F f) {
@@ -190,85 +192,255 @@ template <typename F> __device__ __forceinline__ void with_activation(int act, F
   else if (act == PS_ACT_SILU) f(std::integral_constant<int, PS_ACT_SILU>());
 }
 
-// What the elementwise part reads for four consecutive columns of a row.  Loaded well before it is used: in a tile's read-out nothing else hides
-// the loads (with loads where they were used, the input gradient of 16,384 x 4096 x 4096 with everything on took 787 us, alone 345).
-template <int OP> struct EpiIn { uint2 a, b; };
-template <> struct EpiIn<D_DW> { float4 a; };
-template <int OP, bool FULL>
-__device__ __forceinline__ EpiIn<OP> load_in(const DenseEpi& e, int64_t row, int col, int n, int which) {
-  EpiIn<OP> x;
-  if constexpr (OP == D_DW) {
-    x.a = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (e.accumulate) {
-      const int64_t at = (int64_t)which * e.out0_stride + row * e.out0_pitch + col;
-      x.a = e.out0_fp32 ? load4_f32<FULL>(reinterpret_cast<const float*>(e.out0) + at, n, e.v_out0) : widen4(raw4<FULL>(e.out0, at, n, e.v_out0), e.bf16);
-    }
-  } else {
-    x.a = x.b = make_uint2(0u, 0u);
-    if (e.in1) x.a = raw4<FULL>(e.in1, row * e.in1_pitch + col, n, e.v_in1);
-    if (OP == D_DX && e.out1) x.b = raw4<FULL>(e.in2, row * e.in2_pitch + col, n, e.v_in2);
-  }
-  return x;
+__device__ __forceinline__ u64 widen2(uint32_t w, int bf16) {
+  if (bf16) return pack2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+  const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
+  return pack2(f.x, f.y);
+}
+__device__ __forceinline__ uint32_t narrow_pair(u64 v, int bf16) {
+  float a, b;
+  unpack2(v, a, b);
+  return narrow2(a, b, bf16);
 }
 
-// Everything elementwise for four consecutive columns of R rows, row0 + i * step, of which those below `end` exist.  which: the weight matrix
-// (forward) or the worker (weight gradient); bias: in0's four values.  FULL: nothing is cut off and everything may be moved four values at
-// once.  One kind of work for all rows, then the next: with the rows one after the other, and every choice made for each of them, a tile's read-out was
-// a chain of latencies twice as long as its products (24 workers' rows of 2048 -> 5000 with everything on 317 us -> RAGGED_NOW).
-template <int OP, int R, bool FULL>
-__device__ __forceinline__ void finish_rows(const DenseEpi& e, int64_t row0, int step, int64_t end, int col, int n, int which, const float4& bias, const EpiIn<OP> (&in)[R],
-                                            float4 (&v)[R]) {
+// 32 or 16 bytes of a lane in one access.
+__device__ __forceinline__ void load_words(const void* p, uint32_t (&w)[8]) {
+  asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p));
+}
+__device__ __forceinline__ void store_words(void* p, const uint32_t* w) {
+  asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+               ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+}
+
+// ---- the elementwise part of a tile ------------------------------------------------------------------------------------------
+// which: the weight matrix (forward) or the worker (weight gradient).
+template <int OP> __device__ __forceinline__ int64_t out0_at(const DenseEpi& e, int64_t row, int col, int which) {
+  return (OP == D_DW ? (int64_t)which * e.out0_stride : 0) + row * e.out0_pitch + col;
+}
+
+// Rows: a lane has 32 consecutive columns of a row of its own, whose pieces of 32 or 16 bytes it loads and stores straight from and to global memory:
+// no exchange between lanes.  What is read is loaded a chunk ahead.
+template <int OP> struct RowIn { uint32_t a[OP == D_DW ? 1 : 16], b[OP == D_DX ? 16 : 1]; };
+__device__ __forceinline__ void load_row(const void* base, int64_t at, int wide, uint32_t (&w)[16]) {      // 32 values of 16 bits
+  const uint16_t* p = reinterpret_cast<const uint16_t*>(base) + at;
+  if (wide) {
+    load_words(p, *reinterpret_cast<uint32_t (*)[8]>(&w[0]));
+    load_words(p + 16, *reinterpret_cast<uint32_t (*)[8]>(&w[8]));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint4 v = reinterpret_cast<const uint4*>(p)[i];
+      w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+    }
+  }
+}
+template <int WORDS>
+__device__ __forceinline__ void store_row(void* p, int wide, const uint32_t (&w)[WORDS]) {
+  if (wide) {
+#pragma unroll
+    for (int i = 0; i < WORDS / 8; ++i) store_words(reinterpret_cast<uint8_t*>(p) + 32 * i, w + 8 * i);
+  } else {
+#pragma unroll
+    for (int i = 0; i < WORDS / 4; ++i) reinterpret_cast<uint4*>(p)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+  }
+}
+__device__ __forceinline__ void store_row16(void* base, int64_t at, int wide, int bf16, const u64 (&v)[16]) {
+  uint32_t w[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) w[i] = narrow_pair(v[i], bf16);
+  store_row(reinterpret_cast<uint16_t*>(base) + at, wide, w);
+}
+__device__ __forceinline__ void store_row32(void* base, int64_t at, int wide, const u64 (&v)[16]) {
+  uint32_t w[32];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    w[2 * i] = (uint32_t)v[i];
+    w[2 * i + 1] = (uint32_t)(v[i] >> 32);
+  }
+  store_row(reinterpret_cast<float*>(base) + at, wide, w);
+}
+template <int OP>
+__device__ __forceinline__ void row_ahead(const DenseEpi& e, int64_t row, int col, RowIn<OP>& x) {
+  if constexpr (OP != D_DW) {
+    if (e.in1) load_row(e.in1, row * e.in1_pitch + col, e.wide, x.a);
+    if constexpr (OP == D_DX)
+      if (e.out1) load_row(e.in2, row * e.in2_pitch + col, e.wide, x.b);
+  }
+}
+// bias: 32 floats in shared memory
+template <int OP>
+__device__ __forceinline__ void finish_row(const DenseEpi& e, int64_t row, int col, int which, const float* bias, const RowIn<OP>& x, u64 (&v)[16]) {
+  if constexpr (OP == D_FWD) {
+    if (e.in0) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float4 b = reinterpret_cast<const float4*>(bias)[i];
+        v[2 * i] = add2(v[2 * i], pack2(b.x, b.y));
+        v[2 * i + 1] = add2(v[2 * i + 1], pack2(b.z, b.w));
+      }
+    }
+    if (e.out1) store_row16(e.out1, row * e.out1_pitch + col, e.wide, e.bf16, v);
+    with_activation(e.act, [&](auto act) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) v[i] = activate2<decltype(act)::value>(v[i]);
+    });
+  }
+  if constexpr (OP != D_DW) {
+    if (e.in1) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) v[i] = add2(v[i], widen2(x.a[i], e.bf16));
+    }
+  }
+  if constexpr (OP == D_FWD) {
+    if (e.out0_fp32) store_row32(e.out0, row * e.out0_pitch + col, e.wide, v);
+    else store_row16(e.out0, row * e.out0_pitch + col, e.wide, e.bf16, v);
+  } else if constexpr (OP == D_DX) {
+    if (e.out0) store_row16(e.out0, row * e.out0_pitch + col, e.wide, e.bf16, v);
+    if (e.out1) {
+      with_activation(e.act, [&](auto act) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = through2<decltype(act)::value>(v[i], widen2(x.b[i], e.bf16));
+      });
+      store_row16(e.out1, row * e.out1_pitch + col, e.wide, e.bf16, v);
+    }
+  } else {
+    const int64_t at = out0_at<OP>(e, row, col, which);
+    if (e.out0_fp32) {
+      if (e.accumulate) {
+        const float4* p = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(e.out0) + at);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float4 o = p[i];
+          v[2 * i] = add2(v[2 * i], pack2(o.x, o.y));
+          v[2 * i + 1] = add2(v[2 * i + 1], pack2(o.z, o.w));
+        }
+      }
+      store_row32(e.out0, at, e.wide, v);
+    } else {
+      if (e.accumulate) {
+        uint32_t o[16];
+        load_row(e.out0, at, e.wide, o);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = add2(v[i], widen2(o[i], e.bf16));
+      }
+      store_row16(e.out0, at, e.wide, e.bf16, v);
+    }
+  }
+}
+
+// Columns: a lane has W (1 or 4) consecutive columns of R rows, row0 + i * step, of which those below `end` exist.  W = 1 for matrices of any
+// alignment and at their right edge.
+template <int W> __device__ __forceinline__ void load_few(const void* base, int64_t i, int bf16, float (&v)[W]) {
+  const uint16_t* p = reinterpret_cast<const uint16_t*>(base) + i;
+  if constexpr (W == 1) {
+    v[0] = widen(*p, bf16);
+  } else {
+    const uint2 w = *reinterpret_cast<const uint2*>(p);
+    unpack2(widen2(w.x, bf16), v[0], v[1]);
+    unpack2(widen2(w.y, bf16), v[2], v[3]);
+  }
+}
+template <int W> __device__ __forceinline__ void store_few(void* base, int64_t i, int bf16, const float (&v)[W]) {
+  uint16_t* p = reinterpret_cast<uint16_t*>(base) + i;
+  if constexpr (W == 1) *p = (uint16_t)narrow2(v[0], 0.f, bf16);
+  else *reinterpret_cast<uint2*>(p) = make_uint2(narrow2(v[0], v[1], bf16), narrow2(v[2], v[3], bf16));
+}
+template <int W> __device__ __forceinline__ void load_few_f32(const void* base, int64_t i, float (&v)[W]) {
+  const float* p = reinterpret_cast<const float*>(base) + i;
+  if constexpr (W == 1) {
+    v[0] = *p;
+  } else {
+    const float4 w = *reinterpret_cast<const float4*>(p);
+    v[0] = w.x; v[1] = w.y; v[2] = w.z; v[3] = w.w;
+  }
+}
+template <int W> __device__ __forceinline__ void store_few_f32(void* base, int64_t i, const float (&v)[W]) {
+  float* p = reinterpret_cast<float*>(base) + i;
+  if constexpr (W == 1) *p = v[0];
+  else *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+}
+template <int W, typename F> __device__ __forceinline__ void map_pairs(float (&v)[W], F f) {      // f(pair, index of its first)
+  if constexpr (W == 1) {
+    float unused;
+    unpack2(f(pack2(v[0], v[0]), 0), v[0], unused);
+  } else {
+    unpack2(f(pack2(v[0], v[1]), 0), v[0], v[1]);
+    unpack2(f(pack2(v[2], v[3]), 2), v[2], v[3]);
+  }
+}
+template <int OP, int R, int W> struct ColumnIn { float a[R][W], b[OP == D_DX ? R : 1][W]; };
+template <int OP, int R, int W>
+__device__ __forceinline__ void columns_ahead(const DenseEpi& e, int64_t row0, int step, int64_t end, int col, int which, ColumnIn<OP, R, W>& x) {
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    const int64_t r = row0 + i * step;
+    if (r >= end) continue;
+    if constexpr (OP == D_DW) {
+      if (e.accumulate) {
+        if (e.out0_fp32) load_few_f32<W>(e.out0, out0_at<OP>(e, r, col, which), x.a[i]);
+        else load_few<W>(e.out0, out0_at<OP>(e, r, col, which), e.bf16, x.a[i]);
+      }
+    } else {
+      if (e.in1) load_few<W>(e.in1, r * e.in1_pitch + col, e.bf16, x.a[i]);
+      if constexpr (OP == D_DX)
+        if (e.out1) load_few<W>(e.in2, r * e.in2_pitch + col, e.bf16, x.b[i]);
+    }
+  }
+}
+// One kind of work for all rows, then the next.
+template <int OP, int R, int W>
+__device__ __forceinline__ void finish_columns(const DenseEpi& e, int64_t row0, int step, int64_t end, int col, int which, const float (&bias)[W], const ColumnIn<OP, R, W>& x,
+                                               float (&v)[R][W]) {
   auto each = [&](auto f) {
 #pragma unroll
     for (int i = 0; i < R; ++i)
-      if (FULL || row0 + i * step < end) f(i, row0 + i * step);
+      if (row0 + i * step < end) f(i, row0 + i * step);
+  };
+  auto add_in = [&]() {
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+#pragma unroll
+      for (int j = 0; j < W; ++j) v[i][j] += x.a[i][j];
   };
   if constexpr (OP == D_FWD) {
 #pragma unroll
-    for (int i = 0; i < R; ++i) v[i] = add(v[i], bias);
-    if (e.out1) each([&](int i, int64_t r) { store4<FULL>(e.out1, r * e.out1_pitch + col, n, e.v_out1, e.bf16, v[i]); });
+    for (int i = 0; i < R; ++i)
+#pragma unroll
+      for (int j = 0; j < W; ++j) v[i][j] += bias[j];
+    if (e.out1) each([&](int i, int64_t r) { store_few<W>(e.out1, r * e.out1_pitch + col, e.bf16, v[i]); });
     with_activation(e.act, [&](auto act) {
-      constexpr int A = decltype(act)::value;
 #pragma unroll
-      for (int i = 0; i < R; ++i) v[i] = make_float4(activate<A>(v[i].x), activate<A>(v[i].y), activate<A>(v[i].z), activate<A>(v[i].w));
+      for (int i = 0; i < R; ++i) map_pairs<W>(v[i], [&](u64 z, int) { return activate2<decltype(act)::value>(z); });
     });
-    if (e.in1) {
-#pragma unroll
-      for (int i = 0; i < R; ++i) v[i] = add(v[i], widen4(in[i].a, e.bf16));
-    }
-    if (e.out0_fp32) each([&](int i, int64_t r) { store4_f32<FULL>(reinterpret_cast<float*>(e.out0) + r * e.out0_pitch + col, n, e.v_out0, v[i]); });
-    else each([&](int i, int64_t r) { store4<FULL>(e.out0, r * e.out0_pitch + col, n, e.v_out0, e.bf16, v[i]); });
+    if (e.in1) add_in();
+    if (e.out0_fp32) each([&](int i, int64_t r) { store_few_f32<W>(e.out0, r * e.out0_pitch + col, v[i]); });
+    else each([&](int i, int64_t r) { store_few<W>(e.out0, r * e.out0_pitch + col, e.bf16, v[i]); });
   } else if constexpr (OP == D_DX) {
-    if (e.in1) {
-#pragma unroll
-      for (int i = 0; i < R; ++i) v[i] = add(v[i], widen4(in[i].a, e.bf16));
-    }
-    if (e.out0) each([&](int i, int64_t r) { store4<FULL>(e.out0, r * e.out0_pitch + col, n, e.v_out0, e.bf16, v[i]); });
+    if (e.in1) add_in();
+    if (e.out0) each([&](int i, int64_t r) { store_few<W>(e.out0, r * e.out0_pitch + col, e.bf16, v[i]); });
     if (e.out1) {
       with_activation(e.act, [&](auto act) {
-        constexpr int A = decltype(act)::value;
 #pragma unroll
-        for (int i = 0; i < R; ++i) {
-          const float4 z = widen4(in[i].b, e.bf16);
-          v[i] = make_float4(through<A>(v[i].x, z.x), through<A>(v[i].y, z.y), through<A>(v[i].z, z.z), through<A>(v[i].w, z.w));
-        }
+        for (int i = 0; i < R; ++i)
+          map_pairs<W>(v[i], [&](u64 d, int j) { return through2<decltype(act)::value>(d, pack2(x.b[i][j], x.b[i][W == 1 ? 0 : j + 1])); });
       });
-      each([&](int i, int64_t r) { store4<FULL>(e.out1, r * e.out1_pitch + col, n, e.v_out1, e.bf16, v[i]); });
+      each([&](int i, int64_t r) { store_few<W>(e.out1, r * e.out1_pitch + col, e.bf16, v[i]); });
     }
   } else {
-    if (e.accumulate) {
-#pragma unroll
-      for (int i = 0; i < R; ++i) v[i] = add(v[i], in[i].a);
-    }
-    const int64_t at = (int64_t)which * e.out0_stride + col;
-    if (e.out0_fp32) each([&](int i, int64_t r) { store4_f32<FULL>(reinterpret_cast<float*>(e.out0) + at + r * e.out0_pitch, n, e.v_out0, v[i]); });
-    else each([&](int i, int64_t r) { store4<FULL>(e.out0, at + r * e.out0_pitch, n, e.v_out0, e.bf16, v[i]); });
+    if (e.accumulate) add_in();
+    if (e.out0_fp32) each([&](int i, int64_t r) { store_few_f32<W>(e.out0, out0_at<OP>(e, r, col, which), v[i]); });
+    else each([&](int i, int64_t r) { store_few<W>(e.out0, out0_at<OP>(e, r, col, which), e.bf16, v[i]); });
   }
 }
-template <int OP>
-__device__ __forceinline__ float4 bias4(const DenseEpi& e, int col, int n, int which) {
-  if (OP != D_FWD || !e.in0 || n <= 0) return make_float4(0.f, 0.f, 0.f, 0.f);
-  return widen4(raw4(e.in0, (int64_t)which * e.in0_stride + col, n, e.v_in0), e.bf16);
+template <int OP, int W>
+__device__ __forceinline__ void load_bias(const DenseEpi& e, int col, int which, float (&b)[W]) {
+#pragma unroll
+  for (int j = 0; j < W; ++j) b[j] = 0.f;
+  if (OP == D_FWD && e.in0) {
+#pragma unroll
+    for (int j = 0; j < W; ++j) b[j] = widen(reinterpret_cast<const uint16_t*>(e.in0)[(int64_t)which * e.in0_stride + col + j], e.bf16);
+  }
 }
 
 // ---- pairs of CTAs ---------------------------------------------------------------------------------------------------------
@@ -587,42 +759,50 @@ __global__ void __launch_bounds__(S::THREADS, 1) dense_gemm(const __grid_constan
       int b0, b1;
       block_range(blocks_of(c.red), b0, b1);
       const int m_base = c.m0 + quarter * 32;
-      // 32 columns of this warp's 32 rows through shared memory: a lane has a row of the accumulator and stores four columns of eight rows
-      float4* stage = reinterpret_cast<float4*>(out_stage + (warp - 2) * 4096);
-      constexpr int AHEAD = S::DRAIN ? 4 : 8;      // rows of a lane at a time: the sums take the registers
-      struct Ahead { EpiIn<S::OP> in[AHEAD]; float4 bias; };
-      const bool rows_full = epi.v_all && m_base + 32 <= c.m_end;
-      auto read_ahead = [&](Ahead& x, int j0, int i0) {
-        const int col = c.n0 + col0 + j0 + (lane & 7) * 4, n = c.n_end - col;
-        if (i0 == 0) x.bias = bias4<S::OP>(epi, col, n, c.w);
-        const int64_t m = m_base + i0 * 4 + (lane >> 3);
-        if (rows_full && n >= 4) {
+      // a warp's 4 KB of shared memory: the bias of its columns, or a 32 x 32 block on its way from rows to columns
+      float* stage = reinterpret_cast<float*>(out_stage + (warp - 2) * 4096);
+      const int m = m_base + lane;
+      auto by_rows = [&](int j0) { return epi.rows && c.n_end - (c.n0 + col0 + j0) >= 32; };
+      if (S::OP == D_FWD && !S::SPLIT && epi.in0 && by_rows(0)) {
+        __syncwarp();
 #pragma unroll
-          for (int i = 0; i < AHEAD; ++i) x.in[i] = load_in<S::OP, true>(epi, m + 4 * i, col, n, c.w);
-        } else {
-#pragma unroll
-          for (int i = 0; i < AHEAD; ++i)
-            if (m + 4 * i < c.m_end && n > 0) x.in[i] = load_in<S::OP, false>(epi, m + 4 * i, col, n, c.w);
+        for (int j = 0; j < S::COLS; j += 32) {
+          const int col = c.n0 + col0 + j + lane;
+          stage[j + lane] = col < c.n_end ? widen(reinterpret_cast<const uint16_t*>(epi.in0)[(int64_t)c.w * epi.in0_stride + col], epi.bf16) : 0.f;
         }
+        __syncwarp();
+      }
+      auto read_ahead = [&](RowIn<S::OP>& x, int j0) {
+        if (by_rows(j0) && m < c.m_end) row_ahead<S::OP>(epi, m, c.n0 + col0 + j0, x);
       };
-      auto write_out = [&](const float* v, int j0, Ahead& x) {
-        const int col = c.n0 + col0 + j0 + (lane & 7) * 4, n = c.n_end - col;
-        __syncwarp();
+      auto write_out = [&](u64 (&v)[16], int j0, const RowIn<S::OP>& x) {
+        const int col = c.n0 + col0 + j0;
+        if (by_rows(j0)) {
+          if (m < c.m_end) finish_row<S::OP>(epi, m, col, c.w, stage + j0, x, v);
+        } else if (col < c.n_end) {
+          __syncwarp();      // the bias, if it lies there, has been read: no more whole chunks follow
 #pragma unroll
-        for (int q = 0; q < 8; ++q) stage[lane * 8 + (q ^ (lane & 7))] = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
-        __syncwarp();
-#pragma unroll
-        for (int i0 = 0; i0 < 8; i0 += AHEAD) {
-          if (i0 > 0) read_ahead(x, j0, i0);
-          float4 u[AHEAD];
-#pragma unroll
-          for (int i = 0; i < AHEAD; ++i) {
-            const int r = (i0 + i) * 4 + (lane >> 3);
-            u[i] = stage[r * 8 + ((lane & 7) ^ (r & 7))];
+          for (int j = 0; j < 16; ++j) {
+            float lo, hi;
+            unpack2(v[j], lo, hi);
+            stage[lane * 32 + ((2 * j) ^ lane)] = lo;
+            stage[lane * 32 + ((2 * j + 1) ^ lane)] = hi;
           }
-          const int64_t m = m_base + i0 * 4 + (lane >> 3);
-          if (rows_full && n >= 4) finish_rows<S::OP, AHEAD, true>(epi, m, 4, c.m_end, col, n, c.w, x.bias, x.in, u);
-          else if (n > 0) finish_rows<S::OP, AHEAD, false>(epi, m, 4, c.m_end, col, n, c.w, x.bias, x.in, u);
+          __syncwarp();
+          if (col + lane < c.n_end) {
+            float bias[1];
+            load_bias<S::OP, 1>(epi, col + lane, c.w, bias);
+#pragma unroll 1
+            for (int r0 = 0; r0 < 32 && m_base + r0 < c.m_end; r0 += 8) {
+              ColumnIn<S::OP, 8, 1> in;
+              float u[8][1];
+              columns_ahead<S::OP, 8, 1>(epi, m_base + r0, 1, c.m_end, col + lane, c.w, in);
+#pragma unroll
+              for (int i = 0; i < 8; ++i) u[i][0] = stage[(r0 + i) * 32 + (lane ^ (r0 + i))];
+              finish_columns<S::OP, 8, 1>(epi, m_base + r0, 1, c.m_end, col + lane, c.w, bias, in, u);
+            }
+          }
+          __syncwarp();
         }
       };
       if constexpr (S::DRAIN) {
@@ -661,16 +841,19 @@ __global__ void __launch_bounds__(S::THREADS, 1) dense_gemm(const __grid_constan
         } else {
 #pragma unroll
           for (int j0 = 0; j0 < S::COLS; j0 += 32) {
-            Ahead x;
-            read_ahead(x, j0, 0);
-            write_out(sum + j0, j0, x);
+            RowIn<S::OP> x;
+            read_ahead(x, j0);
+            u64 v[16];
+#pragma unroll
+            for (int j = 0; j < 16; ++j) v[j] = pack2(sum[j0 + 2 * j], sum[j0 + 2 * j + 1]);
+            write_out(v, j0, x);
           }
         }
       } else {
         const int buf = lead % BUFS;
         const bool empty_sum = b1 == b0;      // a worker without rows: its weight gradient is zero
-        Ahead now, next;
-        read_ahead(now, 0, 0);
+        RowIn<S::OP> now, next;
+        read_ahead(now, 0);
         if (!empty_sum) {
           if (!warp_wait(&acc_full[buf], (lead / BUFS) & 1, abort_flag)) { *abort_flag = 1; break; }
           tc_fence_after();
@@ -678,7 +861,7 @@ __global__ void __launch_bounds__(S::THREADS, 1) dense_gemm(const __grid_constan
 #pragma unroll 1
         for (int j0 = 0; j0 < S::COLS; j0 += 32) {
           uint32_t r[32];
-          if (j0 + 32 < S::COLS) read_ahead(next, j0 + 32, 0);
+          if (j0 + 32 < S::COLS) read_ahead(next, j0 + 32);
           if (empty_sum) {
 #pragma unroll
             for (int j = 0; j < 32; ++j) r[j] = 0u;
@@ -686,9 +869,9 @@ __global__ void __launch_bounds__(S::THREADS, 1) dense_gemm(const __grid_constan
             tmem_ld32(t_lane + buf * S::ACC + j0, r);
           }
           if (j0 + 32 >= S::COLS && !empty_sum) release(buf);
-          float v[32];
+          u64 v[16];
 #pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(r[j]);
+          for (int j = 0; j < 16; ++j) v[j] = pack2(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1]));
           write_out(v, j0, now);
           now = next;
         }
@@ -710,30 +893,38 @@ __global__ void __launch_bounds__(S::THREADS, 1) dense_gemm(const __grid_constan
     cg::cluster_group cl = cg::this_cluster();
     cl.sync();
     const int ranks = gridDim.z, me = blockIdx.z;
-    constexpr int QUADS = (S::FEW ? BM : S::BN) / 4;      // of a row of the result
     const int rows = S::FEW ? min(S::BN, c.n_end - c.n0) : min(BM, c.m_end - c.m0);
     const int row0 = S::FEW ? c.n0 : c.m0, column0 = S::FEW ? c.m0 : c.n0, end = S::FEW ? c.m_end : c.n_end;
-    float* part = reinterpret_cast<float*>(tiles);
+    const float* part = reinterpret_cast<const float*>(tiles);
     // a thread keeps its columns and goes down the rows, four at a time
-    constexpr int AT_ONCE = 4, ROWS = S::THREADS / QUADS;      // rows that a CTA covers at once
-    const int q = tid % QUADS, col = column0 + 4 * q, n = end - col, step = ranks * ROWS;
-    if (tid < ROWS * QUADS && n > 0) {
-      const float4 bias = bias4<S::OP>(epi, col, n, c.w);
-      for (int r0 = me * ROWS + tid / QUADS; r0 < rows; r0 += AT_ONCE * step) {
-        EpiIn<S::OP> in[AT_ONCE];
-        float4 v[AT_ONCE];
+    auto finish = [&](auto width) {
+      constexpr int W = decltype(width)::value, ACROSS = (S::FEW ? BM : S::BN) / W, ROWS = S::THREADS / ACROSS, R = 4;      // threads to a row, rows of a CTA at once
+      const int q = tid % ACROSS, col = column0 + W * q, step = ranks * ROWS;
+      if (tid >= ROWS * ACROSS || col >= end) return;
+      float bias[W];
+      load_bias<S::OP, W>(epi, col, c.w, bias);
+#pragma unroll 1
+      for (int r0 = me * ROWS + tid / ACROSS; r0 < rows; r0 += R * step) {
+        ColumnIn<S::OP, R, W> in;
+        float v[R][W];
+        columns_ahead<S::OP, R, W>(epi, row0 + r0, step, row0 + rows, col, c.w, in);
 #pragma unroll
-        for (int i = 0; i < AT_ONCE; ++i)
-          if (r0 + i * step < rows) in[i] = load_in<S::OP, false>(epi, row0 + r0 + i * step, col, n, c.w);
+        for (int i = 0; i < R; ++i) {
 #pragma unroll
-        for (int i = 0; i < AT_ONCE; ++i) {
-          v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+          for (int j = 0; j < W; ++j) v[i][j] = 0.f;
           if (r0 + i * step < rows)
-            for (int k = 0; k < ranks; ++k) v[i] = add(v[i], *reinterpret_cast<const float4*>(cl.map_shared_rank(part, k) + (r0 + i * step) * S::PART_PITCH + 4 * q));
+            for (int k = 0; k < ranks; ++k) {
+              float u[W];
+              load_few_f32<W>(cl.map_shared_rank(part, k), (r0 + i * step) * S::PART_PITCH + W * q, u);
+#pragma unroll
+              for (int j = 0; j < W; ++j) v[i][j] += u[j];
+            }
         }
-        finish_rows<S::OP, AT_ONCE, false>(epi, row0 + r0, step, row0 + rows, col, n, c.w, bias, in, v);
+        finish_columns<S::OP, R, W>(epi, row0 + r0, step, row0 + rows, col, c.w, bias, in, v);
       }
-    }
+    };
+    if (epi.quads) finish(std::integral_constant<int, 4>());
+    else finish(std::integral_constant<int, 1>());
     cl.sync();                               // a CTA's shared memory outlives its readers
   }
   if (tid == 0 && *abort_flag) {
@@ -835,8 +1026,19 @@ constexpr int32_t MAX_FEATURES = 1 << 20;
 constexpr int64_t MAX_ROWS = (1ll << 31) - (1 << 20);
 
 bool tma_ok(const void* p, int64_t pitch) { return ((uintptr_t)p & 15) == 0 && pitch % 8 == 0; }
-int vec_ok(const void* p, int64_t pitch, int64_t stride, int size) {      // four values at once
-  return p && ((uintptr_t)p & (4 * size - 1)) == 0 && pitch % 4 == 0 && stride % 4 == 0;
+// May `bytes` bytes be moved at once, from every multiple of that in a row on?  (No matrix: yes.)
+bool moves(const void* p, int64_t pitch, int64_t stride, int size, int bytes) {
+  return !p || (((uintptr_t)p % bytes) == 0 && (pitch * size) % bytes == 0 && (stride * size) % bytes == 0);
+}
+struct EpiMatrix { const void* p; int64_t pitch, stride; int size; };
+void set_moves(DenseEpi& e, int columns, std::initializer_list<EpiMatrix> list) {
+  e.quads = columns % 4 == 0;
+  e.rows = e.wide = 1;
+  for (const EpiMatrix& m : list) {
+    e.quads = e.quads && moves(m.p, m.pitch, m.stride, m.size, 4 * m.size);
+    e.rows = e.rows && moves(m.p, m.pitch, m.stride, m.size, 16);
+    e.wide = e.wide && moves(m.p, m.pitch, m.stride, m.size, 32);
+  }
 }
 
 // A 16-bit matrix, or a stack of them.
@@ -1141,12 +1343,12 @@ int32_t workers_dense_forward(const ps_dense_layer* l, const ps_dense_output* o)
   if ((rc = lay_out(p.a, ws, p.st)) != PS_OK || (rc = lay_out(p.b, ws, p.st)) != PS_OK) return rc;
   sort_groups(l->rows, l->weight_of, l->groups, p.tab);
   DenseEpi& e = p.epi;
-  e.in0 = o->bias; e.in0_stride = o->bias_stride; e.v_in0 = vec_ok(o->bias, 0, l->n_weights > 1 ? o->bias_stride : 0, 2);
-  e.in1 = o->residual; e.in1_pitch = o->residual_pitch; e.v_in1 = vec_ok(o->residual, o->residual_pitch, 0, 2);
-  e.out0 = o->y; e.out0_pitch = o->y_pitch; e.v_out0 = vec_ok(o->y, o->y_pitch, 0, ys); e.out0_fp32 = ys == 4;
-  e.out1 = o->pre; e.out1_pitch = o->pre_pitch; e.v_out1 = vec_ok(o->pre, o->pre_pitch, 0, 2);
+  e.in0 = o->bias; e.in0_stride = o->bias_stride;
+  e.in1 = o->residual; e.in1_pitch = o->residual_pitch;
+  e.out0 = o->y; e.out0_pitch = o->y_pitch; e.out0_fp32 = ys == 4;
+  e.out1 = o->pre; e.out1_pitch = o->pre_pitch;
   e.act = l->activation; e.bf16 = l->type == PS_TYPE_BF16;
-  e.v_all = e.v_out0 && (!o->pre || e.v_out1) && (!o->residual || e.v_in1);
+  set_moves(e, N, {{o->residual, o->residual_pitch, 0, 2}, {o->y, o->y_pitch, 0, ys}, {o->pre, o->pre_pitch, 0, 2}});
   return run_rows<D_FWD>(p, N, K, ys == 4);
 }
 
@@ -1208,12 +1410,12 @@ int32_t workers_dense_backward(const ps_dense_layer* l, const ps_dense_gradients
     p.b = w;
     sort_groups(l->rows, l->weight_of, l->groups, p.tab);
     DenseEpi& e = p.epi;
-    e.in1 = o->dx_add; e.in1_pitch = o->dx_add_pitch; e.v_in1 = vec_ok(o->dx_add, o->dx_add_pitch, 0, 2);
-    e.in2 = o->x_pre; e.in2_pitch = o->x_pre_pitch; e.v_in2 = vec_ok(o->x_pre, o->x_pre_pitch, 0, 2);
-    e.out0 = o->dx; e.out0_pitch = o->dx_pitch; e.v_out0 = vec_ok(o->dx, o->dx_pitch, 0, 2);
-    e.out1 = o->dx_pre; e.out1_pitch = o->dx_pre_pitch; e.v_out1 = vec_ok(o->dx_pre, o->dx_pre_pitch, 0, 2);
+    e.in1 = o->dx_add; e.in1_pitch = o->dx_add_pitch;
+    e.in2 = o->x_pre; e.in2_pitch = o->x_pre_pitch;
+    e.out0 = o->dx; e.out0_pitch = o->dx_pitch;
+    e.out1 = o->dx_pre; e.out1_pitch = o->dx_pre_pitch;
     e.act = l->activation; e.bf16 = l->type == PS_TYPE_BF16;
-    e.v_all = (!o->dx || e.v_out0) && (!o->dx_pre || (e.v_out1 && e.v_in2)) && (!o->dx_add || e.v_in1);
+    set_moves(e, K, {{o->dx_add, o->dx_add_pitch, 0, 2}, {o->dx_pre ? o->x_pre : nullptr, o->x_pre_pitch, 0, 2}, {o->dx, o->dx_pitch, 0, 2}, {o->dx_pre, o->dx_pre_pitch, 0, 2}});
     if ((rc = run_rows<D_DX>(p, K, N, false)) != PS_OK) return rc;
   }
   if (o->dw) {
@@ -1224,9 +1426,8 @@ int32_t workers_dense_backward(const ps_dense_layer* l, const ps_dense_gradients
     p.tab = workers;
     DenseEpi& e = p.epi;
     e.out0 = o->dw; e.out0_pitch = o->dw_pitch; e.out0_stride = o->dw_stride; e.out0_fp32 = ds == 4; e.accumulate = o->accumulate;
-    e.v_out0 = vec_ok(o->dw, o->dw_pitch, l->groups > 1 ? o->dw_stride : 0, ds);
     e.bf16 = l->type == PS_TYPE_BF16;
-    e.v_all = e.v_out0;
+    set_moves(e, K, {{o->dw, o->dw_pitch, l->groups > 1 ? o->dw_stride : 0, ds}});
     if ((rc = run_weights(p, N, K, ds == 4)) != PS_OK) return rc;
   }
   return PS_OK;
