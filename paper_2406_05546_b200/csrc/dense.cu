@@ -85,7 +85,7 @@ struct DenseEpi {
   void *out0, *out1;
   int64_t in0_stride, in1_pitch, in2_pitch, out0_pitch, out0_stride, out1_pitch;
   int32_t act, bf16, out0_fp32, accumulate;
-  int32_t quads, rows, wide;      // may four values be moved at once, 16 bytes, 32 bytes, in every matrix there is?
+  int32_t pairs, quads, rows, wide;      // may two values, four, 16 bytes, 32 bytes be moved at once, in every matrix there is?
 };
 
 struct DenseArgs {
@@ -329,47 +329,24 @@ __device__ __forceinline__ void finish_row(const DenseEpi& e, int64_t row, int c
   }
 }
 
-// Columns: a lane has W (1 or 4) consecutive columns of R rows, row0 + i * step, of which those below `end` exist.  W = 1 for matrices of any
-// alignment and at their right edge.
-template <int W> __device__ __forceinline__ void load_few(const void* base, int64_t i, int bf16, float (&v)[W]) {
+// Columns, for matrices of any alignment and at their right edge: a lane has W = 1, 2 or 4 consecutive columns of R rows, row0 + i * step, of which
+// those below `end` exist.  Its values are in pairs, of columns (W > 1) or of rows.
+// Value h (0 or 1) of pair p: its row and its column.
+template <int W> __host__ __device__ constexpr int pair_row(int p, int h) { return W == 1 ? 2 * p + h : 2 * p / W; }
+template <int W> __host__ __device__ constexpr int pair_col(int p, int h) { return W == 1 ? 0 : 2 * p % W + h; }
+template <int W> __device__ __forceinline__ void load_few(const void* base, int64_t i, uint32_t (&w)[(W + 1) / 2]) {      // W values of 16 bits
   const uint16_t* p = reinterpret_cast<const uint16_t*>(base) + i;
-  if constexpr (W == 1) {
-    v[0] = widen(*p, bf16);
-  } else {
-    const uint2 w = *reinterpret_cast<const uint2*>(p);
-    unpack2(widen2(w.x, bf16), v[0], v[1]);
-    unpack2(widen2(w.y, bf16), v[2], v[3]);
-  }
+  if constexpr (W == 1) w[0] = *p;
+  else if constexpr (W == 2) w[0] = *reinterpret_cast<const uint32_t*>(p);
+  else { const uint2 v = *reinterpret_cast<const uint2*>(p); w[0] = v.x; w[1] = v.y; }
 }
-template <int W> __device__ __forceinline__ void store_few(void* base, int64_t i, int bf16, const float (&v)[W]) {
-  uint16_t* p = reinterpret_cast<uint16_t*>(base) + i;
-  if constexpr (W == 1) *p = (uint16_t)narrow2(v[0], 0.f, bf16);
-  else *reinterpret_cast<uint2*>(p) = make_uint2(narrow2(v[0], v[1], bf16), narrow2(v[2], v[3], bf16));
-}
-template <int W> __device__ __forceinline__ void load_few_f32(const void* base, int64_t i, float (&v)[W]) {
+template <int W> __device__ __forceinline__ void load_few_f32(const void* base, int64_t i, uint32_t (&w)[W]) {
   const float* p = reinterpret_cast<const float*>(base) + i;
-  if constexpr (W == 1) {
-    v[0] = *p;
-  } else {
-    const float4 w = *reinterpret_cast<const float4*>(p);
-    v[0] = w.x; v[1] = w.y; v[2] = w.z; v[3] = w.w;
-  }
+  if constexpr (W == 1) w[0] = __float_as_uint(*p);
+  else if constexpr (W == 2) { const uint2 v = *reinterpret_cast<const uint2*>(p); w[0] = v.x; w[1] = v.y; }
+  else { const uint4 v = *reinterpret_cast<const uint4*>(p); w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w; }
 }
-template <int W> __device__ __forceinline__ void store_few_f32(void* base, int64_t i, const float (&v)[W]) {
-  float* p = reinterpret_cast<float*>(base) + i;
-  if constexpr (W == 1) *p = v[0];
-  else *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-}
-template <int W, typename F> __device__ __forceinline__ void map_pairs(float (&v)[W], F f) {      // f(pair, index of its first)
-  if constexpr (W == 1) {
-    float unused;
-    unpack2(f(pack2(v[0], v[0]), 0), v[0], unused);
-  } else {
-    unpack2(f(pack2(v[0], v[1]), 0), v[0], v[1]);
-    unpack2(f(pack2(v[2], v[3]), 2), v[2], v[3]);
-  }
-}
-template <int OP, int R, int W> struct ColumnIn { float a[R][W], b[OP == D_DX ? R : 1][W]; };
+template <int OP, int R, int W> struct ColumnIn { uint32_t a[R][OP == D_DW ? W : (W + 1) / 2], b[OP == D_DX ? R : 1][(W + 1) / 2]; };
 template <int OP, int R, int W>
 __device__ __forceinline__ void columns_ahead(const DenseEpi& e, int64_t row0, int step, int64_t end, int col, int which, ColumnIn<OP, R, W>& x) {
 #pragma unroll
@@ -379,58 +356,89 @@ __device__ __forceinline__ void columns_ahead(const DenseEpi& e, int64_t row0, i
     if constexpr (OP == D_DW) {
       if (e.accumulate) {
         if (e.out0_fp32) load_few_f32<W>(e.out0, out0_at<OP>(e, r, col, which), x.a[i]);
-        else load_few<W>(e.out0, out0_at<OP>(e, r, col, which), e.bf16, x.a[i]);
+        else load_few<W>(e.out0, out0_at<OP>(e, r, col, which), *reinterpret_cast<uint32_t (*)[(W + 1) / 2]>(&x.a[i]));
       }
     } else {
-      if (e.in1) load_few<W>(e.in1, r * e.in1_pitch + col, e.bf16, x.a[i]);
+      if (e.in1) load_few<W>(e.in1, r * e.in1_pitch + col, x.a[i]);
       if constexpr (OP == D_DX)
-        if (e.out1) load_few<W>(e.in2, r * e.in2_pitch + col, e.bf16, x.b[i]);
+        if (e.out1) load_few<W>(e.in2, r * e.in2_pitch + col, x.b[i]);
     }
   }
 }
-// One kind of work for all rows, then the next.
+// Pair p of what was loaded as 16 bits.
+template <int R, int W, int N> __device__ __forceinline__ u64 pair_of(const uint32_t (&x)[R][N], int p, int bf16) {
+  if constexpr (W == 1) return widen2(x[2 * p][0] | (x[2 * p + 1][0] << 16), bf16);
+  else return widen2(x[pair_row<W>(p, 0)][pair_col<W>(p, 0) / 2], bf16);
+}
+template <int R, int W> __device__ __forceinline__ void store_columns(void* base, int64_t pitch, int64_t at, int64_t row0, int step, int64_t end, int fp32, int bf16, const u64 (&v)[R * W / 2]) {
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    const int64_t r = row0 + i * step;
+    if (r >= end) continue;
+    float f[4];
+#pragma unroll
+    for (int j = 0; j < W; j += 2) {
+      if (W == 1) {
+        float lo, hi;
+        unpack2(v[i / 2], lo, hi);
+        f[0] = i & 1 ? hi : lo;
+      } else {
+        unpack2(v[i * (W / 2) + j / 2], f[j], f[j + 1]);
+      }
+    }
+    if (fp32) {
+      float* p = reinterpret_cast<float*>(base) + at + r * pitch;
+      if constexpr (W == 1) *p = f[0];
+      else if constexpr (W == 2) *reinterpret_cast<float2*>(p) = make_float2(f[0], f[1]);
+      else *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]);
+    } else {
+      uint16_t* p = reinterpret_cast<uint16_t*>(base) + at + r * pitch;
+      if constexpr (W == 1) *p = (uint16_t)narrow2(f[0], 0.f, bf16);
+      else if constexpr (W == 2) *reinterpret_cast<uint32_t*>(p) = narrow2(f[0], f[1], bf16);
+      else *reinterpret_cast<uint2*>(p) = make_uint2(narrow2(f[0], f[1], bf16), narrow2(f[2], f[3], bf16));
+    }
+  }
+}
+// One kind of work for all rows, then the next.  bias: of the lane's columns.
 template <int OP, int R, int W>
 __device__ __forceinline__ void finish_columns(const DenseEpi& e, int64_t row0, int step, int64_t end, int col, int which, const float (&bias)[W], const ColumnIn<OP, R, W>& x,
-                                               float (&v)[R][W]) {
-  auto each = [&](auto f) {
-#pragma unroll
-    for (int i = 0; i < R; ++i)
-      if (row0 + i * step < end) f(i, row0 + i * step);
-  };
+                                               u64 (&v)[R * W / 2]) {
+  constexpr int N = R * W / 2;
   auto add_in = [&]() {
+    if constexpr (OP != D_DW) {
 #pragma unroll
-    for (int i = 0; i < R; ++i)
-#pragma unroll
-      for (int j = 0; j < W; ++j) v[i][j] += x.a[i][j];
+      for (int p = 0; p < N; ++p) v[p] = add2(v[p], pair_of<R, W>(x.a, p, e.bf16));
+    }
   };
   if constexpr (OP == D_FWD) {
 #pragma unroll
-    for (int i = 0; i < R; ++i)
-#pragma unroll
-      for (int j = 0; j < W; ++j) v[i][j] += bias[j];
-    if (e.out1) each([&](int i, int64_t r) { store_few<W>(e.out1, r * e.out1_pitch + col, e.bf16, v[i]); });
+    for (int p = 0; p < N; ++p) v[p] = add2(v[p], pack2(bias[pair_col<W>(p, 0)], bias[pair_col<W>(p, 1)]));
+    if (e.out1) store_columns<R, W>(e.out1, e.out1_pitch, col, row0, step, end, 0, e.bf16, v);
     with_activation(e.act, [&](auto act) {
 #pragma unroll
-      for (int i = 0; i < R; ++i) map_pairs<W>(v[i], [&](u64 z, int) { return activate2<decltype(act)::value>(z); });
+      for (int p = 0; p < N; ++p) v[p] = activate2<decltype(act)::value>(v[p]);
     });
     if (e.in1) add_in();
-    if (e.out0_fp32) each([&](int i, int64_t r) { store_few_f32<W>(e.out0, r * e.out0_pitch + col, v[i]); });
-    else each([&](int i, int64_t r) { store_few<W>(e.out0, r * e.out0_pitch + col, e.bf16, v[i]); });
+    store_columns<R, W>(e.out0, e.out0_pitch, col, row0, step, end, e.out0_fp32, e.bf16, v);
   } else if constexpr (OP == D_DX) {
     if (e.in1) add_in();
-    if (e.out0) each([&](int i, int64_t r) { store_few<W>(e.out0, r * e.out0_pitch + col, e.bf16, v[i]); });
+    if (e.out0) store_columns<R, W>(e.out0, e.out0_pitch, col, row0, step, end, 0, e.bf16, v);
     if (e.out1) {
       with_activation(e.act, [&](auto act) {
 #pragma unroll
-        for (int i = 0; i < R; ++i)
-          map_pairs<W>(v[i], [&](u64 d, int j) { return through2<decltype(act)::value>(d, pack2(x.b[i][j], x.b[i][W == 1 ? 0 : j + 1])); });
+        for (int p = 0; p < N; ++p) v[p] = through2<decltype(act)::value>(v[p], pair_of<R, W>(x.b, p, e.bf16));
       });
-      each([&](int i, int64_t r) { store_few<W>(e.out1, r * e.out1_pitch + col, e.bf16, v[i]); });
+      store_columns<R, W>(e.out1, e.out1_pitch, col, row0, step, end, 0, e.bf16, v);
     }
   } else {
-    if (e.accumulate) add_in();
-    if (e.out0_fp32) each([&](int i, int64_t r) { store_few_f32<W>(e.out0, out0_at<OP>(e, r, col, which), v[i]); });
-    else each([&](int i, int64_t r) { store_few<W>(e.out0, out0_at<OP>(e, r, col, which), e.bf16, v[i]); });
+    if (e.accumulate) {
+#pragma unroll
+      for (int p = 0; p < N; ++p) {
+        v[p] = add2(v[p], e.out0_fp32 ? pack2(__uint_as_float(x.a[pair_row<W>(p, 0)][pair_col<W>(p, 0)]), __uint_as_float(x.a[pair_row<W>(p, 1)][pair_col<W>(p, 1)]))
+                                      : pair_of<R, W>(x.a, p, e.bf16));
+      }
+    }
+    store_columns<R, W>(e.out0, e.out0_pitch, out0_at<OP>(e, 0, col, which), row0, step, end, e.out0_fp32, e.bf16, v);
   }
 }
 template <int OP, int W>
@@ -789,19 +797,28 @@ __global__ void __launch_bounds__(S::THREADS, 1) dense_gemm(const __grid_constan
             stage[lane * 32 + ((2 * j + 1) ^ lane)] = hi;
           }
           __syncwarp();
-          if (col + lane < c.n_end) {
-            float bias[1];
-            load_bias<S::OP, 1>(epi, col + lane, c.w, bias);
+          // W columns of every 32 / W lanes; rows W at a time side by side
+          auto columns = [&](auto width) {
+            constexpr int W = decltype(width)::value, R = 8;
+            const int at = lane % (32 / W) * W, sub = lane / (32 / W);
+            if (col + at >= c.n_end) return;
+            float bias[W];
+            load_bias<S::OP, W>(epi, col + at, c.w, bias);
 #pragma unroll 1
-            for (int r0 = 0; r0 < 32 && m_base + r0 < c.m_end; r0 += 8) {
-              ColumnIn<S::OP, 8, 1> in;
-              float u[8][1];
-              columns_ahead<S::OP, 8, 1>(epi, m_base + r0, 1, c.m_end, col + lane, c.w, in);
+            for (int r0 = sub; r0 < 32 && m_base + r0 < c.m_end; r0 += R * W) {
+              ColumnIn<S::OP, R, W> in;
+              u64 u[R * W / 2];
+              columns_ahead<S::OP, R, W>(epi, m_base + r0, W, c.m_end, col + at, c.w, in);
 #pragma unroll
-              for (int i = 0; i < 8; ++i) u[i][0] = stage[(r0 + i) * 32 + (lane ^ (r0 + i))];
-              finish_columns<S::OP, 8, 1>(epi, m_base + r0, 1, c.m_end, col + lane, c.w, bias, in, u);
+              for (int p = 0; p < R * W / 2; ++p) {
+                const int r = r0 + W * pair_row<W>(p, 0), r2 = r0 + W * pair_row<W>(p, 1);
+                u[p] = pack2(stage[r * 32 + ((at + pair_col<W>(p, 0)) ^ r)], stage[r2 * 32 + ((at + pair_col<W>(p, 1)) ^ r2)]);
+              }
+              finish_columns<S::OP, R, W>(epi, m_base + r0, W, c.m_end, col + at, c.w, bias, in, u);
             }
-          }
+          };
+          if (epi.pairs) columns(std::integral_constant<int, 2>());
+          else columns(std::integral_constant<int, 1>());
           __syncwarp();
         }
       };
@@ -906,20 +923,23 @@ __global__ void __launch_bounds__(S::THREADS, 1) dense_gemm(const __grid_constan
 #pragma unroll 1
       for (int r0 = me * ROWS + tid / ACROSS; r0 < rows; r0 += R * step) {
         ColumnIn<S::OP, R, W> in;
-        float v[R][W];
+        u64 v[R * W / 2];
         columns_ahead<S::OP, R, W>(epi, row0 + r0, step, row0 + rows, col, c.w, in);
+        float u[R][W];
 #pragma unroll
         for (int i = 0; i < R; ++i) {
 #pragma unroll
-          for (int j = 0; j < W; ++j) v[i][j] = 0.f;
+          for (int j = 0; j < W; ++j) u[i][j] = 0.f;
           if (r0 + i * step < rows)
             for (int k = 0; k < ranks; ++k) {
-              float u[W];
-              load_few_f32<W>(cl.map_shared_rank(part, k), (r0 + i * step) * S::PART_PITCH + W * q, u);
+              uint32_t w[W];
+              load_few_f32<W>(cl.map_shared_rank(part, k), (r0 + i * step) * S::PART_PITCH + W * q, w);
 #pragma unroll
-              for (int j = 0; j < W; ++j) v[i][j] += u[j];
+              for (int j = 0; j < W; ++j) u[i][j] += __uint_as_float(w[j]);
             }
         }
+#pragma unroll
+        for (int p = 0; p < R * W / 2; ++p) v[p] = pack2(u[pair_row<W>(p, 0)][pair_col<W>(p, 0)], u[pair_row<W>(p, 1)][pair_col<W>(p, 1)]);
         finish_columns<S::OP, R, W>(epi, row0 + r0, step, row0 + rows, col, c.w, bias, in, v);
       }
     };
@@ -1009,15 +1029,46 @@ __global__ void __launch_bounds__(CSUM_TPB) column_sums(const __grid_constant__ 
   cl.sync();
 }
 
-// Rows of 16-bit values to a pitch that the tile copies can read.
-__global__ void __launch_bounds__(256) lay_out_rows(const uint16_t* __restrict__ src, uint16_t* __restrict__ dst, int64_t rows, int32_t cols, int64_t pitch, int64_t dst_pitch,
-                                                    int64_t matrix_rows, int64_t matrix_stride) {
+// Matrices of 16-bit values to pitches that the tile copies can read: a warp per piece of LAY_WORDS words of a row, read in aligned words (a row that
+// starts in the middle of one is shifted across the lanes) and written in words.  Up to three stacks in one launch, of a stack of weights those that
+// are used.
+constexpr int LAY_STEPS = 8, LAY_WORDS = 32 * LAY_STEPS;
+struct LayStack {
+  const uint16_t* src; uint16_t* dst;
+  int64_t pitch, dst_pitch, stride, dst_stride, rows;      // of one matrix
+  int32_t cols, pieces;                                    // pieces of a row
+  int64_t first;                                           // units before this stack's
+};
+struct LayArgs { LayStack m[3]; int32_t n; int64_t units; };
+__global__ void __launch_bounds__(256) lay_out_rows(const __grid_constant__ LayArgs a, const __grid_constant__ DenseTab tab) {
   pdl_enter();
-  for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
-    const int64_t w = r / matrix_rows;
-    const uint16_t* s = src + w * matrix_stride + (r - w * matrix_rows) * pitch;
-    uint16_t* d = dst + r * dst_pitch;
-    for (int c = threadIdx.x; c < cols; c += 256) d[c] = s[c];
+  const int lane = threadIdx.x & 31;
+  for (int64_t unit = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); unit < a.units; unit += (int64_t)gridDim.x * 8) {
+    int k = 0;
+    while (k + 1 < a.n && unit >= a.m[k + 1].first) ++k;
+    const LayStack& m = a.m[k];
+    const int64_t l = unit - m.first, row = l / m.pieces;
+    const int piece = (int)(l - row * m.pieces);
+    const int64_t which = row / m.rows, r = row - which * m.rows, w = m.stride ? tab.run_w[which] : 0;
+    const uint16_t* src = m.src + w * m.stride + r * m.pitch;
+    const uintptr_t at = (uintptr_t)src;
+    const bool odd = (at & 2) != 0;
+    const uint32_t* in = reinterpret_cast<const uint32_t*>(at & ~(uintptr_t)3);
+    uint32_t* out = reinterpret_cast<uint32_t*>(m.dst + w * m.dst_stride + r * m.dst_pitch);
+    const int words = (m.cols + 1) / 2, last = (m.cols - 1 + (odd ? 1 : 0)) / 2;      // written; the last one that holds a value
+    const int w0 = piece * LAY_WORDS;
+    uint32_t v[LAY_STEPS + 1];
+#pragma unroll
+    for (int i = 0; i <= LAY_STEPS; ++i) {
+      const int j = w0 + 32 * i + lane;
+      v[i] = j <= last && (i < LAY_STEPS || (odd && lane == 0)) ? in[j] : 0u;
+    }
+#pragma unroll
+    for (int i = 0; i < LAY_STEPS; ++i) {
+      const uint32_t beside = __shfl_down_sync(0xffffffffu, v[i], 1), next = __shfl_sync(0xffffffffu, v[i + 1], 0);
+      const int j = w0 + 32 * i + lane;
+      if (j < words) out[j] = odd ? __funnelshift_r(v[i], lane == 31 ? next : beside, 16) : v[i];
+    }
   }
 }
 
@@ -1032,9 +1083,11 @@ bool moves(const void* p, int64_t pitch, int64_t stride, int size, int bytes) {
 }
 struct EpiMatrix { const void* p; int64_t pitch, stride; int size; };
 void set_moves(DenseEpi& e, int columns, std::initializer_list<EpiMatrix> list) {
+  e.pairs = columns % 2 == 0;
   e.quads = columns % 4 == 0;
   e.rows = e.wide = 1;
   for (const EpiMatrix& m : list) {
+    e.pairs = e.pairs && moves(m.p, m.pitch, m.stride, m.size, 2 * m.size);
     e.quads = e.quads && moves(m.p, m.pitch, m.stride, m.size, 4 * m.size);
     e.rows = e.rows && moves(m.p, m.pitch, m.stride, m.size, 16);
     e.wide = e.wide && moves(m.p, m.pitch, m.stride, m.size, 32);
@@ -1276,19 +1329,38 @@ Operand row_operand(const void* p, int64_t rows, int64_t cols, int64_t pitch) {
 struct Layout {      // hands out the workspace
   uint8_t* at;
   uint64_t left;
+  LayArgs args;
 };
-int32_t lay_out(Operand& o, Layout& ws, cudaStream_t st) {
+// Has the operand laid out, if the tile copies cannot read it as it is.  used: the weight matrices that are (0: this is no stack of weights).
+int32_t lay_out(Operand& o, Layout& ws, int used) {
   if (operand_ok(o)) return PS_OK;
   const uint64_t need = laid_out_bytes(o);
   if (!ws.at || ws.left < need) return fail(PS_ERR_ARENA_TOO_SMALL, "an operand has to be laid out anew (its base is not on 16 bytes or its pitch no multiple of 8): %llu more bytes of workspace needed", (unsigned long long)need);
   uint16_t* d = reinterpret_cast<uint16_t*>(((uintptr_t)ws.at + 255) & ~(uintptr_t)255);
-  const int64_t pitch = (o.cols + 7) / 8 * 8, rows = o.rows * o.count;
-  launch_pdl(lay_out_rows, dim3((unsigned)std::min<int64_t>(rows, 148 * 16)), 256, 0, st, reinterpret_cast<const uint16_t*>(o.p), d, rows, (int32_t)o.cols, o.pitch, pitch, o.rows, o.stride);
-  if (cudaGetLastError() != cudaSuccess) return fail(PS_ERR_CUDA, "operand copy launch");
+  const int64_t pitch = (o.cols + 7) / 8 * 8;
+  LayStack& m = ws.args.m[ws.args.n++];
+  m.src = reinterpret_cast<const uint16_t*>(o.p); m.dst = d;
+  m.pitch = o.pitch; m.dst_pitch = pitch; m.rows = o.rows;
+  m.stride = used && o.count > 1 ? o.stride : 0; m.dst_stride = o.rows * pitch;
+  m.cols = (int32_t)o.cols; m.pieces = (int32_t)(((o.cols + 1) / 2 + LAY_WORDS - 1) / LAY_WORDS);
+  m.first = ws.args.units;
+  ws.args.units += (used ? std::min<int64_t>(used, o.count) : 1) * o.rows * m.pieces;
   ws.at += need;
   ws.left -= need;
   o = Operand{d, o.rows, o.cols, pitch, o.count, o.rows * pitch};
   return PS_OK;
+}
+int32_t run_layout(const Layout& ws, const DenseTab& tab, cudaStream_t st) {
+  if (ws.args.n == 0) return PS_OK;
+  launch_pdl(lay_out_rows, dim3((unsigned)std::min<int64_t>((ws.args.units + 7) / 8, 148 * 32)), 256, 0, st, ws.args, tab);
+  return cudaGetLastError() == cudaSuccess ? PS_OK : fail(PS_ERR_CUDA, "operand copy launch");
+}
+// The weight matrices in use, each once, into run_w (cut_rows makes the same list again).
+int list_used(DenseTab& tab) {
+  tab.runs = 0;
+  for (int g = 0; g < tab.groups; ++g)
+    if (g == 0 || tab.w[g] != tab.w[g - 1]) tab.run_w[tab.runs++] = tab.w[g];
+  return tab.runs;
 }
 
 }  // namespace
@@ -1339,9 +1411,9 @@ int32_t workers_dense_forward(const ps_dense_layer* l, const ps_dense_output* o)
   p.st = (cudaStream_t)l->stream;
   p.a = row_operand(l->x, rows, K, l->x_pitch);
   p.b = weight_operand(l);
-  Layout ws = {(uint8_t*)l->workspace, l->workspace_bytes};
-  if ((rc = lay_out(p.a, ws, p.st)) != PS_OK || (rc = lay_out(p.b, ws, p.st)) != PS_OK) return rc;
   sort_groups(l->rows, l->weight_of, l->groups, p.tab);
+  Layout ws = {(uint8_t*)l->workspace, l->workspace_bytes, {}};
+  if ((rc = lay_out(p.a, ws, 0)) != PS_OK || (rc = lay_out(p.b, ws, list_used(p.tab))) != PS_OK || (rc = run_layout(ws, p.tab, p.st)) != PS_OK) return rc;
   DenseEpi& e = p.epi;
   e.in0 = o->bias; e.in0_stride = o->bias_stride;
   e.in1 = o->residual; e.in1_pitch = o->residual_pitch;
@@ -1372,12 +1444,15 @@ int32_t workers_dense_backward(const ps_dense_layer* l, const ps_dense_gradients
   if ((rc = setup()) != PS_OK) return rc;
   cudaStream_t st = (cudaStream_t)l->stream;
   Operand x = row_operand(l->x, rows, K, l->x_pitch), dy = row_operand(o->dy, rows, N, o->dy_pitch), w = weight_operand(l);
-  Layout ws = {(uint8_t*)l->workspace, l->workspace_bytes};
+  DenseTab sorted = {};
   if (rows > 0) {
+    sort_groups(l->rows, l->weight_of, l->groups, sorted);
     const bool want_x = o->dw != nullptr, want_w = o->dx || o->dx_pre;
-    if ((want_x || want_w) && (rc = lay_out(dy, ws, st)) != PS_OK) return rc;
-    if (want_x && (rc = lay_out(x, ws, st)) != PS_OK) return rc;
-    if (want_w && (rc = lay_out(w, ws, st)) != PS_OK) return rc;
+    Layout ws = {(uint8_t*)l->workspace, l->workspace_bytes, {}};
+    if ((want_x || want_w) && (rc = lay_out(dy, ws, 0)) != PS_OK) return rc;
+    if (want_x && (rc = lay_out(x, ws, 0)) != PS_OK) return rc;
+    if (want_w && (rc = lay_out(w, ws, list_used(sorted))) != PS_OK) return rc;
+    if ((rc = run_layout(ws, sorted, st)) != PS_OK) return rc;
   } else {      // nobody has a row: the gradients are zero
     cudaError_t ce = cudaSuccess;
     for (int g = 0; g < l->groups && !o->accumulate && ce == cudaSuccess; ++g) {
@@ -1394,9 +1469,9 @@ int32_t workers_dense_backward(const ps_dense_layer* l, const ps_dense_gradients
   }
   if (o->db) {
     ColumnSumArgs c = {};
-    c.dy = o->dy; c.db = o->db; c.pitch = o->dy_pitch; c.db_stride = o->db_stride;
+    c.dy = dy.p; c.db = o->db; c.pitch = dy.pitch; c.db_stride = o->db_stride;
     c.N = N; c.bf16 = l->type == PS_TYPE_BF16; c.db_fp32 = ds == 4; c.accumulate = o->accumulate;
-    c.vec = ((uintptr_t)o->dy & 15) == 0 && o->dy_pitch % 8 == 0;
+    c.vec = operand_ok(dy);
     const int blocks = div_up(N, CSUM_COLS) * l->groups;
     int split = 1;
     while (split < 8 && blocks * split < 4 * g_sm_count && rows / l->groups >= CSUM_ROWS * split) split *= 2;
@@ -1408,7 +1483,7 @@ int32_t workers_dense_backward(const ps_dense_layer* l, const ps_dense_gradients
     p.st = st;
     p.a = dy;
     p.b = w;
-    sort_groups(l->rows, l->weight_of, l->groups, p.tab);
+    p.tab = sorted;
     DenseEpi& e = p.epi;
     e.in1 = o->dx_add; e.in1_pitch = o->dx_add_pitch;
     e.in2 = o->x_pre; e.in2_pitch = o->x_pre_pitch;

@@ -221,7 +221,8 @@ def _bind_torch():
     import torch
     global _cuda
     load()
-    _marshal.bind_torch(torch.float32, lambda size, device: torch.empty(size, dtype=torch.uint8, device=f"cuda:{device}"))
+    devices = [torch.device("cuda", i) for i in range(torch.cuda.device_count())]
+    _marshal.bind_torch(torch.float32, lambda size, device: torch.empty(size, dtype=torch.uint8, device=devices[device]))
     _cuda = torch._C
 
 
