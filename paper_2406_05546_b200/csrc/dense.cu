@@ -192,15 +192,20 @@ template <typename F> __device__ __forceinline__ void with_activation(int act, F
   else if (act == PS_ACT_SILU) f(std::integral_constant<int, PS_ACT_SILU>());
 }
 
-__device__ __forceinline__ u64 widen2(uint32_t w, int bf16) {
-  if (bf16) return pack2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+// f(whether the operands are BF16, as a constant): asked once for a chunk of a tile
+template <typename F> __device__ __forceinline__ void with_type(int bf16, F f) {
+  if (bf16) f(std::true_type());
+  else f(std::false_type());
+}
+template <bool BF16> __device__ __forceinline__ u64 widen2(uint32_t w) {
+  if (BF16) return pack2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
   const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
   return pack2(f.x, f.y);
 }
-__device__ __forceinline__ uint32_t narrow_pair(u64 v, int bf16) {
+template <bool BF16> __device__ __forceinline__ uint32_t narrow_pair(u64 v) {
   float a, b;
   unpack2(v, a, b);
-  return narrow2(a, b, bf16);
+  return narrow2(a, b, BF16);
 }
 
 // 32 or 16 bytes of a lane in one access.
@@ -245,10 +250,11 @@ __device__ __forceinline__ void store_row(void* p, int wide, const uint32_t (&w)
     for (int i = 0; i < WORDS / 4; ++i) reinterpret_cast<uint4*>(p)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
   }
 }
-__device__ __forceinline__ void store_row16(void* base, int64_t at, int wide, int bf16, const u64 (&v)[16]) {
+template <bool BF16>
+__device__ __forceinline__ void store_row16(void* base, int64_t at, int wide, const u64 (&v)[16]) {
   uint32_t w[16];
 #pragma unroll
-  for (int i = 0; i < 16; ++i) w[i] = narrow_pair(v[i], bf16);
+  for (int i = 0; i < 16; ++i) w[i] = narrow_pair<BF16>(v[i]);
   store_row(reinterpret_cast<uint16_t*>(base) + at, wide, w);
 }
 __device__ __forceinline__ void store_row32(void* base, int64_t at, int wide, const u64 (&v)[16]) {
@@ -269,8 +275,8 @@ __device__ __forceinline__ void row_ahead(const DenseEpi& e, int64_t row, int co
   }
 }
 // bias: 32 floats in shared memory
-template <int OP>
-__device__ __forceinline__ void finish_row(const DenseEpi& e, int64_t row, int col, int which, const float* bias, const RowIn<OP>& x, u64 (&v)[16]) {
+template <int OP, bool BF16>
+__device__ __forceinline__ void finish_row_of(const DenseEpi& e, int64_t row, int col, int which, const float* bias, const RowIn<OP>& x, u64 (&v)[16]) {
   if constexpr (OP == D_FWD) {
     if (e.in0) {
 #pragma unroll
@@ -280,7 +286,7 @@ __device__ __forceinline__ void finish_row(const DenseEpi& e, int64_t row, int c
         v[2 * i + 1] = add2(v[2 * i + 1], pack2(b.z, b.w));
       }
     }
-    if (e.out1) store_row16(e.out1, row * e.out1_pitch + col, e.wide, e.bf16, v);
+    if (e.out1) store_row16<BF16>(e.out1, row * e.out1_pitch + col, e.wide, v);
     with_activation(e.act, [&](auto act) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) v[i] = activate2<decltype(act)::value>(v[i]);
@@ -289,20 +295,20 @@ __device__ __forceinline__ void finish_row(const DenseEpi& e, int64_t row, int c
   if constexpr (OP != D_DW) {
     if (e.in1) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) v[i] = add2(v[i], widen2(x.a[i], e.bf16));
+      for (int i = 0; i < 16; ++i) v[i] = add2(v[i], widen2<BF16>(x.a[i]));
     }
   }
   if constexpr (OP == D_FWD) {
     if (e.out0_fp32) store_row32(e.out0, row * e.out0_pitch + col, e.wide, v);
-    else store_row16(e.out0, row * e.out0_pitch + col, e.wide, e.bf16, v);
+    else store_row16<BF16>(e.out0, row * e.out0_pitch + col, e.wide, v);
   } else if constexpr (OP == D_DX) {
-    if (e.out0) store_row16(e.out0, row * e.out0_pitch + col, e.wide, e.bf16, v);
+    if (e.out0) store_row16<BF16>(e.out0, row * e.out0_pitch + col, e.wide, v);
     if (e.out1) {
       with_activation(e.act, [&](auto act) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = through2<decltype(act)::value>(v[i], widen2(x.b[i], e.bf16));
+        for (int i = 0; i < 16; ++i) v[i] = through2<decltype(act)::value>(v[i], widen2<BF16>(x.b[i]));
       });
-      store_row16(e.out1, row * e.out1_pitch + col, e.wide, e.bf16, v);
+      store_row16<BF16>(e.out1, row * e.out1_pitch + col, e.wide, v);
     }
   } else {
     const int64_t at = out0_at<OP>(e, row, col, which);
@@ -322,11 +328,16 @@ __device__ __forceinline__ void finish_row(const DenseEpi& e, int64_t row, int c
         uint32_t o[16];
         load_row(e.out0, at, e.wide, o);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = add2(v[i], widen2(o[i], e.bf16));
+        for (int i = 0; i < 16; ++i) v[i] = add2(v[i], widen2<BF16>(o[i]));
       }
-      store_row16(e.out0, at, e.wide, e.bf16, v);
+      store_row16<BF16>(e.out0, at, e.wide, v);
     }
   }
+}
+
+template <int OP>
+__device__ __forceinline__ void finish_row(const DenseEpi& e, int64_t row, int col, int which, const float* bias, const RowIn<OP>& x, u64 (&v)[16]) {
+  with_type(e.bf16, [&](auto bf16) { finish_row_of<OP, decltype(bf16)::value>(e, row, col, which, bias, x, v); });
 }
 
 // Columns, for matrices of any alignment and at their right edge: a lane has W = 1, 2 or 4 consecutive columns of R rows, row0 + i * step, of which
@@ -347,99 +358,122 @@ template <int W> __device__ __forceinline__ void load_few_f32(const void* base, 
   else { const uint4 v = *reinterpret_cast<const uint4*>(p); w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w; }
 }
 template <int OP, int R, int W> struct ColumnIn { uint32_t a[R][OP == D_DW ? W : (W + 1) / 2], b[OP == D_DX ? R : 1][(W + 1) / 2]; };
-template <int OP, int R, int W>
-__device__ __forceinline__ void columns_ahead(const DenseEpi& e, int64_t row0, int step, int64_t end, int col, int which, ColumnIn<OP, R, W>& x) {
+// f(i) for the rows that exist; FULL: all R do.  Nothing else is asked for a row: a branch a row took longer than the row.
+template <int R, bool FULL, typename F> __device__ __forceinline__ void each_row(int64_t row0, int step, int64_t end, F f) {
 #pragma unroll
-  for (int i = 0; i < R; ++i) {
-    const int64_t r = row0 + i * step;
-    if (r >= end) continue;
-    if constexpr (OP == D_DW) {
-      if (e.accumulate) {
-        if (e.out0_fp32) load_few_f32<W>(e.out0, out0_at<OP>(e, r, col, which), x.a[i]);
-        else load_few<W>(e.out0, out0_at<OP>(e, r, col, which), *reinterpret_cast<uint32_t (*)[(W + 1) / 2]>(&x.a[i]));
-      }
-    } else {
-      if (e.in1) load_few<W>(e.in1, r * e.in1_pitch + col, x.a[i]);
-      if constexpr (OP == D_DX)
-        if (e.out1) load_few<W>(e.in2, r * e.in2_pitch + col, x.b[i]);
+  for (int i = 0; i < R; ++i)
+    if (FULL || row0 + i * step < end) f(i);
+}
+template <int OP, int R, int W, bool FULL>
+__device__ __forceinline__ void columns_ahead_of(const DenseEpi& e, int64_t row0, int step, int64_t end, int col, int which, ColumnIn<OP, R, W>& x) {
+  if constexpr (OP == D_DW) {
+    if (e.accumulate) {
+      const int64_t at = out0_at<OP>(e, row0, col, which), down = step * e.out0_pitch;
+      if (e.out0_fp32) each_row<R, FULL>(row0, step, end, [&](int i) { load_few_f32<W>(e.out0, at + i * down, x.a[i]); });
+      else each_row<R, FULL>(row0, step, end, [&](int i) { load_few<W>(e.out0, at + i * down, *reinterpret_cast<uint32_t (*)[(W + 1) / 2]>(&x.a[i])); });
     }
+  } else {
+    if (e.in1) {
+      const int64_t at = row0 * e.in1_pitch + col, down = step * e.in1_pitch;
+      each_row<R, FULL>(row0, step, end, [&](int i) { load_few<W>(e.in1, at + i * down, x.a[i]); });
+    }
+    if constexpr (OP == D_DX)
+      if (e.out1) {
+        const int64_t at = row0 * e.in2_pitch + col, down = step * e.in2_pitch;
+        each_row<R, FULL>(row0, step, end, [&](int i) { load_few<W>(e.in2, at + i * down, x.b[i]); });
+      }
   }
 }
-// Pair p of what was loaded as 16 bits.
-template <int R, int W, int N> __device__ __forceinline__ u64 pair_of(const uint32_t (&x)[R][N], int p, int bf16) {
-  if constexpr (W == 1) return widen2(x[2 * p][0] | (x[2 * p + 1][0] << 16), bf16);
-  else return widen2(x[pair_row<W>(p, 0)][pair_col<W>(p, 0) / 2], bf16);
+template <int OP, int R, int W>
+__device__ __forceinline__ void columns_ahead(const DenseEpi& e, int64_t row0, int step, int64_t end, int col, int which, ColumnIn<OP, R, W>& x) {
+  if (row0 + (R - 1) * step < end) columns_ahead_of<OP, R, W, true>(e, row0, step, end, col, which, x);
+  else columns_ahead_of<OP, R, W, false>(e, row0, step, end, col, which, x);
 }
-template <int R, int W> __device__ __forceinline__ void store_columns(void* base, int64_t pitch, int64_t at, int64_t row0, int step, int64_t end, int fp32, int bf16, const u64 (&v)[R * W / 2]) {
-#pragma unroll
-  for (int i = 0; i < R; ++i) {
-    const int64_t r = row0 + i * step;
-    if (r >= end) continue;
-    float f[4];
-#pragma unroll
-    for (int j = 0; j < W; j += 2) {
-      if (W == 1) {
-        float lo, hi;
-        unpack2(v[i / 2], lo, hi);
-        f[0] = i & 1 ? hi : lo;
+// Pair p of what was loaded as 16 bits.
+template <int R, int W, bool BF16, int N> __device__ __forceinline__ u64 pair_of(const uint32_t (&x)[R][N], int p) {
+  if constexpr (W == 1) return widen2<BF16>(x[2 * p][0] | (x[2 * p + 1][0] << 16));
+  else return widen2<BF16>(x[pair_row<W>(p, 0)][pair_col<W>(p, 0) / 2]);
+}
+// at: the first row's element
+template <int R, int W, bool BF16, bool FULL>
+__device__ __forceinline__ void store_columns(void* base, int64_t pitch, int64_t at, int64_t row0, int step, int64_t end, int fp32, const u64 (&v)[R * W / 2]) {
+  const int64_t down = step * pitch;
+  if (fp32) {
+    each_row<R, FULL>(row0, step, end, [&](int i) {
+      float* p = reinterpret_cast<float*>(base) + at + i * down;
+      if constexpr (W == 1) {
+        *p = __uint_as_float(i & 1 ? (uint32_t)(v[i / 2] >> 32) : (uint32_t)v[i / 2]);
+      } else if constexpr (W == 2) {
+        *reinterpret_cast<u64*>(p) = v[i];
       } else {
-        unpack2(v[i * (W / 2) + j / 2], f[j], f[j + 1]);
+        *reinterpret_cast<ulonglong2*>(p) = make_ulonglong2(v[2 * i], v[2 * i + 1]);
       }
-    }
-    if (fp32) {
-      float* p = reinterpret_cast<float*>(base) + at + r * pitch;
-      if constexpr (W == 1) *p = f[0];
-      else if constexpr (W == 2) *reinterpret_cast<float2*>(p) = make_float2(f[0], f[1]);
-      else *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]);
-    } else {
-      uint16_t* p = reinterpret_cast<uint16_t*>(base) + at + r * pitch;
-      if constexpr (W == 1) *p = (uint16_t)narrow2(f[0], 0.f, bf16);
-      else if constexpr (W == 2) *reinterpret_cast<uint32_t*>(p) = narrow2(f[0], f[1], bf16);
-      else *reinterpret_cast<uint2*>(p) = make_uint2(narrow2(f[0], f[1], bf16), narrow2(f[2], f[3], bf16));
-    }
+    });
+  } else {
+    uint32_t w[R * W / 2];
+#pragma unroll
+    for (int p = 0; p < R * W / 2; ++p) w[p] = narrow_pair<BF16>(v[p]);
+    each_row<R, FULL>(row0, step, end, [&](int i) {
+      uint16_t* p = reinterpret_cast<uint16_t*>(base) + at + i * down;
+      if constexpr (W == 1) *p = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
+      else if constexpr (W == 2) *reinterpret_cast<uint32_t*>(p) = w[i];
+      else *reinterpret_cast<uint2*>(p) = make_uint2(w[2 * i], w[2 * i + 1]);
+    });
   }
 }
 // One kind of work for all rows, then the next.  bias: of the lane's columns.
-template <int OP, int R, int W>
-__device__ __forceinline__ void finish_columns(const DenseEpi& e, int64_t row0, int step, int64_t end, int col, int which, const float (&bias)[W], const ColumnIn<OP, R, W>& x,
-                                               u64 (&v)[R * W / 2]) {
+template <int OP, int R, int W, bool BF16, bool FULL>
+__device__ __forceinline__ void finish_columns_of(const DenseEpi& e, int64_t row0, int step, int64_t end, int col, int which, const float (&bias)[W], const ColumnIn<OP, R, W>& x,
+                                                  u64 (&v)[R * W / 2]) {
   constexpr int N = R * W / 2;
-  auto add_in = [&]() {
-    if constexpr (OP != D_DW) {
-#pragma unroll
-      for (int p = 0; p < N; ++p) v[p] = add2(v[p], pair_of<R, W>(x.a, p, e.bf16));
-    }
-  };
+  auto store = [&](void* base, int64_t pitch, int fp32) { store_columns<R, W, BF16, FULL>(base, pitch, row0 * pitch + col, row0, step, end, fp32, v); };
   if constexpr (OP == D_FWD) {
 #pragma unroll
     for (int p = 0; p < N; ++p) v[p] = add2(v[p], pack2(bias[pair_col<W>(p, 0)], bias[pair_col<W>(p, 1)]));
-    if (e.out1) store_columns<R, W>(e.out1, e.out1_pitch, col, row0, step, end, 0, e.bf16, v);
+    if (e.out1) store(e.out1, e.out1_pitch, 0);
     with_activation(e.act, [&](auto act) {
 #pragma unroll
       for (int p = 0; p < N; ++p) v[p] = activate2<decltype(act)::value>(v[p]);
     });
-    if (e.in1) add_in();
-    store_columns<R, W>(e.out0, e.out0_pitch, col, row0, step, end, e.out0_fp32, e.bf16, v);
+  }
+  if constexpr (OP != D_DW) {
+    if (e.in1) {
+#pragma unroll
+      for (int p = 0; p < N; ++p) v[p] = add2(v[p], pair_of<R, W, BF16>(x.a, p));
+    }
+  }
+  if constexpr (OP == D_FWD) {
+    store(e.out0, e.out0_pitch, e.out0_fp32);
   } else if constexpr (OP == D_DX) {
-    if (e.in1) add_in();
-    if (e.out0) store_columns<R, W>(e.out0, e.out0_pitch, col, row0, step, end, 0, e.bf16, v);
+    if (e.out0) store(e.out0, e.out0_pitch, 0);
     if (e.out1) {
       with_activation(e.act, [&](auto act) {
 #pragma unroll
-        for (int p = 0; p < N; ++p) v[p] = through2<decltype(act)::value>(v[p], pair_of<R, W>(x.b, p, e.bf16));
+        for (int p = 0; p < N; ++p) v[p] = through2<decltype(act)::value>(v[p], pair_of<R, W, BF16>(x.b, p));
       });
-      store_columns<R, W>(e.out1, e.out1_pitch, col, row0, step, end, 0, e.bf16, v);
+      store(e.out1, e.out1_pitch, 0);
     }
   } else {
     if (e.accumulate) {
+      if (e.out0_fp32) {
 #pragma unroll
-      for (int p = 0; p < N; ++p) {
-        v[p] = add2(v[p], e.out0_fp32 ? pack2(__uint_as_float(x.a[pair_row<W>(p, 0)][pair_col<W>(p, 0)]), __uint_as_float(x.a[pair_row<W>(p, 1)][pair_col<W>(p, 1)]))
-                                      : pair_of<R, W>(x.a, p, e.bf16));
+        for (int p = 0; p < N; ++p)
+          v[p] = add2(v[p], pack2(__uint_as_float(x.a[pair_row<W>(p, 0)][pair_col<W>(p, 0)]), __uint_as_float(x.a[pair_row<W>(p, 1)][pair_col<W>(p, 1)])));
+      } else {
+#pragma unroll
+        for (int p = 0; p < N; ++p) v[p] = add2(v[p], pair_of<R, W, BF16>(x.a, p));
       }
     }
-    store_columns<R, W>(e.out0, e.out0_pitch, out0_at<OP>(e, 0, col, which), row0, step, end, e.out0_fp32, e.bf16, v);
+    store_columns<R, W, BF16, FULL>(e.out0, e.out0_pitch, out0_at<OP>(e, row0, col, which), row0, step, end, e.out0_fp32, v);
   }
+}
+template <int OP, int R, int W>
+__device__ __forceinline__ void finish_columns(const DenseEpi& e, int64_t row0, int step, int64_t end, int col, int which, const float (&bias)[W], const ColumnIn<OP, R, W>& x,
+                                               u64 (&v)[R * W / 2]) {
+  with_type(e.bf16, [&](auto bf16) {
+    if (row0 + (R - 1) * step < end) finish_columns_of<OP, R, W, decltype(bf16)::value, true>(e, row0, step, end, col, which, bias, x, v);
+    else finish_columns_of<OP, R, W, decltype(bf16)::value, false>(e, row0, step, end, col, which, bias, x, v);
+  });
 }
 template <int OP, int W>
 __device__ __forceinline__ void load_bias(const DenseEpi& e, int col, int which, float (&b)[W]) {
@@ -788,38 +822,43 @@ __global__ void __launch_bounds__(S::THREADS, 1) dense_gemm(const __grid_constan
         if (by_rows(j0)) {
           if (m < c.m_end) finish_row<S::OP>(epi, m, col, c.w, stage + j0, x, v);
         } else if (col < c.n_end) {
-          __syncwarp();      // the bias, if it lies there, has been read: no more whole chunks follow
-#pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            float lo, hi;
-            unpack2(v[j], lo, hi);
-            stage[lane * 32 + ((2 * j) ^ lane)] = lo;
-            stage[lane * 32 + ((2 * j + 1) ^ lane)] = hi;
-          }
-          __syncwarp();
-          // W columns of every 32 / W lanes; rows W at a time side by side
+          // W columns of every 32 / W lanes, rows W at a time side by side; everything is loaded before the block is turned round
           auto columns = [&](auto width) {
-            constexpr int W = decltype(width)::value, R = 8;
-            const int at = lane % (32 / W) * W, sub = lane / (32 / W);
-            if (col + at >= c.n_end) return;
+            constexpr int W = decltype(width)::value, R = S::DRAIN || (S::OP == D_DX && W == 1) ? 8 : 32 / W;
+            const int at = lane % (32 / W) * W, sub = lane / (32 / W), here = col + at;
+            const bool mine = here < c.n_end;
             float bias[W];
-            load_bias<S::OP, W>(epi, col + at, c.w, bias);
-#pragma unroll 1
-            for (int r0 = sub; r0 < 32 && m_base + r0 < c.m_end; r0 += R * W) {
-              ColumnIn<S::OP, R, W> in;
-              u64 u[R * W / 2];
-              columns_ahead<S::OP, R, W>(epi, m_base + r0, W, c.m_end, col + at, c.w, in);
-#pragma unroll
-              for (int p = 0; p < R * W / 2; ++p) {
-                const int r = r0 + W * pair_row<W>(p, 0), r2 = r0 + W * pair_row<W>(p, 1);
-                u[p] = pack2(stage[r * 32 + ((at + pair_col<W>(p, 0)) ^ r)], stage[r2 * 32 + ((at + pair_col<W>(p, 1)) ^ r2)]);
-              }
-              finish_columns<S::OP, R, W>(epi, m_base + r0, W, c.m_end, col + at, c.w, bias, in, u);
+            ColumnIn<S::OP, R, W> in;
+            if (mine) {
+              load_bias<S::OP, W>(epi, here, c.w, bias);
+              columns_ahead<S::OP, R, W>(epi, m_base + sub, W, c.m_end, here, c.w, in);
             }
+            __syncwarp();      // the bias, if it lies there, has been read: no more whole chunks follow
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+              float lo, hi;
+              unpack2(v[j], lo, hi);
+              stage[lane * 32 + ((2 * j) ^ lane)] = lo;
+              stage[lane * 32 + ((2 * j + 1) ^ lane)] = hi;
+            }
+            __syncwarp();
+            if (mine) {
+#pragma unroll 1
+              for (int r0 = sub; r0 < 32 && m_base + r0 < c.m_end; r0 += R * W) {
+                if (r0 != sub) columns_ahead<S::OP, R, W>(epi, m_base + r0, W, c.m_end, here, c.w, in);
+                u64 u[R * W / 2];
+#pragma unroll
+                for (int p = 0; p < R * W / 2; ++p) {
+                  const int r = r0 + W * pair_row<W>(p, 0), r2 = r0 + W * pair_row<W>(p, 1);
+                  u[p] = pack2(stage[r * 32 + ((at + pair_col<W>(p, 0)) ^ r)], stage[r2 * 32 + ((at + pair_col<W>(p, 1)) ^ r2)]);
+                }
+                finish_columns<S::OP, R, W>(epi, m_base + r0, W, c.m_end, here, c.w, bias, in, u);
+              }
+            }
+            __syncwarp();
           };
           if (epi.pairs) columns(std::integral_constant<int, 2>());
           else columns(std::integral_constant<int, 1>());
-          __syncwarp();
         }
       };
       if constexpr (S::DRAIN) {
@@ -913,18 +952,20 @@ __global__ void __launch_bounds__(S::THREADS, 1) dense_gemm(const __grid_constan
     const int rows = S::FEW ? min(S::BN, c.n_end - c.n0) : min(BM, c.m_end - c.m0);
     const int row0 = S::FEW ? c.n0 : c.m0, column0 = S::FEW ? c.m0 : c.n0, end = S::FEW ? c.m_end : c.n_end;
     const float* part = reinterpret_cast<const float*>(tiles);
-    // a thread keeps its columns and goes down the rows, four at a time
+    // a thread keeps its columns and goes down the rows, R at a time, the next ones' loads under way
     auto finish = [&](auto width) {
-      constexpr int W = decltype(width)::value, ACROSS = (S::FEW ? BM : S::BN) / W, ROWS = S::THREADS / ACROSS, R = 4;      // threads to a row, rows of a CTA at once
-      const int q = tid % ACROSS, col = column0 + W * q, step = ranks * ROWS;
-      if (tid >= ROWS * ACROSS || col >= end) return;
+      constexpr int W = decltype(width)::value, R = W == 4 ? 4 : 8;
+      const int across = (min(S::FEW ? BM : S::BN, end - column0) + W - 1) / W, at_once = S::THREADS / across, step = ranks * at_once;      // threads to a row; rows of a CTA at once
+      const int q = tid % across, col = column0 + W * q, first = me * at_once + tid / across;
+      if (tid >= at_once * across || first >= rows) return;
       float bias[W];
       load_bias<S::OP, W>(epi, col, c.w, bias);
+      ColumnIn<S::OP, R, W> in, next;
+      columns_ahead<S::OP, R, W>(epi, row0 + first, step, row0 + rows, col, c.w, in);
 #pragma unroll 1
-      for (int r0 = me * ROWS + tid / ACROSS; r0 < rows; r0 += R * step) {
-        ColumnIn<S::OP, R, W> in;
+      for (int r0 = first; r0 < rows; r0 += R * step) {
+        if (r0 + R * step < rows) columns_ahead<S::OP, R, W>(epi, row0 + r0 + R * step, step, row0 + rows, col, c.w, next);
         u64 v[R * W / 2];
-        columns_ahead<S::OP, R, W>(epi, row0 + r0, step, row0 + rows, col, c.w, in);
         float u[R][W];
 #pragma unroll
         for (int i = 0; i < R; ++i) {
@@ -941,6 +982,7 @@ __global__ void __launch_bounds__(S::THREADS, 1) dense_gemm(const __grid_constan
 #pragma unroll
         for (int p = 0; p < R * W / 2; ++p) v[p] = pack2(u[pair_row<W>(p, 0)][pair_col<W>(p, 0)], u[pair_row<W>(p, 1)][pair_col<W>(p, 1)]);
         finish_columns<S::OP, R, W>(epi, row0 + r0, step, row0 + rows, col, c.w, bias, in, v);
+        in = next;
       }
     };
     if (epi.quads) finish(std::integral_constant<int, 4>());
