@@ -56,7 +56,7 @@ template <int OP_, int CTAS_, int BN_, int STAGES_, bool SPLIT_, bool FEW_, bool
   static constexpr int B_ROWS = BN / CTAS;
   static constexpr int A_BYTES = BM * BK * 2, B_BYTES = B_ROWS * BK * 2, STAGE = A_BYTES + B_BYTES;
   static constexpr int BUFS = SPLIT ? 1 : 2, ACC = BN < 32 ? 32 : BN;
-  static constexpr int EPI_WARPS = FEW ? 4 : 8, THREADS = 64 + 32 * EPI_WARPS, COLS = FEW ? BN : BN / 2;
+  static constexpr int EPI_WARPS = FEW ? 4 : 8, THREADS = 64 + 32 * EPI_WARPS, COLS = BN / (EPI_WARPS / 4);
   static constexpr int OUT_BYTES = SPLIT ? 0 : EPI_WARPS * 4096;      // a 32 x 32 block per warp on its way to whole rows
   static constexpr int SMEM = 1024 + STAGES * STAGE + OUT_BYTES + BARRIER_BYTES;
   static constexpr int PART_PITCH = FEW ? BM + 4 : BN + 4, PART_BYTES = (FEW ? BN : BM) * PART_PITCH * 4;
@@ -208,13 +208,14 @@ template <bool BF16> __device__ __forceinline__ uint32_t narrow_pair(u64 v) {
   return narrow2(a, b, BF16);
 }
 
-// 32 or 16 bytes of a lane in one access.
+// 32 bytes of a lane in one access, first out of L2 again: what the epilogue moves is not needed there, what the products read is (8,192 x 2048 -> 5120
+// with everything on 154 -> 141 us).
 __device__ __forceinline__ void load_words(const void* p, uint32_t (&w)[8]) {
-  asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+  asm volatile("ld.global.L1::no_allocate.L2::evict_first.L2::256B.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
                : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p));
 }
 __device__ __forceinline__ void store_words(void* p, const uint32_t* w) {
-  asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+  asm volatile("st.global.L1::no_allocate.L2::evict_first.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
                ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
 }
 
@@ -824,7 +825,7 @@ __global__ void __launch_bounds__(S::THREADS, 1) dense_gemm(const __grid_constan
         } else if (col < c.n_end) {
           // W columns of every 32 / W lanes, rows W at a time side by side; everything is loaded before the block is turned round
           auto columns = [&](auto width) {
-            constexpr int W = decltype(width)::value, R = S::DRAIN || (S::OP == D_DX && W == 1) ? 8 : 32 / W;
+            constexpr int W = decltype(width)::value, R = S::DRAIN ? 8 / W : 8;
             const int at = lane % (32 / W) * W, sub = lane / (32 / W), here = col + at;
             const bool mine = here < c.n_end;
             float bias[W];
