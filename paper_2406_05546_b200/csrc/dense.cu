@@ -66,7 +66,7 @@ template <int OP_, int CTAS_, int BN_, int STAGES_, bool SPLIT_, bool FEW_, bool
 };
 template <int OP, bool DRAIN> using Pair = DenseShape<OP, 2, 256, 6, false, false, DRAIN>;
 template <int OP, bool DRAIN> using Single = DenseShape<OP, 1, 256, 4, false, false, DRAIN>;
-template <int OP> using Split = DenseShape<OP, 1, 128, 3, true, false, true>;
+template <int OP> using Split = DenseShape<OP, 1, 128, 6, true, false, true>;
 template <int OP, int BN> using Few = DenseShape<OP, 1, BN, BN == 64 ? 4 : 5, true, true, true>;
 
 // Forward and input gradient: groups of rows [row0[g], row1[g]), those with the same weights next to each other (a run), cut into blocks of rows;
@@ -948,38 +948,45 @@ __global__ void __launch_bounds__(S::THREADS, 1) dense_gemm(const __grid_constan
     DenseTile c;
     decode_tile<S>(a, tab, blockIdx.x, 0, c);
     cg::cluster_group cl = cg::this_cluster();
-    cl.sync();
     const int ranks = gridDim.z, me = blockIdx.z;
     const int rows = S::FEW ? min(S::BN, c.n_end - c.n0) : min(BM, c.m_end - c.m0);
     const int row0 = S::FEW ? c.n0 : c.m0, column0 = S::FEW ? c.m0 : c.n0, end = S::FEW ? c.m_end : c.n_end;
     const float* part = reinterpret_cast<const float*>(tiles);
-    // a thread keeps its columns and goes down the rows, R at a time, the next ones' loads under way
+    // a thread keeps its columns and goes down the rows, R at a time, what is read for the next ones under way (for the first, while the cluster's
+    // CTAs wait for one another)
     auto finish = [&](auto width) {
       constexpr int W = decltype(width)::value, R = W == 4 ? 4 : 8;
       const int across = (min(S::FEW ? BM : S::BN, end - column0) + W - 1) / W, at_once = S::THREADS / across, step = ranks * at_once;      // threads to a row; rows of a CTA at once
       const int q = tid % across, col = column0 + W * q, first = me * at_once + tid / across;
-      if (tid >= at_once * across || first >= rows) return;
+      const bool active = tid < at_once * across && first < rows;
       float bias[W];
-      load_bias<S::OP, W>(epi, col, c.w, bias);
       ColumnIn<S::OP, R, W> in, next;
-      columns_ahead<S::OP, R, W>(epi, row0 + first, step, row0 + rows, col, c.w, in);
+      if (active) {
+        load_bias<S::OP, W>(epi, col, c.w, bias);
+        columns_ahead<S::OP, R, W>(epi, row0 + first, step, row0 + rows, col, c.w, in);
+      }
+      cl.sync();
+      if (!active) return;
 #pragma unroll 1
       for (int r0 = first; r0 < rows; r0 += R * step) {
         if (r0 + R * step < rows) columns_ahead<S::OP, R, W>(epi, row0 + r0 + R * step, step, row0 + rows, col, c.w, next);
-        u64 v[R * W / 2];
         float u[R][W];
 #pragma unroll
-        for (int i = 0; i < R; ++i) {
+        for (int i = 0; i < R; ++i)
 #pragma unroll
           for (int j = 0; j < W; ++j) u[i][j] = 0.f;
-          if (r0 + i * step < rows)
-            for (int k = 0; k < ranks; ++k) {
-              uint32_t w[W];
-              load_few_f32<W>(cl.map_shared_rank(part, k), (r0 + i * step) * S::PART_PITCH + W * q, w);
+        for (int k = 0; k < ranks; ++k) {
+          const float* from = (ranks == 1 ? part : cl.map_shared_rank(part, k)) + r0 * S::PART_PITCH + W * q;
+          auto take = [&](int i) {
+            uint32_t w[W];
+            load_few_f32<W>(from, i * step * S::PART_PITCH, w);
 #pragma unroll
-              for (int j = 0; j < W; ++j) u[i][j] += __uint_as_float(w[j]);
-            }
+            for (int j = 0; j < W; ++j) u[i][j] += __uint_as_float(w[j]);
+          };
+          if (r0 + (R - 1) * step < rows) each_row<R, true>(r0, step, rows, take);
+          else each_row<R, false>(r0, step, rows, take);
         }
+        u64 v[R * W / 2];
 #pragma unroll
         for (int p = 0; p < R * W / 2; ++p) v[p] = pack2(u[pair_row<W>(p, 0)][pair_col<W>(p, 0)], u[pair_row<W>(p, 1)][pair_col<W>(p, 1)]);
         finish_columns<S::OP, R, W>(epi, row0 + r0, step, row0 + rows, col, c.w, bias, in, v);
@@ -1190,7 +1197,7 @@ int32_t launch(const Problem& p, int split) {
   DenseArgs a = p.args;
   a.idesc = (1u << 4) | (p.epi.bf16 ? (1u << 7) | (1u << 10) : 0u) | (S::A_MN ? 1u << 15 : 0u) | (S::B_MN ? 1u << 16 : 0u) | ((uint32_t)(S::BN >> 3) << 17) |
             ((uint32_t)(S::TM >> 4) << 24);
-  a.chunk = S::DRAIN ? DRAIN_BLOCKS : 1 << 30;
+  a.chunk = S::DRAIN && p.epi.out0_fp32 ? DRAIN_BLOCKS : 1 << 30;
   cudaLaunchConfig_t cfg = {};
   const int walkers = g_sm_count / S::CTAS;
   cfg.gridDim = S::SPLIT ? dim3(a.n_tiles, 1, split) : dim3(S::CTAS * std::min(a.n_tiles, walkers));
@@ -1276,7 +1283,7 @@ int32_t run_rows(Problem& p, int features, int red, bool fp32_out) {
     return launch<Pair<OP, false>>(p, 1);
   }
   a.m_tiles = (int)row_blocks;
-  if (singles * 3 >= sms * 2) {
+  if (singles * 3 >= sms * 2 || row_blocks * div_up(features, 128) > sms) {
     a.n_tiles = (int)singles;
     if constexpr (OP == D_FWD) if (fp32_out) return launch<Single<OP, true>>(p, 1);
     return launch<Single<OP, false>>(p, 1);
@@ -1302,7 +1309,7 @@ int32_t run_weights(Problem& p, int N, int K, bool fp32_out) {
     a.n_tiles = (int)tiles(256);
     return fp32_out ? launch<Pair<D_DW, true>>(p, 1) : launch<Pair<D_DW, false>>(p, 1);
   }
-  if (singles * 3 >= sms * 2) {
+  if (singles * 3 >= sms * 2 || singles / a.n_tiles_n * div_up(K, 128) > sms) {
     a.n_tiles = (int)tiles(128);
     return fp32_out ? launch<Single<D_DW, true>>(p, 1) : launch<Single<D_DW, false>>(p, 1);
   }
