@@ -293,6 +293,27 @@ def test_8_bit_second_moments_follow_in_the_mean():
     assert mean() / first == pytest.approx(0.999 ** steps, abs=6 * sigma)
 
 
+@gpu
+@pytest.mark.parametrize("state_bits", [8, 32])
+def test_a_tensor_past_32_bits(state_bits):
+    """2^31 elements and some: the last ones, and those around the 2^31st, as a small tensor of the same values has them (whose second moments'
+    random bits, another matter, are looked at above)."""
+    n, tail = (1 << 31) + 2048 + 77, 2048 + 77
+    kind = torch.uint8 if state_bits == 8 else torch.float32
+    p, g = torch.full((n,), 0.5, dtype=torch.bfloat16, device="cuda"), torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    g[-tail:] = torch.randn(tail, generator=torch.Generator("cuda").manual_seed(2), device="cuda").bfloat16()
+    m, v = (torch.zeros(n, dtype=kind, device="cuda") for _ in range(2))
+    q, h = p[-tail:].clone(), g[-tail:].clone()
+    opt, ref = AdamW([p], [g], state_bits=state_bits, m=[m], v=[v]), AdamW([q], [h], state_bits=state_bits)
+    for o in (opt, ref):
+        o.ps_adamw_step(step=1, clip_norm=0.25, **HYPER)
+    torch.cuda.synchronize()
+    assert opt.ps_adamw_read_info()["grad_norm"] == ref.ps_adamw_read_info()["grad_norm"]
+    assert torch.equal(p[-tail:], q) and torch.equal(m[-tail:], ref.m[0])
+    assert (p[: 1 << 20] == p[0]).all() and not m[: 1 << 20].any() and not v[: 1 << 20].any()
+    opt.close()
+
+
 # ---- the gradient queue --------------------------------------------------------------------------------------------------
 def server(K, **more):
     theta = synth.init_params(1)

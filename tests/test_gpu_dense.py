@@ -355,6 +355,86 @@ def test_a_training_step_of_two_layers():
         assert all(torch.equal(c, p.bfloat16()) for c, p in zip(copies, master))
 
 
+@gpu
+@pytest.mark.parametrize("N", [256, 250, 251])
+@pytest.mark.parametrize("rows", [[5, 2], [140, 60], [2600]])
+def test_the_added_gradient_may_lie_where_the_result_goes(rows, N):
+    gen = torch.Generator("cuda").manual_seed(4)
+    make = lambda *s: torch.randn(*s, generator=gen, device="cuda").bfloat16()
+    K, M, G = N, sum(rows), len(rows)
+    x, w, dy, extra, z = make(M, K), make(G, N, K), make(M, N), make(M, K), make(M, K)
+    apart, apart_pre, pre = torch.empty_like(x), torch.empty_like(x), torch.empty_like(x)
+    workers_dense_backward(dy, x, w, rows, x_pre=z, activation="silu", dx_add=extra, dx=apart, dx_pre=apart_pre)
+    workers_dense_backward(dy, x, w, rows, x_pre=z, activation="silu", dx_add=extra, dx=extra, dx_pre=pre)
+    assert torch.equal(apart, extra) and torch.equal(apart_pre, pre)
+
+
+@gpu
+def test_odd_sizes_captured_and_replayed():
+    """Operands that are laid out anew: the workspace is the graph's own."""
+    gen = torch.Generator("cuda").manual_seed(5)
+    make = lambda *s: torch.randn(*s, generator=gen, device="cuda").bfloat16()
+    rows, K, N = [33, 0, 150], 77, 91
+    x, w, dy = make(183, K), make(3, N, K), make(183, N)
+    y, dx, dw, db = make(183, N), make(183, K), torch.zeros(3, N, K, device="cuda"), torch.zeros(3, N, device="cuda")
+
+    def call():
+        workers_dense_forward(x, w, rows, y=y)
+        workers_dense_backward(dy, x, w, rows, dx=dx, dw=dw, db=db)
+    call()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for _ in range(2):
+        x.copy_(make(183, K))
+        w.copy_(make(3, N, K))
+        graph.replay()
+        other = torch.randn(1 << 20, device="cuda")      # other work in memory that the calls outside the graph had
+        got = [t.clone() for t in (y, dx, dw, db)]
+        call()
+        assert all(torch.equal(a, b) for a, b in zip(got, (y, dx, dw, db)))
+        del other
+    del graph
+
+
+@gpu
+@pytest.mark.parametrize("K,N", [(16, 32768), (24, 32774)])
+def test_offsets_past_32_bits(K, N):
+    """Results of more than 2^31 elements: the last rows, and those on either side of the 2^31st element."""
+    M = (1 << 31) // N + 300
+    gen = torch.Generator("cuda").manual_seed(6)
+    x, w = torch.randn(M, K, generator=gen, device="cuda").bfloat16(), torch.randn(1, N, K, generator=gen, device="cuda").bfloat16()
+    y = torch.empty(M, N, dtype=torch.bfloat16, device="cuda")
+    workers_dense_forward(x, w, [M], y=y)
+    edge = (1 << 31) // N
+    for r in (slice(0, 3), slice(edge - 2, edge + 2), slice(M - 3, M)):
+        want = x[r].double() @ w[0].double().T
+        e = sum_error(x[r].double().abs() @ w[0].double().abs().T, K, False)
+        assert ((y[r].double() - want).abs() <= e + half_step(want.abs() + e, torch.bfloat16)).all()
+    # and read: a gradient whose rows lie that far out
+    dx = torch.empty(M, K, dtype=torch.bfloat16, device="cuda")
+    workers_dense_backward(y, x, w, [M], dx=dx)
+    r = slice(M - 3, M)
+    want = y[r].double() @ w[0].double()
+    e = sum_error(y[r].double().abs() @ w[0].double().abs(), N, False)
+    assert ((dx[r].double() - want).abs() <= e + half_step(want.abs() + e, torch.bfloat16)).all()
+
+
+@gpu
+def test_weight_gradients_past_32_bits():
+    """A gradient per worker, the last one's beyond the 2^31st element."""
+    G, N, K = 9, 16384, 16384
+    gen = torch.Generator("cuda").manual_seed(7)
+    x, dy = torch.randn(G, K, generator=gen, device="cuda").bfloat16(), torch.randn(G, N, generator=gen, device="cuda").bfloat16()
+    w, dw = torch.empty(1, N, K, dtype=torch.bfloat16, device="cuda"), torch.empty(G, N, K, dtype=torch.bfloat16, device="cuda")
+    workers_dense_backward(dy, x, w, [1] * G, weight_of=[0] * G, dw=dw)
+    for g in (0, G - 1):
+        want = dy[g].double()[:, None] * x[g].double()[None, :256]
+        assert ((dw[g][:, :256].double() - want).abs() <= half_step(want, torch.bfloat16) * 1.01).all()
+        want = dy[g].double()[-64:, None] * x[g].double()[None]
+        assert ((dw[g][-64:].double() - want).abs() <= half_step(want, torch.bfloat16) * 1.01).all()
+
+
 # ---- refusals --------------------------------------------------------------------------------------------------------------
 def layer(**more):
     """A layer whose addresses are never read: every refusal comes before any launch."""
