@@ -46,12 +46,14 @@ namespace cg = cooperative_groups;
 
 enum { D_FWD = 0, D_DX = 1, D_DW = 2 };
 constexpr int BM = 128, BK = 64;
+constexpr int THIN_RED = 256;        // reductions up to this length are bound by what they write: Thin tiles
 constexpr int DRAIN_BLOCKS = 8;      // blocks of k whose sums share an accumulator where the result is FP32
 constexpr int SMEM_MOST = 227 * 1024, BARRIER_BYTES = 256;
 
-template <int OP_, int CTAS_, int BN_, int STAGES_, bool SPLIT_, bool FEW_, bool DRAIN_> struct DenseShape {
+template <int OP_, int CTAS_, int BN_, int STAGES_, bool SPLIT_, bool FEW_, bool DRAIN_, int PER_SM_ = 1> struct DenseShape {
   static constexpr int OP = OP_, CTAS = CTAS_, BN = BN_, STAGES = STAGES_, TM = BM * CTAS;
   static constexpr bool SPLIT = SPLIT_, FEW = FEW_, DRAIN = DRAIN_;
+  static constexpr int PER_SM = PER_SM_;      // CTAs that an SM holds
   static constexpr bool A_MN = FEW ? OP == D_DX : OP == D_DW, B_MN = !FEW && OP != D_FWD;      // is the operand's row index contiguous?
   static constexpr int B_ROWS = BN / CTAS;
   static constexpr int A_BYTES = BM * BK * 2, B_BYTES = B_ROWS * BK * 2, STAGE = A_BYTES + B_BYTES;
@@ -66,6 +68,7 @@ template <int OP_, int CTAS_, int BN_, int STAGES_, bool SPLIT_, bool FEW_, bool
 };
 template <int OP, bool DRAIN> using Pair = DenseShape<OP, 2, 256, 6, false, false, DRAIN>;
 template <int OP, bool DRAIN> using Single = DenseShape<OP, 1, 256, 4, false, false, DRAIN>;
+template <int OP> using Thin = DenseShape<OP, 1, 128, 2, false, false, false, 2>;
 template <int OP> using Split = DenseShape<OP, 1, 128, 6, true, false, true>;
 template <int OP, int BN> using Few = DenseShape<OP, 1, BN, BN == 64 ? 4 : 5, true, true, true>;
 
@@ -623,7 +626,7 @@ __device__ __forceinline__ void decode_tile(const DenseArgs& a, const DenseTab& 
 __device__ __forceinline__ int blocks_of(int red) { return (red + BK - 1) / BK; }
 
 template <class S>
-__global__ void __launch_bounds__(S::THREADS, 1) dense_gemm(const __grid_constant__ DenseMaps maps, const __grid_constant__ DenseArgs a,
+__global__ void __launch_bounds__(S::THREADS, S::PER_SM) dense_gemm(const __grid_constant__ DenseMaps maps, const __grid_constant__ DenseArgs a,
                                                             const __grid_constant__ DenseEpi epi, const __grid_constant__ DenseTab tab) {
   constexpr int STAGES = S::STAGES, BUFS = S::BUFS, EPI = S::EPI_WARPS;
   constexpr bool PAIR = S::CTAS == 2, RAGGED = S::OP == D_DW;
@@ -1173,7 +1176,7 @@ int32_t setup() {      // once per device
   bool ok = configure_tc5_kernels() == 0;
   const cudaError_t e[] = {allow<Pair<D_FWD, false>>(), allow<Pair<D_FWD, true>>(), allow<Pair<D_DX, false>>(), allow<Pair<D_DW, false>>(), allow<Pair<D_DW, true>>(),
                            allow<Single<D_FWD, false>>(), allow<Single<D_FWD, true>>(), allow<Single<D_DX, false>>(), allow<Single<D_DW, false>>(), allow<Single<D_DW, true>>(),
-                           allow<Split<D_FWD>>(), allow<Split<D_DX>>(), allow<Split<D_DW>>(),
+                           allow<Thin<D_FWD>>(), allow<Thin<D_DX>>(), allow<Thin<D_DW>>(), allow<Split<D_FWD>>(), allow<Split<D_DX>>(), allow<Split<D_DW>>(),
                            allow<Few<D_FWD, 16>>(), allow<Few<D_FWD, 32>>(), allow<Few<D_FWD, 64>>(), allow<Few<D_DX, 16>>(), allow<Few<D_DX, 32>>(), allow<Few<D_DX, 64>>()};
   for (cudaError_t x : e) ok = ok && x == cudaSuccess;
   if (!ok) return fail(PS_ERR_CUDA, "kernel configuration failed: %s", cudaGetErrorString(cudaGetLastError()));
@@ -1199,7 +1202,7 @@ int32_t launch(const Problem& p, int split) {
             ((uint32_t)(S::TM >> 4) << 24);
   a.chunk = S::DRAIN && p.epi.out0_fp32 ? DRAIN_BLOCKS : 1 << 30;
   cudaLaunchConfig_t cfg = {};
-  const int walkers = g_sm_count / S::CTAS;
+  const int walkers = g_sm_count * S::PER_SM / S::CTAS;
   cfg.gridDim = S::SPLIT ? dim3(a.n_tiles, 1, split) : dim3(S::CTAS * std::min(a.n_tiles, walkers));
   cfg.blockDim = dim3(S::THREADS);
   cfg.dynamicSmemBytes = S::SMEM;
@@ -1273,6 +1276,14 @@ int32_t run_rows(Problem& p, int features, int red, bool fp32_out) {
     if (bn == 32) return launch<Few<OP, 32>>(p, split);
     return launch<Few<OP, 64>>(p, split);
   }
+  if (red <= THIN_RED && cut_rows(tab, BM, false) * div_up(features, 128) > sms) {
+    a.n_tiles_n = div_up(features, 128);
+    const int64_t t = cut_rows(tab, BM, false) * a.n_tiles_n;
+    if (t >= 1 << 30) return fail(PS_ERR_BAD_ARG, "too many tiles");
+    a.m_tiles = (int)(t / a.n_tiles_n);
+    a.n_tiles = (int)t;
+    return launch<Thin<OP>>(p, 1);
+  }
   a.n_tiles_n = div_up(features, 256);
   const int64_t row_blocks = cut_rows(tab, BM, false), pairs = cut_rows(tab, BM, true), singles = row_blocks * a.n_tiles_n;
   if (singles >= 1 << 30) return fail(PS_ERR_BAD_ARG, "too many tiles");
@@ -1301,8 +1312,13 @@ int32_t run_weights(Problem& p, int N, int K, bool fp32_out) {
   fp32_out = fp32_out && most > DRAIN_BLOCKS * BK;
   const int sms = g_sm_count;
   a.m_side = N; a.n_side = K; a.red = 0;
-  a.n_tiles_n = div_up(K, 256);
   auto tiles = [&](int tm) { a.m_tiles = div_up(N, tm); return (int64_t)tab.groups * a.m_tiles * a.n_tiles_n; };
+  a.n_tiles_n = div_up(K, 128);
+  if (most <= THIN_RED && tiles(128) > sms && tiles(128) < 1 << 30) {
+    a.n_tiles = (int)tiles(128);
+    return launch<Thin<D_DW>>(p, 1);
+  }
+  a.n_tiles_n = div_up(K, 256);
   const int64_t pairs = tiles(256), singles = tiles(128);
   if (singles >= 1 << 30) return fail(PS_ERR_BAD_ARG, "too many tiles");
   if (pairs * 2 >= sms && pairs * 2 <= singles + singles / 5) {
