@@ -10,10 +10,11 @@
 //   Pair   256 x 256 by two CTAs that share each MMA (cta_group::2): half of the right operand each, so that a CTA brings in 32 KB for
 //          128 x 256 x 64 products.  Two accumulators of 256 columns are used in turn: one is read out while the other fills.
 //   Single 128 x 256 by one CTA: workers with less than 256 rows.
+//   Thin   128 x 128, two CTAs on an SM, for reductions so short that writing bounds them.
 //   Split  128 x 128, the blocks of k dealt out over a cluster of CTAs whose partial tiles are added through distributed shared memory
 //          in a fixed order: few tiles.
 //   Few    weights as the left operand, 128 of their rows x 16, 32 or 64 rows of a worker, split likewise: bound by reading the weights.
-// Pair and Single run one CTA (pair) per SM that walks over the tiles; the others one cluster per tile.
+// Pair, Single and Thin run as many CTAs (pairs) as the SMs hold, which walk over the tiles; the others one cluster per tile.
 //
 // Precision: the accumulators drop the low bits of every sum, always towards zero (bf16x3.cuh).  For results in FP32 the sums over 512 values
 // of k are handed to registers and added there, rounded; for 16-bit results their own rounding is 100 times what is lost.
@@ -46,7 +47,11 @@ namespace cg = cooperative_groups;
 
 enum { D_FWD = 0, D_DX = 1, D_DW = 2 };
 constexpr int BM = 128, BK = 64;
-constexpr int THIN_RED = 256;        // reductions up to this length are bound by what they write: Thin tiles
+// Reductions up to this length are bound by what they write: Thin tiles.  us, Pair or Single -> Thin: forward, 8,192 rows -> 4096 with residual and GELU, K =
+// 64 53 -> 44, 256 57 -> 52, 384 61 -> 57, 512 65 -> 64, 768 72 -> 76; weight gradient, 16 workers of 1568 x 512 in FP32, 64 rows each 16.6 -> 13.2,
+// 300 20.6 -> 19.5, 500 24.7 -> 26.3, 8 workers of 2048 x 2048, 300 rows 30 -> 33.  The input gradient, which reads two matrices more, has not the
+// registers for it (64 -> 117).
+constexpr int THIN_RED_FWD = 384, THIN_RED_DW = 256;
 constexpr int DRAIN_BLOCKS = 8;      // blocks of k whose sums share an accumulator where the result is FP32
 constexpr int SMEM_MOST = 227 * 1024, BARRIER_BYTES = 256;
 
@@ -1176,7 +1181,7 @@ int32_t setup() {      // once per device
   bool ok = configure_tc5_kernels() == 0;
   const cudaError_t e[] = {allow<Pair<D_FWD, false>>(), allow<Pair<D_FWD, true>>(), allow<Pair<D_DX, false>>(), allow<Pair<D_DW, false>>(), allow<Pair<D_DW, true>>(),
                            allow<Single<D_FWD, false>>(), allow<Single<D_FWD, true>>(), allow<Single<D_DX, false>>(), allow<Single<D_DW, false>>(), allow<Single<D_DW, true>>(),
-                           allow<Thin<D_FWD>>(), allow<Thin<D_DX>>(), allow<Thin<D_DW>>(), allow<Split<D_FWD>>(), allow<Split<D_DX>>(), allow<Split<D_DW>>(),
+                           allow<Thin<D_FWD>>(), allow<Thin<D_DW>>(), allow<Split<D_FWD>>(), allow<Split<D_DX>>(), allow<Split<D_DW>>(),
                            allow<Few<D_FWD, 16>>(), allow<Few<D_FWD, 32>>(), allow<Few<D_FWD, 64>>(), allow<Few<D_DX, 16>>(), allow<Few<D_DX, 32>>(), allow<Few<D_DX, 64>>()};
   for (cudaError_t x : e) ok = ok && x == cudaSuccess;
   if (!ok) return fail(PS_ERR_CUDA, "kernel configuration failed: %s", cudaGetErrorString(cudaGetLastError()));
@@ -1276,13 +1281,14 @@ int32_t run_rows(Problem& p, int features, int red, bool fp32_out) {
     if (bn == 32) return launch<Few<OP, 32>>(p, split);
     return launch<Few<OP, 64>>(p, split);
   }
-  if (red <= THIN_RED && cut_rows(tab, BM, false) * div_up(features, 128) > sms) {
+  if constexpr (OP == D_FWD) {
     a.n_tiles_n = div_up(features, 128);
-    const int64_t t = cut_rows(tab, BM, false) * a.n_tiles_n;
-    if (t >= 1 << 30) return fail(PS_ERR_BAD_ARG, "too many tiles");
-    a.m_tiles = (int)(t / a.n_tiles_n);
-    a.n_tiles = (int)t;
-    return launch<Thin<OP>>(p, 1);
+    const int64_t row_blocks = cut_rows(tab, BM, false), t = row_blocks * a.n_tiles_n;
+    if (red <= THIN_RED_FWD && t > sms && t < 1 << 30) {
+      a.m_tiles = (int)row_blocks;
+      a.n_tiles = (int)t;
+      return launch<Thin<OP>>(p, 1);
+    }
   }
   a.n_tiles_n = div_up(features, 256);
   const int64_t row_blocks = cut_rows(tab, BM, false), pairs = cut_rows(tab, BM, true), singles = row_blocks * a.n_tiles_n;
@@ -1314,7 +1320,7 @@ int32_t run_weights(Problem& p, int N, int K, bool fp32_out) {
   a.m_side = N; a.n_side = K; a.red = 0;
   auto tiles = [&](int tm) { a.m_tiles = div_up(N, tm); return (int64_t)tab.groups * a.m_tiles * a.n_tiles_n; };
   a.n_tiles_n = div_up(K, 128);
-  if (most <= THIN_RED && tiles(128) > sms && tiles(128) < 1 << 30) {
+  if (most <= THIN_RED_DW && tiles(128) > sms && tiles(128) < 1 << 30) {
     a.n_tiles = (int)tiles(128);
     return launch<Thin<D_DW>>(p, 1);
   }
