@@ -591,13 +591,22 @@ __device__ __forceinline__ int find_start(const int32_t* start, int n, int at) {
   return lo;
 }
 
+// Tile t of m_tiles x n_tiles: bands of eight along the left side, so that tiles under way together share operands in L2.
+__device__ __forceinline__ void in_bands(int t, int m_tiles, int n_tiles, int& m, int& n) {
+  const int per = 8 * n_tiles, band = t / per, in = min(8, m_tiles - 8 * band), l = t - band * per;
+  m = 8 * band + l % in;
+  n = l / in;
+}
+
 template <class S>
 __device__ __forceinline__ void decode_tile(const DenseArgs& a, const DenseTab& tab, int t, int rank, DenseTile& c) {
   if (S::OP == D_DW) {
     const int per = a.m_tiles * a.n_tiles_n, g = t / per, l = t - g * per;
     c.w = g;
-    c.m0 = (l % a.m_tiles) * S::TM + rank * BM; c.m_end = a.m_side;
-    c.n0 = (l / a.m_tiles) * S::BN; c.n_end = a.n_side;
+    int m, n;
+    in_bands(l, a.m_tiles, a.n_tiles_n, m, n);
+    c.m0 = m * S::TM + rank * BM; c.m_end = a.m_side;
+    c.n0 = n * S::BN; c.n_end = a.n_side;
     c.red0 = tab.row0[g]; c.red = tab.row1[g] - c.red0;
     return;
   }
@@ -610,9 +619,9 @@ __device__ __forceinline__ void decode_tile(const DenseArgs& a, const DenseTab& 
     c.n0 = tab.row0[g] + (blk - tab.blk0[g]) * S::BN; c.n_end = tab.row1[g];
     return;
   }
-  // bands of eight (pairs of) blocks, so that tiles under way together share operands in L2
-  const int per = 8 * a.n_tiles_n, band = t / per, in = min(8, a.m_tiles - 8 * band), l = t - band * per, m = 8 * band + l % in;
-  c.n0 = (l / in) * S::BN; c.n_end = a.n_side;
+  int m, n;
+  in_bands(t, a.m_tiles, a.n_tiles_n, m, n);
+  c.n0 = n * S::BN; c.n_end = a.n_side;
   int blk = m;
   if (S::CTAS == 2) {
     const int r = find_start(tab.run_pair0, tab.runs, m);
