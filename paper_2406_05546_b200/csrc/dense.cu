@@ -72,6 +72,9 @@ template <int OP_, int CTAS_, int BN_, int STAGES_, bool SPLIT_, bool FEW_, bool
   static constexpr int A_BYTES = BM * BK * 2, B_BYTES = B_ROWS * BK * 2, STAGE = A_BYTES + B_BYTES;
   static constexpr int BUFS = SPLIT ? 1 : 2, ACC = BN < 32 ? 32 : BN;
   static constexpr int EPI_WARPS = FEW ? 4 : 8, THREADS = 64 + 32 * EPI_WARPS, COLS = BN / (EPI_WARPS / 4);
+  // May pieces of rows change lanes?  Not where there are no registers left for it: the sums of a drained accumulator (weight gradient in FP32, 16,384 x
+  // 4096 x 4096 457 -> 641 us), two CTAs on an SM (forward, 8,192 x 64 -> 4096 with everything on 64 -> 91).
+  static constexpr bool TURN = !DRAIN && PER_SM == 1;
   static constexpr int OUT_BYTES = SPLIT ? 0 : EPI_WARPS * 4096;      // a 32 x 32 block per warp on its way to whole rows
   static constexpr int SMEM = 1024 + STAGES * STAGE + OUT_BYTES + BARRIER_BYTES;
   static constexpr int PART_PITCH = FEW ? BM + 4 : BN + 4, PART_BYTES = (FEW ? BN : BM) * PART_PITCH * 4;
@@ -241,59 +244,134 @@ template <int OP> __device__ __forceinline__ int64_t out0_at(const DenseEpi& e, 
   return (OP == D_DW ? (int64_t)which * e.out0_stride : 0) + row * e.out0_pitch + col;
 }
 
-// Rows: a lane has 32 consecutive columns of a row of its own, whose pieces of 32 or 16 bytes it loads and stores straight from and to global memory:
-// no exchange between lanes.  What is read is loaded a chunk ahead.
+// Rows: a lane has 32 consecutive columns of a row of its own.  Where 32 bytes can be moved at once it loads and stores them straight from and to
+// global memory.  Where only 16 can, a lane alone would write half sectors, and the rest of each in another access: there four lanes
+// move 64 consecutive bytes of a row, and pieces of 16 bytes change lanes in shared memory (11,776 x 2048 -> 5000 with everything on 284 -> 236 us).
+// What is read is loaded a chunk ahead.
 template <int OP> struct RowIn { uint32_t a[OP == D_DW ? 1 : 16], b[OP == D_DX ? 16 : 1]; };
-__device__ __forceinline__ void load_row(const void* base, int64_t at, int wide, uint32_t (&w)[16]) {      // 32 values of 16 bits
-  const uint16_t* p = reinterpret_cast<const uint16_t*>(base) + at;
+// TURN: may pieces change lanes?  Then every lane of the warp comes along, and the existence of its rows is asked where they are moved; if not, only
+// lanes with a row come at all.
+template <bool TURN> struct RowPlace {
+  int row0, end, lane;      // the warp's first row; the rows' end
+  uint8_t* turn;            // 2 KB of shared memory
+  __device__ __forceinline__ int row() const { return row0 + lane; }
+  __device__ __forceinline__ int piece_row(int i) const { return row0 + 8 * i + (lane >> 2); }      // of a lane's piece i, where four lanes share a row
+};
+__device__ __forceinline__ uint4* turn_at(const RowPlace<true>& p, int row, int piece) {      // without conflicts, by rows and by pieces
+  return reinterpret_cast<uint4*>(p.turn + row * 64 + ((piece ^ ((row >> 1) & 3)) << 4));
+}
+// 64 bytes of a row per lane -> pieces, and back
+__device__ __forceinline__ void to_pieces(const RowPlace<true>& p, uint32_t* w) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) *turn_at(p, p.lane, i) = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint4 v = *turn_at(p, 8 * i + (p.lane >> 2), p.lane & 3);
+    w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+  }
+  __syncwarp();
+}
+__device__ __forceinline__ void to_rows(const RowPlace<true>& p, uint32_t* w) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) *turn_at(p, 8 * i + (p.lane >> 2), p.lane & 3) = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint4 v = *turn_at(p, p.lane, i);
+    w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+  }
+  __syncwarp();
+}
+template <bool TURN> __device__ __forceinline__ void loaded(const RowPlace<TURN>& p, int wide, uint32_t* w) {
+  if constexpr (TURN)
+    if (!wide) to_rows(p, w);
+}
+// 64 bytes of each row from `base` on, pitch in bytes; as pieces where not wide.
+template <bool TURN>
+__device__ __forceinline__ void load_row(const void* base, int64_t pitch, const RowPlace<TURN>& p, int wide, uint32_t (&w)[16]) {
+  const uint8_t* b = reinterpret_cast<const uint8_t*>(base);
   if (wide) {
-    load_words(p, *reinterpret_cast<uint32_t (*)[8]>(&w[0]));
-    load_words(p + 16, *reinterpret_cast<uint32_t (*)[8]>(&w[8]));
-  } else {
+    if (!TURN || p.row() < p.end) {
+      load_words(b + p.row() * pitch, *reinterpret_cast<uint32_t (*)[8]>(&w[0]));
+      load_words(b + p.row() * pitch + 32, *reinterpret_cast<uint32_t (*)[8]>(&w[8]));
+    }
+  } else if (!TURN) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const uint4 v = reinterpret_cast<const uint4*>(p)[i];
+      const uint4 v = *reinterpret_cast<const uint4*>(b + p.row() * pitch + 16 * i);
       w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
     }
-  }
-}
-template <int WORDS>
-__device__ __forceinline__ void store_row(void* p, int wide, const uint32_t (&w)[WORDS]) {
-  if (wide) {
-#pragma unroll
-    for (int i = 0; i < WORDS / 8; ++i) store_words(reinterpret_cast<uint8_t*>(p) + 32 * i, w + 8 * i);
   } else {
 #pragma unroll
-    for (int i = 0; i < WORDS / 4; ++i) reinterpret_cast<uint4*>(p)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+    for (int i = 0; i < 4; ++i)
+      if (p.piece_row(i) < p.end) {
+        const uint4 v = *reinterpret_cast<const uint4*>(b + p.piece_row(i) * pitch + 16 * (p.lane & 3));
+        w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+      }
   }
 }
-template <bool BF16>
-__device__ __forceinline__ void store_row16(void* base, int64_t at, int wide, const u64 (&v)[16]) {
+template <bool TURN>
+__device__ __forceinline__ void store_row(void* base, int64_t pitch, const RowPlace<TURN>& p, int wide, uint32_t* w) {
+  uint8_t* b = reinterpret_cast<uint8_t*>(base);
+  if (wide) {
+    if (!TURN || p.row() < p.end) {
+      store_words(b + p.row() * pitch, w);
+      store_words(b + p.row() * pitch + 32, w + 8);
+    }
+  } else if constexpr (!TURN) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(b + p.row() * pitch + 16 * i) = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+  } else {
+    to_pieces(p, w);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (p.piece_row(i) < p.end) *reinterpret_cast<uint4*>(b + p.piece_row(i) * pitch + 16 * (p.lane & 3)) = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+  }
+}
+template <bool BF16, bool TURN>
+__device__ __forceinline__ void store_row16(void* base, int64_t pitch, const RowPlace<TURN>& p, int col, int wide, const u64 (&v)[16]) {
   uint32_t w[16];
 #pragma unroll
   for (int i = 0; i < 16; ++i) w[i] = narrow_pair<BF16>(v[i]);
-  store_row(reinterpret_cast<uint16_t*>(base) + at, wide, w);
+  store_row(reinterpret_cast<uint16_t*>(base) + col, 2 * pitch, p, wide, w);
 }
-__device__ __forceinline__ void store_row32(void* base, int64_t at, int wide, const u64 (&v)[16]) {
-  uint32_t w[32];
+// add: to what is there
+template <bool TURN>
+__device__ __forceinline__ void store_row32(void* base, int64_t pitch, const RowPlace<TURN>& p, int col, int wide, int add, u64 (&v)[16]) {
+  float* at = reinterpret_cast<float*>(base) + col;
+  if (add) {
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    w[2 * i] = (uint32_t)v[i];
-    w[2 * i + 1] = (uint32_t)(v[i] >> 32);
+    for (int h = 0; h < 2; ++h) {
+      uint32_t o[16];
+      load_row(at + 16 * h, 4 * pitch, p, wide, o);
+      loaded(p, wide, o);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[8 * h + i] = add2(v[8 * h + i], pack2(__uint_as_float(o[2 * i]), __uint_as_float(o[2 * i + 1])));
+    }
   }
-  store_row(reinterpret_cast<float*>(base) + at, wide, w);
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    uint32_t w[16];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      w[2 * i] = (uint32_t)v[8 * h + i];
+      w[2 * i + 1] = (uint32_t)(v[8 * h + i] >> 32);
+    }
+    store_row(at + 16 * h, 4 * pitch, p, wide, w);
+  }
 }
-template <int OP>
-__device__ __forceinline__ void row_ahead(const DenseEpi& e, int64_t row, int col, RowIn<OP>& x) {
+template <int OP, bool TURN>
+__device__ __forceinline__ void row_ahead(const DenseEpi& e, const RowPlace<TURN>& p, int col, RowIn<OP>& x) {
   if constexpr (OP != D_DW) {
-    if (e.in1) load_row(e.in1, row * e.in1_pitch + col, e.wide, x.a);
+    if (e.in1) load_row(reinterpret_cast<const uint16_t*>(e.in1) + col, 2 * e.in1_pitch, p, e.wide, x.a);
     if constexpr (OP == D_DX)
-      if (e.out1) load_row(e.in2, row * e.in2_pitch + col, e.wide, x.b);
+      if (e.out1) load_row(reinterpret_cast<const uint16_t*>(e.in2) + col, 2 * e.in2_pitch, p, e.wide, x.b);
   }
 }
 // bias: 32 floats in shared memory
-template <int OP, bool BF16>
-__device__ __forceinline__ void finish_row_of(const DenseEpi& e, int64_t row, int col, int which, const float* bias, const RowIn<OP>& x, u64 (&v)[16]) {
+template <int OP, bool BF16, bool TURN>
+__device__ __forceinline__ void finish_row_of(const DenseEpi& e, const RowPlace<TURN>& p, int col, int which, const float* bias, RowIn<OP>& x, u64 (&v)[16]) {
   if constexpr (OP == D_FWD) {
     if (e.in0) {
 #pragma unroll
@@ -303,7 +381,7 @@ __device__ __forceinline__ void finish_row_of(const DenseEpi& e, int64_t row, in
         v[2 * i + 1] = add2(v[2 * i + 1], pack2(b.z, b.w));
       }
     }
-    if (e.out1) store_row16<BF16>(e.out1, row * e.out1_pitch + col, e.wide, v);
+    if (e.out1) store_row16<BF16>(e.out1, e.out1_pitch, p, col, e.wide, v);
     with_activation(e.act, [&](auto act) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) v[i] = activate2<decltype(act)::value>(v[i]);
@@ -311,50 +389,46 @@ __device__ __forceinline__ void finish_row_of(const DenseEpi& e, int64_t row, in
   }
   if constexpr (OP != D_DW) {
     if (e.in1) {
+      loaded(p, e.wide, x.a);
 #pragma unroll
       for (int i = 0; i < 16; ++i) v[i] = add2(v[i], widen2<BF16>(x.a[i]));
     }
   }
   if constexpr (OP == D_FWD) {
-    if (e.out0_fp32) store_row32(e.out0, row * e.out0_pitch + col, e.wide, v);
-    else store_row16<BF16>(e.out0, row * e.out0_pitch + col, e.wide, v);
+    if (e.out0_fp32) store_row32(e.out0, e.out0_pitch, p, col, e.wide, 0, v);
+    else store_row16<BF16>(e.out0, e.out0_pitch, p, col, e.wide, v);
   } else if constexpr (OP == D_DX) {
-    if (e.out0) store_row16<BF16>(e.out0, row * e.out0_pitch + col, e.wide, v);
+    if (e.out0) store_row16<BF16>(e.out0, e.out0_pitch, p, col, e.wide, v);
     if (e.out1) {
+      loaded(p, e.wide, x.b);
       with_activation(e.act, [&](auto act) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) v[i] = through2<decltype(act)::value>(v[i], widen2<BF16>(x.b[i]));
       });
-      store_row16<BF16>(e.out1, row * e.out1_pitch + col, e.wide, v);
+      store_row16<BF16>(e.out1, e.out1_pitch, p, col, e.wide, v);
     }
   } else {
-    const int64_t at = out0_at<OP>(e, row, col, which);
+    const int64_t first = (int64_t)which * e.out0_stride;
     if (e.out0_fp32) {
-      if (e.accumulate) {
-        const float4* p = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(e.out0) + at);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float4 o = p[i];
-          v[2 * i] = add2(v[2 * i], pack2(o.x, o.y));
-          v[2 * i + 1] = add2(v[2 * i + 1], pack2(o.z, o.w));
-        }
-      }
-      store_row32(e.out0, at, e.wide, v);
+      float* out = reinterpret_cast<float*>(e.out0) + first;
+      store_row32(out, e.out0_pitch, p, col, e.wide, e.accumulate, v);
     } else {
+      uint16_t* out = reinterpret_cast<uint16_t*>(e.out0) + first;
       if (e.accumulate) {
         uint32_t o[16];
-        load_row(e.out0, at, e.wide, o);
+        load_row(out + col, 2 * e.out0_pitch, p, e.wide, o);
+        loaded(p, e.wide, o);
 #pragma unroll
         for (int i = 0; i < 16; ++i) v[i] = add2(v[i], widen2<BF16>(o[i]));
       }
-      store_row16<BF16>(e.out0, at, e.wide, v);
+      store_row16<BF16>(out, e.out0_pitch, p, col, e.wide, v);
     }
   }
 }
 
-template <int OP>
-__device__ __forceinline__ void finish_row(const DenseEpi& e, int64_t row, int col, int which, const float* bias, const RowIn<OP>& x, u64 (&v)[16]) {
-  with_type(e.bf16, [&](auto bf16) { finish_row_of<OP, decltype(bf16)::value>(e, row, col, which, bias, x, v); });
+template <int OP, bool TURN>
+__device__ __forceinline__ void finish_row(const DenseEpi& e, const RowPlace<TURN>& p, int col, int which, const float* bias, RowIn<OP>& x, u64 (&v)[16]) {
+  with_type(e.bf16, [&](auto bf16) { finish_row_of<OP, decltype(bf16)::value, TURN>(e, p, col, which, bias, x, v); });
 }
 
 // Columns, for matrices of any alignment and at their right edge: a lane has W = 1, 2 or 4 consecutive columns of R rows, row0 + i * step, of which
@@ -827,9 +901,9 @@ __global__ void __launch_bounds__(S::THREADS, S::PER_SM) dense_gemm(const __grid
       int b0, b1;
       block_range(blocks_of(c.red), b0, b1);
       const int m_base = c.m0 + quarter * 32;
-      // a warp's 4 KB of shared memory: the bias of its columns, or a 32 x 32 block on its way from rows to columns
+      // a warp's 4 KB of shared memory: the bias of its columns and 2 KB where pieces of rows change lanes, or a 32 x 32 block on its way from rows to columns
       float* stage = reinterpret_cast<float*>(out_stage + (warp - 2) * 4096);
-      const int m = m_base + lane;
+      const RowPlace<S::TURN> place{m_base, c.m_end, lane, reinterpret_cast<uint8_t*>(stage) + 2048};
       auto by_rows = [&](int j0) { return epi.rows && c.n_end - (c.n0 + col0 + j0) >= 32; };
       if (S::OP == D_FWD && !S::SPLIT && epi.in0 && by_rows(0)) {
         __syncwarp();
@@ -841,12 +915,12 @@ __global__ void __launch_bounds__(S::THREADS, S::PER_SM) dense_gemm(const __grid
         __syncwarp();
       }
       auto read_ahead = [&](RowIn<S::OP>& x, int j0) {
-        if (by_rows(j0) && m < c.m_end) row_ahead<S::OP>(epi, m, c.n0 + col0 + j0, x);
+        if (by_rows(j0) && (S::TURN || place.row() < place.end)) row_ahead<S::OP>(epi, place, c.n0 + col0 + j0, x);
       };
-      auto write_out = [&](u64 (&v)[16], int j0, const RowIn<S::OP>& x) {
+      auto write_out = [&](u64 (&v)[16], int j0, RowIn<S::OP>& x) {
         const int col = c.n0 + col0 + j0;
         if (by_rows(j0)) {
-          if (m < c.m_end) finish_row<S::OP>(epi, m, col, c.w, stage + j0, x, v);
+          if (S::TURN || place.row() < place.end) finish_row<S::OP>(epi, place, col, c.w, stage + j0, x, v);
         } else if (col < c.n_end) {
           // W columns of every 32 / W lanes, rows W at a time side by side; everything is loaded before the block is turned round
           auto columns = [&](auto width) {
@@ -1299,10 +1373,12 @@ int32_t run_rows(Problem& p, int features, int red, bool fp32_out) {
     if (bn == 32) return launch<Few<OP, 32>>(p, split);
     return launch<Few<OP, 64>>(p, split);
   }
+  // Thin tiles lack the registers to turn pieces of 16 bytes: such rows go to the others (us, 8,192 x 200 -> 5000 with pre: Thin 124, Pair 81; with everything
+  // 142, 114); rows that go by columns stay (8,192 x 200 -> 4999 with everything: Thin 118, Pair 163).
   if constexpr (OP == D_FWD) {
     a.n_tiles_n = div_up(features, 128);
     const int64_t row_blocks = cut_rows(tab, BM, false), t = row_blocks * a.n_tiles_n;
-    if (red <= THIN_RED_FWD && t > sms && t < 1 << 30) {
+    if (red <= THIN_RED_FWD && (p.epi.wide || !p.epi.rows) && t > sms && t < 1 << 30) {
       a.m_tiles = (int)row_blocks;
       a.n_tiles = (int)t;
       return launch<Thin<OP>>(p, 1);

@@ -214,6 +214,19 @@ def test_backward_odd_sizes_and_pitches(shape, pad, accumulate):
     one_backward(shape, "bf16", "gelu", True, True, True, bool(accumulate), accumulate, pad=pad, extra=3)
 
 
+# rows that start on 16 bytes but not on 32 (pad 0), and on 32 (pad 8), of every persistent tile shape
+@gpu
+@pytest.mark.parametrize("shape", [([1300, 77, 0, 513, 1, 900], 6, None, 520, 1032), ([2701, 2299], 2, None, 776, 1032), ([1111, 1500], 2, None, 200, 2568)],
+                         ids=lambda s: f"{len(s[0])}x{sum(s[0])}-{s[3]}-{s[4]}")
+@pytest.mark.parametrize("pad", [0, 8])
+@pytest.mark.parametrize("kind,wide_results", [("bf16", False), ("fp16", True)])
+def test_rows_on_sixteen_and_on_thirty_two_bytes(shape, pad, kind, wide_results):
+    one_forward(shape, kind, "gelu", True, True, True, wide_results, pad=(pad,) * 4, extra=3)
+    one_forward(shape, kind, "relu", False, False, True, wide_results, pad=(pad,) * 4)
+    for accumulate in (0, 1):
+        one_backward(shape, kind, "silu", True, True, True, wide_results, accumulate, pad=(pad,) * 4, extra=3)
+
+
 @gpu
 @pytest.mark.parametrize("rows", [[70, 5, 0, 33, 200], [1000, 1, 77]])
 @pytest.mark.parametrize("N,K", [(136, 200), (2048, 2304)])
