@@ -57,9 +57,11 @@ enum { D_FWD = 0, D_DX = 1, D_DW = 2 };
 constexpr int BM = 128, BK = 64;
 // Reductions up to this length are bound by what they write: Thin tiles.  us, Pair or Single -> Thin: forward, 8,192 rows -> 4096 with residual and GELU, K =
 // 64 53 -> 44, 256 57 -> 52, 384 61 -> 57, 512 65 -> 64, 768 72 -> 76; weight gradient, 16 workers of 1568 x 512 in FP32, 64 rows each 16.6 -> 13.2,
-// 300 20.6 -> 19.5, 500 24.7 -> 26.3, 8 workers of 2048 x 2048, 300 rows 30 -> 33.  The input gradient, which reads two matrices more, has not the
+// 300 20.6 -> 19.5, 500 24.7 -> 26.3, 8 workers of 2048 x 2048, 300 rows 30 -> 33;
+// a few larger workers among small ones (16 workers, 290 rows the most of 1,024: 23.6 -> 21.5, 480 of 930: 25.6 -> 23.6; 600 of 1,340: no gain; half with
+// 400, half with 100: 27.7 -> 31.7).  The input gradient, which reads two matrices more, has not the
 // registers for it (64 -> 117).
-constexpr int THIN_RED_FWD = 384, THIN_RED_DW = 256;
+constexpr int THIN_RED_FWD = 384, THIN_RED_DW = 256, THIN_MOST_DW = 512, THIN_MEAN_DW = 128;
 constexpr int DRAIN_BLOCKS = 8;      // blocks of k whose sums share an accumulator where the result is FP32
 constexpr int SMEM_MOST = 227 * 1024, BARRIER_BYTES = 256;
 
@@ -85,6 +87,7 @@ template <int OP_, int CTAS_, int BN_, int STAGES_, bool SPLIT_, bool FEW_, bool
 template <int OP, bool DRAIN> using Pair = DenseShape<OP, 2, 256, 6, false, false, DRAIN>;
 template <int OP, bool DRAIN> using Single = DenseShape<OP, 1, 256, 4, false, false, DRAIN>;
 template <int OP> using Thin = DenseShape<OP, 1, 128, 2, false, false, false, 2>;
+static_assert(THIN_RED_FWD <= DRAIN_BLOCKS * BK && THIN_MOST_DW <= DRAIN_BLOCKS * BK, "Thin tiles do not drain their accumulators");
 template <int OP> using Split = DenseShape<OP, 1, 128, 6, true, false, true>;
 template <int OP, int BN> using Few = DenseShape<OP, 1, BN, BN == 64 ? 4 : 5, true, true, true>;
 
@@ -1408,13 +1411,18 @@ int32_t run_weights(Problem& p, int N, int K, bool fp32_out) {
   DenseTab& tab = p.tab;
   DenseArgs& a = p.args;
   int most = 0;
-  for (int g = 0; g < tab.groups; ++g) most = std::max(most, tab.row1[g] - tab.row0[g]);
+  int64_t rows = 0;
+  for (int g = 0; g < tab.groups; ++g) {
+    most = std::max(most, tab.row1[g] - tab.row0[g]);
+    rows += tab.row1[g] - tab.row0[g];
+  }
+  const bool few = most <= THIN_RED_DW || (most <= THIN_MOST_DW && rows <= (int64_t)THIN_MEAN_DW * tab.groups);
   fp32_out = fp32_out && most > DRAIN_BLOCKS * BK;
   const int sms = g_sm_count;
   a.m_side = N; a.n_side = K; a.red = 0;
   auto tiles = [&](int tm) { a.m_tiles = div_up(N, tm); return (int64_t)tab.groups * a.m_tiles * a.n_tiles_n; };
   a.n_tiles_n = div_up(K, 128);
-  if (most <= THIN_RED_DW && tiles(128) > sms && tiles(128) < 1 << 30) {
+  if (few && tiles(128) > sms && tiles(128) < 1 << 30) {
     a.n_tiles = (int)tiles(128);
     return launch<Thin<D_DW>>(p, 1);
   }
