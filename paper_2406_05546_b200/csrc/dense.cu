@@ -110,6 +110,14 @@ struct DenseEpi {
   int32_t pairs, quads, rows, wide;      // may two values, four, 16 bytes, 32 bytes be moved at once, in every matrix there is?
 };
 
+// The kernels of one backward call read nothing of one another's.  The first enters as every kernel does (pdl_enter); the others need not wait for it,
+// whose entry says that all work before the call is done: they start when it has started, and wait for the one before them where they
+// have brought in all they will, so that what follows the call, which waits for its last kernel only, finds all of them done.  A kernel starts only when every
+// CTA of the one before it has its SM, shared memory and tensor memory: none waits for a CTA that has no place.
+// us a call in a row, db, dx and dw one after another -> so: 16 ragged workers of 1,024 rows 1568 -> 512 33.5 -> 27, 4,096 x 1024 x 1024 43 -> 36, x 2048 x
+// 2048 75 -> 66, 16,384 x 4096 x 4096 970 -> 965.
+enum { JOIN_FIRST = 0, JOIN_BETWEEN = 1, JOIN_LAST = 2 };
+
 struct DenseArgs {
   int32_t n_tiles, m_tiles, n_side, n_tiles_n;      // tiles; along the left side; length and tiles of the right side (Few: of the left)
   int32_t m_side;                                   // weight gradient: length of the left side
@@ -117,6 +125,7 @@ struct DenseArgs {
   int32_t rows;                                     // of all groups
   int32_t chunk;                                    // blocks of k per accumulator
   uint32_t idesc;
+  int32_t join;                                     // JOIN_*
 };
 
 // Set when a wait gives up, until workers_dense_status reads it: these entry points have no context to keep it in.
@@ -579,6 +588,10 @@ __device__ __forceinline__ void load_bias(const DenseEpi& e, int col, int which,
   }
 }
 
+// pdl_enter's two halves (JOIN_*).
+__device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void pdl_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 // ---- pairs of CTAs ---------------------------------------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t cluster_rank() {
   uint32_t r;
@@ -764,7 +777,8 @@ __global__ void __launch_bounds__(S::THREADS, S::PER_SM) dense_gemm(const __grid
   if (PAIR) cg::this_cluster().sync();
   tc_fence_after();
   const uint32_t tmem = warp_uniform(*tmem_slot);
-  pdl_enter();
+  if (a.join == JOIN_FIRST) pdl_enter();
+  else if (a.join == JOIN_BETWEEN) pdl_next();
 
   // this CTA's blocks of k of a tile with `n` of them
   auto block_range = [&](int n, int& b0, int& b1) {
@@ -820,6 +834,8 @@ __global__ void __launch_bounds__(S::THREADS, S::PER_SM) dense_gemm(const __grid
         if (++s == STAGES) { s = 0; ++use; }
       }
     }
+    if (a.join != JOIN_FIRST) pdl_wait();
+    if (a.join == JOIN_LAST) pdl_next();
   } else if (warp == 1) {
     // ---------------- MMA (a pair's: by its first CTA; the second's warp cleans up its own ragged blocks)
     // zeroes k rows [valid, next multiple of sixteen) of a stage whose operands both have k as their rows
@@ -1665,6 +1681,7 @@ int32_t workers_dense_backward(const ps_dense_layer* l, const ps_dense_gradients
     e.out1 = o->dx_pre; e.out1_pitch = o->dx_pre_pitch;
     e.act = l->activation; e.bf16 = l->type == PS_TYPE_BF16;
     set_moves(e, K, {{o->dx_add, o->dx_add_pitch, 0, 2}, {o->dx_pre ? o->x_pre : nullptr, o->x_pre_pitch, 0, 2}, {o->dx, o->dx_pitch, 0, 2}, {o->dx_pre, o->dx_pre_pitch, 0, 2}});
+    p.args.join = !o->db ? JOIN_FIRST : (o->dw ? JOIN_BETWEEN : JOIN_LAST);
     if ((rc = run_rows<D_DX>(p, K, N, false)) != PS_OK) return rc;
   }
   if (o->dw) {
@@ -1677,6 +1694,7 @@ int32_t workers_dense_backward(const ps_dense_layer* l, const ps_dense_gradients
     e.out0 = o->dw; e.out0_pitch = o->dw_pitch; e.out0_stride = o->dw_stride; e.out0_fp32 = ds == 4; e.accumulate = o->accumulate;
     e.bf16 = l->type == PS_TYPE_BF16;
     set_moves(e, K, {{o->dw, o->dw_pitch, l->groups > 1 ? o->dw_stride : 0, ds}});
+    p.args.join = o->db || o->dx || o->dx_pre ? JOIN_LAST : JOIN_FIRST;
     if ((rc = run_weights(p, N, K, ds == 4)) != PS_OK) return rc;
   }
   return PS_OK;

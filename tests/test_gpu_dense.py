@@ -311,6 +311,50 @@ def test_captured_replayed_and_on_two_streams(shape):
     del graph
 
 
+# The kernels of a backward call run beside one another: what follows the call must find all of them done, and what came before it too.
+@gpu
+@pytest.mark.parametrize("rows,K,N", [([9, 290, 95, 0, 57, 127], 1568, 512), ([3, 1, 7], 520, 1032), ([4000], 512, 768), ([64] * 12, 264, 520), ([700, 300], 251, 333)],
+                         ids=lambda v: str(v) if isinstance(v, int) else f"{len(v)}x{sum(v)}")
+@pytest.mark.parametrize("parts", ["db dx dw", "dx dw", "db dw", "db dx"])
+def test_nothing_before_or_after_a_backward_call_meets_it(rows, K, N, parts):
+    M, G = sum(rows), len(rows)
+    gen = torch.Generator("cuda").manual_seed(7)
+    x0 = torch.randn(M, K, generator=gen, device="cuda").bfloat16()
+    dy0 = torch.randn(M, N, generator=gen, device="cuda").bfloat16()
+    w = torch.randn(G, N, K, generator=gen, device="cuda").bfloat16()
+    x, dy = torch.empty_like(x0), torch.empty_like(dy0)
+    out = {"dx": torch.empty_like(x), "dw": torch.empty(G, N, K, device="cuda"), "db": torch.empty(G, N, device="cuda")}
+    out = {k: v for k, v in out.items() if k in parts.split()}
+    x.copy_(x0)
+    dy.copy_(dy0)
+    workers_dense_backward(dy, x, w, rows, **out)
+    torch.cuda.synchronize()
+    want = {k: v.clone() for k, v in out.items()}
+    for _ in range(10):
+        for v in (x, dy, *out.values()):
+            v.fill_(77)
+        x.copy_(x0)
+        dy.copy_(dy0)
+        workers_dense_backward(dy, x, w, rows, **out)
+        x.fill_(math.nan)
+        dy.fill_(math.nan)
+        got = {k: v.clone() for k, v in out.items()}
+        workers_dense_status()
+        assert all(torch.equal(got[k], want[k]) for k in want)
+    # and the next call reads what this one has written
+    if "dx" in out:
+        x.copy_(x0)
+        dy.copy_(dy0)
+        y, v = torch.empty(M, N, device="cuda", dtype=torch.bfloat16), torch.empty(M, N, device="cuda", dtype=torch.bfloat16)
+        for _ in range(5):
+            out["dx"].zero_()
+            workers_dense_backward(dy, x, w, rows, **out)
+            workers_dense_forward(out["dx"], w, rows, y=y)
+        workers_dense_forward(want["dx"], w, rows, y=v)
+        workers_dense_status()
+        assert torch.equal(y, v)
+
+
 @gpu
 def test_gradients_against_differences():
     """d/dt of sum(c * y(t)) along random directions of x, W and b, y from the forward call in FP32: the differences' error is that of the values
