@@ -502,6 +502,10 @@ typedef struct {
  * No output may overlap an input, but for dx and dx_add.  Errors as workers_dense_forward. */
 int32_t workers_dense_backward(const ps_dense_layer* layer, const ps_dense_gradients* out);
 
+/* workers_dense_backward whose products give up a wait after limit_cycles (1..2e9; 2e9, about a second, in every other call): shows that no wait
+ * grows with the work of a call. */
+int32_t workers_dense_selftest_backward(const ps_dense_layer* layer, const ps_dense_gradients* out, int64_t limit_cycles);
+
 /* Workspace bytes of a call with these operands; dy NULL: of the forward call. */
 int32_t workers_dense_workspace(const ps_dense_layer* layer, const void* dy, int64_t dy_pitch, uint64_t* bytes);
 

@@ -126,6 +126,7 @@ struct DenseArgs {
   int32_t chunk;                                    // blocks of k per accumulator
   uint32_t idesc;
   int32_t join;                                     // JOIN_*
+  int64_t limit;                                    // clocks that a wait may last
 };
 
 // Set when a wait gives up, until workers_dense_status reads it: these entry points have no context to keep it in.
@@ -617,14 +618,32 @@ __device__ __forceinline__ bool cluster_try(uint32_t addr, uint32_t parity) {
   return done != 0;
 }
 // The bounded wait of a whole warp for arrivals from both CTAs.
-__device__ __forceinline__ bool pair_wait(uint64_t* bar, uint32_t parity, const volatile uint32_t* abort_flag) {
+__device__ __forceinline__ bool pair_wait(uint64_t* bar, uint32_t parity, const volatile uint32_t* abort_flag, long long limit) {
   const uint32_t addr = smem_u32(bar);
   bool done = cluster_try(addr, parity);
   if (!done) {
     const long long t0 = clock64();
     do {
       done = cluster_try(addr, parity);
-    } while (!done && clock64() - t0 <= WAIT_LIMIT_CYCLES);
+    } while (!done && clock64() - t0 <= limit);
+  }
+  return __all_sync(0xffffffffu, done && !*abort_flag);
+}
+// The wait for a ragged block of a warp that passes over the blocks before it, perhaps a second's worth and more: the limit starts anew whenever the
+// CTA's copying warp, whose own waits are bounded, has brought in another block.
+__device__ __forceinline__ bool tail_wait(uint64_t* bar, uint32_t parity, const volatile uint32_t* abort_flag, const volatile uint32_t* copied, long long limit) {
+  const uint32_t addr = smem_u32(bar);
+  uint32_t seen = *copied;
+  long long t0 = clock64();
+  bool done;
+  while (!(done = mbar_try(addr, parity)) && !*abort_flag) {
+    const uint32_t now = *copied;
+    if (now != seen) {
+      seen = now;
+      t0 = clock64();
+    } else if (clock64() - t0 > limit) {
+      break;
+    }
   }
   return __all_sync(0xffffffffu, done && !*abort_flag);
 }
@@ -754,6 +773,7 @@ __global__ void __launch_bounds__(S::THREADS, S::PER_SM) dense_gemm(const __grid
   uint64_t* tail_ready = tail_full + STAGES; // [STAGES] the second CTA's such warp -> MMA
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(tail_ready + STAGES);
   volatile uint32_t* abort_flag = tmem_slot + 1;
+  volatile uint32_t* copied = tmem_slot + 2;      // blocks that the copying warp has asked for (a pair's second CTA, ragged reductions)
   const int tid = threadIdx.x, warp = warp_uniform(tid >> 5), lane = tid & 31;
   const uint32_t rank = PAIR ? cluster_rank() : 0u;
   const int first_tile = PAIR ? blockIdx.x >> 1 : blockIdx.x, tile_step = S::SPLIT ? a.n_tiles : (PAIR ? gridDim.x >> 1 : gridDim.x);
@@ -761,6 +781,7 @@ __global__ void __launch_bounds__(S::THREADS, S::PER_SM) dense_gemm(const __grid
     for (int s = 0; s < STAGES; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); mbar_init(&tail_full[s], 1); mbar_init(&tail_ready[s], 1); }
     for (int i = 0; i < BUFS; ++i) { mbar_init(&acc_full[i], 1); mbar_init(&acc_empty[i], EPI * S::CTAS); }
     *abort_flag = 0;
+    *copied = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) {
@@ -793,7 +814,7 @@ __global__ void __launch_bounds__(S::THREADS, S::PER_SM) dense_gemm(const __grid
     // ---------------- copies
     const uint32_t full0 = smem_u32(full), full_of_pair = PAIR ? leaders(full) : full0, tail0 = smem_u32(tail_full);
     int s = 0;
-    uint32_t use = 0;
+    uint32_t use = 0, blocks = 0;
     bool ok = true;
     for (int t = first_tile; t < a.n_tiles && ok; t += tile_step) {
       DenseTile c;
@@ -802,7 +823,7 @@ __global__ void __launch_bounds__(S::THREADS, S::PER_SM) dense_gemm(const __grid
       block_range(blocks_of(c.red), b0, b1);
       const int am = c.m0, bn = c.n0 + (int)rank * S::B_ROWS;
       for (int kb = b0; kb < b1; ++kb) {
-        if (use > 0 && !warp_wait(&empty[s], (use - 1) & 1, abort_flag)) { *abort_flag = 1; ok = false; break; }
+        if (use > 0 && !warp_wait(&empty[s], (use - 1) & 1, abort_flag, a.limit)) { *abort_flag = 1; ok = false; break; }
         const uint32_t A = base + s * S::STAGE, B = A + S::A_BYTES;
         const int k0 = kb * BK, r0 = c.red0 + k0;
         auto load = [&](auto remote, uint32_t bar) {
@@ -831,6 +852,7 @@ __global__ void __launch_bounds__(S::THREADS, S::PER_SM) dense_gemm(const __grid
           if (rank == 0) expect_tx_warp(full0 + 8 * s, 2 * S::STAGE);
           load(std::true_type(), full_of_pair + 8 * s);
         }
+        if (PAIR && RAGGED && rank != 0) *copied = ++blocks;
         if (++s == STAGES) { s = 0; ++use; }
       }
     }
@@ -861,7 +883,7 @@ __global__ void __launch_bounds__(S::THREADS, S::PER_SM) dense_gemm(const __grid
       if (PAIR && rank != 0) {
         if (RAGGED && c.red % BK != 0) {
           const int at = (s + b1 - 1) % STAGES;
-          if (!warp_wait(&tail_full[at], (tails >> at) & 1, abort_flag)) { *abort_flag = 1; break; }
+          if (!tail_wait(&tail_full[at], (tails >> at) & 1, abort_flag, copied, a.limit)) { *abort_flag = 1; break; }
           tails ^= 1u << at;
           clean(at, c.red % BK);
           if (lane == 0) arrive_at(leaders(&tail_ready[at]));
@@ -873,14 +895,14 @@ __global__ void __launch_bounds__(S::THREADS, S::PER_SM) dense_gemm(const __grid
         const bool first = (kb - b0) % a.chunk == 0, last = (kb - b0) % a.chunk == a.chunk - 1 || kb + 1 == b1;
         if (first && lead >= BUFS) {
           const uint32_t p = ((lead / BUFS) - 1) & 1;
-          if (!(PAIR ? pair_wait(&acc_empty[lead % BUFS], p, abort_flag) : warp_wait(&acc_empty[lead % BUFS], p, abort_flag))) { *abort_flag = 1; ok = false; break; }
+          if (!(PAIR ? pair_wait(&acc_empty[lead % BUFS], p, abort_flag, a.limit) : warp_wait(&acc_empty[lead % BUFS], p, abort_flag, a.limit))) { *abort_flag = 1; ok = false; break; }
         }
-        if (!(PAIR ? pair_wait(&full[s], parity, abort_flag) : warp_wait(&full[s], parity, abort_flag))) { *abort_flag = 1; ok = false; break; }
+        if (!(PAIR ? pair_wait(&full[s], parity, abort_flag, a.limit) : warp_wait(&full[s], parity, abort_flag, a.limit))) { *abort_flag = 1; ok = false; break; }
         const int valid = min(BK, c.red - kb * BK);
         if (RAGGED && valid < BK) {
-          if (PAIR && !warp_wait(&tail_full[s], (tails >> s) & 1, abort_flag)) { *abort_flag = 1; ok = false; break; }
+          if (PAIR && !warp_wait(&tail_full[s], (tails >> s) & 1, abort_flag, a.limit)) { *abort_flag = 1; ok = false; break; }
           clean(s, valid);
-          if (PAIR && !pair_wait(&tail_ready[s], (tails >> s) & 1, abort_flag)) { *abort_flag = 1; ok = false; break; }
+          if (PAIR && !pair_wait(&tail_ready[s], (tails >> s) & 1, abort_flag, a.limit)) { *abort_flag = 1; ok = false; break; }
           tails ^= 1u << s;
         }
         tc_fence_after();
@@ -987,7 +1009,7 @@ __global__ void __launch_bounds__(S::THREADS, S::PER_SM) dense_gemm(const __grid
         bool ok = true;
         for (int kb = b0; kb < b1; kb += a.chunk) {
           const int buf = lead % BUFS;
-          if (!warp_wait(&acc_full[buf], (lead / BUFS) & 1, abort_flag)) { ok = false; break; }
+          if (!warp_wait(&acc_full[buf], (lead / BUFS) & 1, abort_flag, a.limit)) { ok = false; break; }
           tc_fence_after();
 #pragma unroll
           for (int j0 = 0; j0 < S::COLS; j0 += 32) {
@@ -1030,7 +1052,7 @@ __global__ void __launch_bounds__(S::THREADS, S::PER_SM) dense_gemm(const __grid
         RowIn<S::OP> now, next;
         read_ahead(now, 0);
         if (!empty_sum) {
-          if (!warp_wait(&acc_full[buf], (lead / BUFS) & 1, abort_flag)) { *abort_flag = 1; break; }
+          if (!warp_wait(&acc_full[buf], (lead / BUFS) & 1, abort_flag, a.limit)) { *abort_flag = 1; break; }
           tc_fence_after();
         }
 #pragma unroll 1
@@ -1305,6 +1327,7 @@ struct Problem {
   DenseArgs args;
   DenseEpi epi;
   Operand a, b;          // left and right operand of the plain orientation
+  int64_t limit = WAIT_LIMIT_CYCLES;
   cudaStream_t st;
 };
 
@@ -1314,6 +1337,7 @@ int32_t launch(const Problem& p, int split) {
   const Operand &l = S::FEW ? p.b : p.a, &r = S::FEW ? p.a : p.b;
   if (!operand_map(&maps.a, l, S::A_MN ? 64 : BM) || !operand_map(&maps.b, r, S::B_MN ? 64 : S::B_ROWS)) return fail(PS_ERR_CUDA, "tensor map");
   DenseArgs a = p.args;
+  a.limit = p.limit;
   a.idesc = (1u << 4) | (p.epi.bf16 ? (1u << 7) | (1u << 10) : 0u) | (S::A_MN ? 1u << 15 : 0u) | (S::B_MN ? 1u << 16 : 0u) | ((uint32_t)(S::BN >> 3) << 17) |
             ((uint32_t)(S::TM >> 4) << 24);
   a.chunk = S::DRAIN && p.epi.out0_fp32 ? DRAIN_BLOCKS : 1 << 30;
@@ -1614,7 +1638,7 @@ int32_t workers_dense_forward(const ps_dense_layer* l, const ps_dense_output* o)
   return run_rows<D_FWD>(p, N, K, ys == 4);
 }
 
-int32_t workers_dense_backward(const ps_dense_layer* l, const ps_dense_gradients* o) {
+static int32_t backward(const ps_dense_layer* l, const ps_dense_gradients* o, int64_t limit) {
   int64_t rows = 0;
   int32_t rc = check_layer(l, &rows);
   if (rc != PS_OK) return rc;
@@ -1681,6 +1705,7 @@ int32_t workers_dense_backward(const ps_dense_layer* l, const ps_dense_gradients
     e.out1 = o->dx_pre; e.out1_pitch = o->dx_pre_pitch;
     e.act = l->activation; e.bf16 = l->type == PS_TYPE_BF16;
     set_moves(e, K, {{o->dx_add, o->dx_add_pitch, 0, 2}, {o->dx_pre ? o->x_pre : nullptr, o->x_pre_pitch, 0, 2}, {o->dx, o->dx_pitch, 0, 2}, {o->dx_pre, o->dx_pre_pitch, 0, 2}});
+    p.limit = limit;
     p.args.join = !o->db ? JOIN_FIRST : (o->dw ? JOIN_BETWEEN : JOIN_LAST);
     if ((rc = run_rows<D_DX>(p, K, N, false)) != PS_OK) return rc;
   }
@@ -1694,10 +1719,18 @@ int32_t workers_dense_backward(const ps_dense_layer* l, const ps_dense_gradients
     e.out0 = o->dw; e.out0_pitch = o->dw_pitch; e.out0_stride = o->dw_stride; e.out0_fp32 = ds == 4; e.accumulate = o->accumulate;
     e.bf16 = l->type == PS_TYPE_BF16;
     set_moves(e, K, {{o->dw, o->dw_pitch, l->groups > 1 ? o->dw_stride : 0, ds}});
+    p.limit = limit;
     p.args.join = o->db || o->dx || o->dx_pre ? JOIN_LAST : JOIN_FIRST;
     if ((rc = run_weights(p, N, K, ds == 4)) != PS_OK) return rc;
   }
   return PS_OK;
+}
+
+int32_t workers_dense_backward(const ps_dense_layer* l, const ps_dense_gradients* o) { return backward(l, o, WAIT_LIMIT_CYCLES); }
+
+int32_t workers_dense_selftest_backward(const ps_dense_layer* l, const ps_dense_gradients* o, int64_t limit_cycles) {
+  if (limit_cycles < 1 || limit_cycles > WAIT_LIMIT_CYCLES) return fail(PS_ERR_BAD_ARG, "limit_cycles must be 1..2e9");
+  return backward(l, o, limit_cycles);
 }
 
 }  // extern "C"

@@ -41,8 +41,8 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, long l
 
 // A bounded wait of a whole warp that another role's abort ends too: the same answer in every lane, for the warp-wide
 // tensor-memory reads behind it.
-__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, const volatile uint32_t* abort_flag) {
-  return __all_sync(0xffffffffu, mbar_wait(bar, parity) && !*abort_flag);
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, const volatile uint32_t* abort_flag, long long limit_cycles = WAIT_LIMIT_CYCLES) {
+  return __all_sync(0xffffffffu, mbar_wait(bar, parity, limit_cycles) && !*abort_flag);
 }
 
 // What several warps do next: true in all of their THREADS threads if `ok` holds in every one of them, false in all otherwise.

@@ -30,7 +30,7 @@ EXPORTS = ["ps_query_bytes", "ps_create", "ps_destroy", "ps_pull_snapshot", "ps_
            "ps_tick_host_submit", "ps_tick_host_wait",
            "ps_profile", "ps_profile_read", "ps_selftest_wait_timeout", "ps_last_error", "ps_replay_sum_static", "ps_replay_sum_static_error",
            "ps_apply_adamw", "ps_adamw_query_bytes", "ps_adamw_create", "ps_adamw_destroy", "ps_adamw_set_grads", "ps_adamw_step", "ps_adamw_read_info",
-           "workers_dense_workspace", "workers_dense_forward", "workers_dense_backward", "workers_dense_status"]
+           "workers_dense_workspace", "workers_dense_forward", "workers_dense_backward", "workers_dense_selftest_backward", "workers_dense_status"]
 
 
 class PSError(RuntimeError):
@@ -152,6 +152,7 @@ def load(path=None):
     sig["workers_dense_workspace"] = [C.POINTER(DenseLayer), vp, i64, C.POINTER(u64)]
     sig["workers_dense_forward"] = [C.POINTER(DenseLayer), C.POINTER(DenseOutput)]
     sig["workers_dense_backward"] = [C.POINTER(DenseLayer), C.POINTER(DenseGradients)]
+    sig["workers_dense_selftest_backward"] = [C.POINTER(DenseLayer), C.POINTER(DenseGradients), i64]
     sig["workers_dense_status"] = [vp]
     sig["ps_profile"] = [vp, i32]
     sig["ps_selftest_wait_timeout"] = [vp, i64]

@@ -492,6 +492,36 @@ def test_weight_gradients_past_32_bits():
         assert ((dw[g][-64:].double() - want).abs() <= half_step(want, torch.bfloat16) * 1.01).all()
 
 
+def backward_within(limit, dy, x, w, rows, dw):
+    """dw of a backward call whose waits end after `limit` clocks."""
+    counts, G, N, K = np.array(rows, dtype=np.int32), len(rows), dy.shape[1], x.shape[1]
+    kind = {torch.bfloat16: ps.TYPE_BF16, torch.float16: ps.TYPE_FP16, torch.float32: ps.TYPE_FP32}
+    shared = np.zeros(G, dtype=np.int32)
+    l = ps.DenseLayer(G, 1, counts.ctypes.data, shared.ctypes.data, K, N, kind[x.dtype], 0, x.data_ptr(), x.stride(0), w.data_ptr(), K, N * K, None, 0,
+                      torch.cuda.current_stream().cuda_stream)
+    out = ps.DenseGradients(dy=dy.data_ptr(), dy_pitch=dy.stride(0), dw=dw.data_ptr(), dw_pitch=K, dw_stride=N * K, dw_type=kind[dw.dtype])
+    assert ps.load().workers_dense_selftest_backward(C.byref(l), C.byref(out), limit) == 0
+    workers_dense_status()
+
+
+@gpu
+@pytest.mark.parametrize("kind,result", [("bf16", torch.float32)])
+def test_no_wait_grows_with_the_work(kind, result):
+    """A worker of 2^19 rows, some five million clocks of products to a pair of CTAs, ahead of one whose last block is ragged: no single wait takes 600,000."""
+    rows, N, K = [1 << 19, 100], 1792, 1792
+    gen = torch.Generator("cuda").manual_seed(11)
+    x, dy = ((torch.randn(sum(rows), c, generator=gen, device="cuda", dtype=TYPES[kind]) * 0.25) for c in (K, N))
+    w = torch.empty(N, K, device="cuda", dtype=TYPES[kind])
+    dw = torch.full((2, N, K), 77, device="cuda", dtype=result)
+    backward_within(600000, dy, x, w, rows, dw)
+    for g, s in spans(rows):
+        cols = slice(0, K) if g else slice(K - 32, K)
+        gy, gx = dy[s].double(), x[s, cols].double()
+        want, e = gy.T @ gx, sum_error(gy.abs().T @ gx.abs(), rows[g], result == torch.float32)
+        limit = e + (want.abs() * 2.0 ** -23 if result == torch.float32 else half_step(want.abs() + e, result))
+        assert ((dw[g][:, cols].double() - want).abs() <= limit).all(), g
+
+
 # ---- refusals --------------------------------------------------------------------------------------------------------------
 def layer(**more):
     """A layer whose addresses are never read: every refusal comes before any launch."""
@@ -541,6 +571,11 @@ def test_refused_gradients(bad):
     for k, v in bad.items():
         setattr(grads, k, v)
     assert ps.load().workers_dense_backward(C.byref(layer()), C.byref(grads)) == -1
+
+
+def test_refused_limits():
+    for limit in (0, -1, 2000000001):
+        assert ps.load().workers_dense_selftest_backward(C.byref(layer()), C.byref(ps.DenseGradients()), limit) == -1
 
 
 def test_workspace_is_asked_for_where_tile_copies_cannot_read():
