@@ -28,8 +28,9 @@ namespace psk {
 
 constexpr int PIECES = 3;
 
-// The part of a leading sum that truncation takes from it on average: (n - 1) / 2 times 1.3e-8 to 1.6e-8 for n instructions, whatever the
-// operands' signs (partial sums grow towards the whole in the mean).  It is the same for every sample, so that it does not average out in a
+// The part of a leading sum that truncation takes from it on average: (n - 1) / 2 times 1.3e-8 to 1.6e-8 for n instructions, where one
+// operand has both signs (partial sums grow towards the whole in the mean; products all of one sign lose 1.7e-7 to 2.0e-7 instead, since each
+// of the sixteen is cut).  It is the same for every sample, so that it does not average out in a
 // sum over samples as rounding does.  In the forward products, on which every gradient depends, sums are short (4 or 5 instructions) and the
 // weights' last pieces are larger by as much (the dense layer's input gradient, of 8 instructions, has the same operand).  Mean relative
 // error without / with both: second convolution -6.4e-8 (one sum of 9 instructions) / -0.04e-8, dense layer -4.7e-8 (8) / -0.01e-8, its input

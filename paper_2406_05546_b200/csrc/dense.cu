@@ -24,8 +24,10 @@
 //   41 rows on 16 of 4096 x 4096 reading the weights: 404 MB, 75, 5.4 TB/s
 //   1 row, 1568 -> 512           the host's call, 5 to 7
 //
-// Precision: the accumulators drop the low bits of every sum, always towards zero (bf16x3.cuh).  For results in FP32 the sums over 512 values
-// of k are handed to registers and added there, rounded; for 16-bit results their own rounding is 100 times what is lost.
+// Precision: the accumulators drop low bits with every instruction (16 products), of each of its terms and always towards zero: of products of both signs
+// (n - 1) / 2 times 1.3e-8 to 1.6e-8 after n instructions (bf16x3.cuh), of products of one sign 1.7e-7 to 2.0e-7.  So the sums over a bounded number of
+// values of k are handed to registers and added there, rounded: over 512 for results in FP32 (2.6e-6 is lost at most, whatever the length), over
+// 8,192 in FP16 and 65,536 in BF16 (5.2e-5 and 4e-4: a fifth of what their own rounding takes at least, 2^-12 and 2^-9).
 //
 // Ragged reductions (weight gradient): a tile's last block of 64 rows may reach into the next worker's.  Those rows are zeroed in shared
 // memory, in both operands (a NaN times zero would stay), before the MMA reads them.
@@ -62,7 +64,7 @@ constexpr int BM = 128, BK = 64;
 // 400, half with 100: 27.7 -> 31.7).  The input gradient, which reads two matrices more, has not the
 // registers for it (64 -> 117).
 constexpr int THIN_RED_FWD = 384, THIN_RED_DW = 256, THIN_MOST_DW = 512, THIN_MEAN_DW = 128;
-constexpr int DRAIN_BLOCKS = 8;      // blocks of k whose sums share an accumulator where the result is FP32
+constexpr int DRAIN_FP32 = 8, DRAIN_FP16 = 128, DRAIN_BF16 = 1024;      // blocks of k whose sums share an accumulator, by the result's type
 constexpr int SMEM_MOST = 227 * 1024, BARRIER_BYTES = 256;
 
 template <int OP_, int CTAS_, int BN_, int STAGES_, bool SPLIT_, bool FEW_, bool DRAIN_, int PER_SM_ = 1> struct DenseShape {
@@ -87,7 +89,7 @@ template <int OP_, int CTAS_, int BN_, int STAGES_, bool SPLIT_, bool FEW_, bool
 template <int OP, bool DRAIN> using Pair = DenseShape<OP, 2, 256, 6, false, false, DRAIN>;
 template <int OP, bool DRAIN> using Single = DenseShape<OP, 1, 256, 4, false, false, DRAIN>;
 template <int OP> using Thin = DenseShape<OP, 1, 128, 2, false, false, false, 2>;
-static_assert(THIN_RED_FWD <= DRAIN_BLOCKS * BK && THIN_MOST_DW <= DRAIN_BLOCKS * BK, "Thin tiles do not drain their accumulators");
+static_assert(THIN_RED_FWD <= DRAIN_FP32 * BK && THIN_MOST_DW <= DRAIN_FP32 * BK, "Thin tiles do not drain their accumulators");
 template <int OP> using Split = DenseShape<OP, 1, 128, 6, true, false, true>;
 template <int OP, int BN> using Few = DenseShape<OP, 1, BN, BN == 64 ? 4 : 5, true, true, true>;
 
@@ -1312,8 +1314,8 @@ int32_t setup() {      // once per device
   std::lock_guard<std::mutex> lock(mutex);
   if (done[dev]) return PS_OK;
   bool ok = configure_tc5_kernels() == 0;
-  const cudaError_t e[] = {allow<Pair<D_FWD, false>>(), allow<Pair<D_FWD, true>>(), allow<Pair<D_DX, false>>(), allow<Pair<D_DW, false>>(), allow<Pair<D_DW, true>>(),
-                           allow<Single<D_FWD, false>>(), allow<Single<D_FWD, true>>(), allow<Single<D_DX, false>>(), allow<Single<D_DW, false>>(), allow<Single<D_DW, true>>(),
+  const cudaError_t e[] = {allow<Pair<D_FWD, false>>(), allow<Pair<D_FWD, true>>(), allow<Pair<D_DX, false>>(), allow<Pair<D_DX, true>>(), allow<Pair<D_DW, false>>(), allow<Pair<D_DW, true>>(),
+                           allow<Single<D_FWD, false>>(), allow<Single<D_FWD, true>>(), allow<Single<D_DX, false>>(), allow<Single<D_DX, true>>(), allow<Single<D_DW, false>>(), allow<Single<D_DW, true>>(),
                            allow<Thin<D_FWD>>(), allow<Thin<D_DW>>(), allow<Split<D_FWD>>(), allow<Split<D_DX>>(), allow<Split<D_DW>>(),
                            allow<Few<D_FWD, 16>>(), allow<Few<D_FWD, 32>>(), allow<Few<D_FWD, 64>>(), allow<Few<D_DX, 16>>(), allow<Few<D_DX, 32>>(), allow<Few<D_DX, 64>>()};
   for (cudaError_t x : e) ok = ok && x == cudaSuccess;
@@ -1321,6 +1323,8 @@ int32_t setup() {      // once per device
   done[dev] = true;
   return PS_OK;
 }
+
+int drain_blocks(const DenseEpi& e) { return e.out0_fp32 ? DRAIN_FP32 : (e.bf16 ? DRAIN_BF16 : DRAIN_FP16); }
 
 struct Problem {
   DenseTab tab;          // merged groups (forward, input gradient) or workers (weight gradient)
@@ -1340,7 +1344,7 @@ int32_t launch(const Problem& p, int split) {
   a.limit = p.limit;
   a.idesc = (1u << 4) | (p.epi.bf16 ? (1u << 7) | (1u << 10) : 0u) | (S::A_MN ? 1u << 15 : 0u) | (S::B_MN ? 1u << 16 : 0u) | ((uint32_t)(S::BN >> 3) << 17) |
             ((uint32_t)(S::TM >> 4) << 24);
-  a.chunk = S::DRAIN && p.epi.out0_fp32 ? DRAIN_BLOCKS : 1 << 30;
+  a.chunk = S::DRAIN ? drain_blocks(p.epi) : 1 << 30;
   cudaLaunchConfig_t cfg = {};
   const int walkers = g_sm_count * S::PER_SM / S::CTAS;
   cfg.gridDim = S::SPLIT ? dim3(a.n_tiles, 1, split) : dim3(S::CTAS * std::min(a.n_tiles, walkers));
@@ -1391,7 +1395,7 @@ int split_for(int64_t tiles, int blocks, int room) {
 
 // Forward and input gradient: rows of groups x `features` columns, reduction over `red`.
 template <int OP>
-int32_t run_rows(Problem& p, int features, int red, bool fp32_out) {
+int32_t run_rows(Problem& p, int features, int red) {
   DenseTab& tab = p.tab;
   int most = 0;
   int64_t rows = 0;
@@ -1404,7 +1408,7 @@ int32_t run_rows(Problem& p, int features, int red, bool fp32_out) {
   a.n_side = features;
   a.red = red;
   a.rows = (int32_t)rows;
-  fp32_out = fp32_out && red > DRAIN_BLOCKS * BK;      // a shorter sum takes one accumulator either way
+  const bool drain = blocks > drain_blocks(p.epi);      // a shorter sum takes one accumulator either way
   if (rows <= 48ll * tab.groups) {
     const int bn = most <= 16 ? 16 : (most <= 32 ? 32 : 64);
     a.n_tiles_n = div_up(features, BM);
@@ -1433,21 +1437,19 @@ int32_t run_rows(Problem& p, int features, int red, bool fp32_out) {
   if (pairs * a.n_tiles_n * 2 >= sms && pairs * 10 <= row_blocks * 6) {
     a.m_tiles = (int)pairs;
     a.n_tiles = (int)pairs * a.n_tiles_n;
-    if constexpr (OP == D_FWD) if (fp32_out) return launch<Pair<OP, true>>(p, 1);
-    return launch<Pair<OP, false>>(p, 1);
+    return drain ? launch<Pair<OP, true>>(p, 1) : launch<Pair<OP, false>>(p, 1);
   }
   a.m_tiles = (int)row_blocks;
   if (singles * 3 >= sms * 2 || row_blocks * div_up(features, 128) > sms) {
     a.n_tiles = (int)singles;
-    if constexpr (OP == D_FWD) if (fp32_out) return launch<Single<OP, true>>(p, 1);
-    return launch<Single<OP, false>>(p, 1);
+    return drain ? launch<Single<OP, true>>(p, 1) : launch<Single<OP, false>>(p, 1);
   }
   a.n_tiles_n = div_up(features, 128);
   a.n_tiles = (int)row_blocks * a.n_tiles_n;
   return launch<Split<OP>>(p, split_for(a.n_tiles, blocks, sms));
 }
 
-int32_t run_weights(Problem& p, int N, int K, bool fp32_out) {
+int32_t run_weights(Problem& p, int N, int K) {
   DenseTab& tab = p.tab;
   DenseArgs& a = p.args;
   int most = 0;
@@ -1457,7 +1459,7 @@ int32_t run_weights(Problem& p, int N, int K, bool fp32_out) {
     rows += tab.row1[g] - tab.row0[g];
   }
   const bool few = most <= THIN_RED_DW || (most <= THIN_MOST_DW && rows <= (int64_t)THIN_MEAN_DW * tab.groups);
-  fp32_out = fp32_out && most > DRAIN_BLOCKS * BK;
+  const bool drain = div_up(most, BK) > drain_blocks(p.epi);
   const int sms = g_sm_count;
   a.m_side = N; a.n_side = K; a.red = 0;
   auto tiles = [&](int tm) { a.m_tiles = div_up(N, tm); return (int64_t)tab.groups * a.m_tiles * a.n_tiles_n; };
@@ -1471,11 +1473,11 @@ int32_t run_weights(Problem& p, int N, int K, bool fp32_out) {
   if (singles >= 1 << 30) return fail(PS_ERR_BAD_ARG, "too many tiles");
   if (pairs * 2 >= sms && pairs * 2 <= singles + singles / 5) {
     a.n_tiles = (int)tiles(256);
-    return fp32_out ? launch<Pair<D_DW, true>>(p, 1) : launch<Pair<D_DW, false>>(p, 1);
+    return drain ? launch<Pair<D_DW, true>>(p, 1) : launch<Pair<D_DW, false>>(p, 1);
   }
   if (singles * 3 >= sms * 2 || singles / a.n_tiles_n * div_up(K, 128) > sms) {
     a.n_tiles = (int)tiles(128);
-    return fp32_out ? launch<Single<D_DW, true>>(p, 1) : launch<Single<D_DW, false>>(p, 1);
+    return drain ? launch<Single<D_DW, true>>(p, 1) : launch<Single<D_DW, false>>(p, 1);
   }
   a.n_tiles_n = div_up(K, 128);
   a.n_tiles = (int)tiles(128);
@@ -1635,7 +1637,7 @@ int32_t workers_dense_forward(const ps_dense_layer* l, const ps_dense_output* o)
   e.out1 = o->pre; e.out1_pitch = o->pre_pitch;
   e.act = l->activation; e.bf16 = l->type == PS_TYPE_BF16;
   set_moves(e, N, {{o->residual, o->residual_pitch, 0, 2}, {o->y, o->y_pitch, 0, ys}, {o->pre, o->pre_pitch, 0, 2}});
-  return run_rows<D_FWD>(p, N, K, ys == 4);
+  return run_rows<D_FWD>(p, N, K);
 }
 
 static int32_t backward(const ps_dense_layer* l, const ps_dense_gradients* o, int64_t limit) {
@@ -1707,7 +1709,7 @@ static int32_t backward(const ps_dense_layer* l, const ps_dense_gradients* o, in
     set_moves(e, K, {{o->dx_add, o->dx_add_pitch, 0, 2}, {o->dx_pre ? o->x_pre : nullptr, o->x_pre_pitch, 0, 2}, {o->dx, o->dx_pitch, 0, 2}, {o->dx_pre, o->dx_pre_pitch, 0, 2}});
     p.limit = limit;
     p.args.join = !o->db ? JOIN_FIRST : (o->dw ? JOIN_BETWEEN : JOIN_LAST);
-    if ((rc = run_rows<D_DX>(p, K, N, false)) != PS_OK) return rc;
+    if ((rc = run_rows<D_DX>(p, K, N)) != PS_OK) return rc;
   }
   if (o->dw) {
     Problem p = {};
@@ -1721,7 +1723,7 @@ static int32_t backward(const ps_dense_layer* l, const ps_dense_gradients* o, in
     set_moves(e, K, {{o->dw, o->dw_pitch, l->groups > 1 ? o->dw_stride : 0, ds}});
     p.limit = limit;
     p.args.join = o->db || o->dx || o->dx_pre ? JOIN_LAST : JOIN_FIRST;
-    if ((rc = run_weights(p, N, K, ds == 4)) != PS_OK) return rc;
+    if ((rc = run_weights(p, N, K)) != PS_OK) return rc;
   }
   return PS_OK;
 }

@@ -505,7 +505,7 @@ def backward_within(limit, dy, x, w, rows, dw):
 
 
 @gpu
-@pytest.mark.parametrize("kind,result", [("bf16", torch.float32)])
+@pytest.mark.parametrize("kind,result", [("bf16", torch.float32), ("fp16", torch.float16)])
 def test_no_wait_grows_with_the_work(kind, result):
     """A worker of 2^19 rows, some five million clocks of products to a pair of CTAs, ahead of one whose last block is ragged: no single wait takes 600,000."""
     rows, N, K = [1 << 19, 100], 1792, 1792
@@ -520,6 +520,52 @@ def test_no_wait_grows_with_the_work(kind, result):
         want, e = gy.T @ gx, sum_error(gy.abs().T @ gx.abs(), rows[g], result == torch.float32)
         limit = e + (want.abs() * 2.0 ** -23 if result == torch.float32 else half_step(want.abs() + e, result))
         assert ((dw[g][:, cols].double() - want).abs() <= limit).all(), g
+
+
+# Sums of one sign so long that an accumulator's truncation would come near the result's rounding and pass it.  An instruction cuts its sixteen products and the
+# accumulator at 2^-25 of a power of two that is not above their sum: half of that each in the mean, 17 / 2 * 2^-25 of the partial sum, and half as much
+# of the whole, since partial sums grow evenly: n instructions lose 17 / 4 * 2^-25 n of it.  (Measured, of 1,024: 1.04e-4, where this gives 1.3e-4.)
+# It is the same for all results while their roundings average out (rows and columns differ in scale), so the mean of the relative errors shows it.  An accumulator takes 512 (FP16) or
+# 4,096 (BF16) at most; the mean of n roundings, each within half a step u and evenly spread, has a deviation of u / sqrt(3 n).
+LONG_SUMS = [("dw", "fp16", 1 << 18, 1664, 1664), ("dw", "fp16", 1 << 18, 2304, 2304), ("dw", "fp16", 1 << 21, 64, 72), ("dw", "bf16", 1 << 21, 1664, 1664),
+             ("forward", "fp16", 2600, 2048, 1 << 18), ("forward", "fp16", 600, 1040, 1 << 18), ("forward", "fp16", 3, 520, 1 << 20),
+             ("dx", "fp16", 2600, 1 << 18, 2048), ("dx", "fp16", 600, 1 << 18, 1040), ("dx", "fp16", 3, 1 << 20, 520), ("dx", "bf16", 2600, 1 << 20, 2048)]
+
+
+@gpu
+@pytest.mark.parametrize("op,kind,M,N,K", LONG_SUMS)
+def test_long_sums_keep_their_low_bits(op, kind, M, N, K):
+    t = TYPES[kind]
+    gen = torch.Generator("cuda").manual_seed(12)
+    def positive(*s, scaled):      # along dimension `scaled` the values differ in scale
+        shape = [1] * len(s)
+        shape[scaled] = s[scaled]
+        return (torch.rand(*s, generator=gen, device="cuda", dtype=t) * 0.0625 + 0.03125) * (0.5 + 0.5 * torch.rand(*shape, generator=gen, device="cuda")).to(t)
+    length = {"dw": M, "forward": K, "dx": N}[op]
+    if op == "dw":
+        x, dy, w = positive(M, K, scaled=1), positive(M, N, scaled=1), torch.empty(1, N, K, device="cuda", dtype=t)
+        got = torch.empty(1, N, K, device="cuda", dtype=t)
+        workers_dense_backward(dy, x, w, [M], dw=got)
+        got, left, right = got[0, :, -512:], dy.T, x[:, -512:]
+    elif op == "forward":
+        x, w = positive(M, K, scaled=0), positive(1, N, K, scaled=1)
+        got = workers_dense_forward(x, w, [M])
+        got, left, right = got[:, -512:], x, w[0, -512:].T
+    else:
+        dy, w = positive(M, N, scaled=0), positive(1, N, K, scaled=2)
+        got = torch.empty(M, K, device="cuda", dtype=t)
+        workers_dense_backward(dy, torch.empty(M, K, device="cuda", dtype=t), w, [M], dx=got)
+        got, left, right = got[:, -512:], dy, w[0, :, -512:]
+    workers_dense_status()
+    want = torch.zeros(got.shape, device="cuda", dtype=torch.float64)
+    for a in range(0, length, 1 << 16):
+        want += left[:, a:a + (1 << 16)].double() @ right[a:a + (1 << 16)].double()
+    assert torch.isfinite(got).all()
+    off = (got.double() - want) / want
+    u = torch.finfo(t).eps / 2
+    lost = 17 / 4 * 2.0 ** -25 * {"fp16": 512, "bf16": 4096}[kind]
+    assert (off.abs() <= u + 2 * lost).all()
+    assert abs(float(off.mean())) <= lost + 6 * u / math.sqrt(3 * off.numel())
 
 
 # ---- refusals --------------------------------------------------------------------------------------------------------------
