@@ -1080,6 +1080,8 @@ __global__ void __launch_bounds__(S::THREADS, S::PER_SM) dense_gemm(const __grid
   }
   tc_fence_before();
   __syncthreads();
+  if (*abort_flag)      // copies and products already issued end before the memory that they write is given up
+    for (int i = 0; i < 1000; ++i) __nanosleep(1000);
   if (PAIR) cg::this_cluster().sync();      // no CTA leaves while the other may still arrive at its barriers
   if (warp == 1) {
     tc_fence_after();
@@ -1139,10 +1141,7 @@ __global__ void __launch_bounds__(S::THREADS, S::PER_SM) dense_gemm(const __grid
     else finish(std::integral_constant<int, 1>());
     cl.sync();                               // a CTA's shared memory outlives its readers
   }
-  if (tid == 0 && *abort_flag) {
-    atomicOr(&g_dense_status, STATUS_WAIT_TIMEOUT);
-    for (int i = 0; i < 1000; ++i) __nanosleep(1000);      // let copies already issued land before the CTA ends
-  }
+  if (tid == 0 && *abort_flag) atomicOr(&g_dense_status, STATUS_WAIT_TIMEOUT);
 }
 
 // ---- the bias gradient: column sums of each worker's rows ------------------------------------------------------------------
