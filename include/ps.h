@@ -509,8 +509,11 @@ int32_t workers_dense_selftest_backward(const ps_dense_layer* layer, const ps_de
 /* Workspace bytes of a call with these operands; dy NULL: of the forward call. */
 int32_t workers_dense_workspace(const ps_dense_layer* layer, const void* dy, int64_t dy_pitch, uint64_t* bytes);
 
-/* Synchronises the stream; PS_ERR_DEVICE_STATUS if a bounded wait of a dense-layer kernel on the current device gave up since the last call. */
+/* Synchronises the stream; PS_ERR_DEVICE_STATUS if a bounded wait of a dense-layer kernel on the current device gave up, whoever called it, since the
+ * calling thread last asked (its first time: since the library was loaded).  Asking takes the answer away from no other thread. */
 int32_t workers_dense_status(void* stream);
+/* Launches a kernel on the current device whose wait, of limit_cycles (1..2e9), is bound to give up. */
+int32_t workers_dense_selftest_wait_timeout(int64_t limit_cycles, void* stream);
 
 const char* ps_last_error(ps_ctx* ctx);
 

@@ -32,7 +32,7 @@
 // Ragged reductions (weight gradient): a tile's last block of 64 rows may reach into the next worker's.  Those rows are zeroed in shared
 // memory, in both operands (a NaN times zero would stay), before the MMA reads them.
 //
-// Every wait on an mbarrier is bounded; a CTA that gives up sets a status word that workers_dense_status reads.
+// Every wait on an mbarrier is bounded; a CTA that gives up counts itself in a word that workers_dense_status reads.
 #include <cooperative_groups.h>
 #include <cuda.h>
 #include <cuda_fp16.h>
@@ -131,8 +131,20 @@ struct DenseArgs {
   int64_t limit;                                    // clocks that a wait may last
 };
 
-// Set when a wait gives up, until workers_dense_status reads it: these entry points have no context to keep it in.
-__device__ uint32_t g_dense_status;
+// CTAs whose wait gave up, on this device: these entry points have no context to keep it in.  It is never written by a reader, so that none takes a
+// failure away from another, or loses one that comes while it reads.
+__device__ uint32_t g_dense_failures;
+
+__global__ void __launch_bounds__(32) dense_wait_probe(long long limit) {
+  __shared__ uint64_t never;
+  if (threadIdx.x == 0) {
+    mbar_init(&never, 1);      // one arrival expected; nobody ever arrives
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncwarp();
+  const bool ok = __all_sync(0xffffffffu, mbar_wait(&never, 0, limit));
+  if (!ok && threadIdx.x == 0) atomicAdd(&g_dense_failures, 1u);
+}
 
 struct DenseMaps { CUtensorMap a, b; };
 
@@ -1141,7 +1153,7 @@ __global__ void __launch_bounds__(S::THREADS, S::PER_SM) dense_gemm(const __grid
     else finish(std::integral_constant<int, 1>());
     cl.sync();                               // a CTA's shared memory outlives its readers
   }
-  if (tid == 0 && *abort_flag) atomicOr(&g_dense_status, STATUS_WAIT_TIMEOUT);
+  if (tid == 0 && *abort_flag) atomicAdd(&g_dense_failures, 1u);
 }
 
 // ---- the bias gradient: column sums of each worker's rows ------------------------------------------------------------------
@@ -1266,6 +1278,7 @@ __global__ void __launch_bounds__(256) lay_out_rows(const __grid_constant__ LayA
 
 // ---- host ----------------------------------------------------------------------------------------------------------------
 constexpr int32_t MAX_FEATURES = 1 << 20;
+constexpr int MAX_DEVICES = 64;
 constexpr int64_t MAX_ROWS = (1ll << 31) - (1 << 20);
 
 bool tma_ok(const void* p, int64_t pitch) { return ((uintptr_t)p & 15) == 0 && pitch % 8 == 0; }
@@ -1307,9 +1320,9 @@ template <class S> cudaError_t allow() { return allow_smem((const void*)dense_ge
 
 int32_t setup() {      // once per device
   static std::mutex mutex;
-  static bool done[64] = {false};
+  static bool done[MAX_DEVICES] = {false};
   int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return fail(PS_ERR_CUDA, "no current device");
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= MAX_DEVICES) return fail(PS_ERR_CUDA, "no current device");
   std::lock_guard<std::mutex> lock(mutex);
   if (done[dev]) return PS_OK;
   bool ok = configure_tc5_kernels() == 0;
@@ -1599,12 +1612,24 @@ int32_t workers_dense_workspace(const ps_dense_layer* l, const void* dy, int64_t
 }
 
 int32_t workers_dense_status(void* stream) {
-  uint32_t word = 0, zero = 0;
-  cudaError_t e = cudaMemcpyFromSymbolAsync(&word, g_dense_status, sizeof(word), 0, cudaMemcpyDeviceToHost, (cudaStream_t)stream);
-  if (e == cudaSuccess) e = cudaMemcpyToSymbolAsync(g_dense_status, &zero, sizeof(zero), 0, cudaMemcpyHostToDevice, (cudaStream_t)stream);
+  static thread_local uint32_t seen[MAX_DEVICES] = {0};
+  uint32_t count = 0;
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess && (dev < 0 || dev >= MAX_DEVICES)) return fail(PS_ERR_CUDA, "no current device");
+  if (e == cudaSuccess) e = cudaMemcpyFromSymbolAsync(&count, g_dense_failures, sizeof(count), 0, cudaMemcpyDeviceToHost, (cudaStream_t)stream);
   if (e == cudaSuccess) e = cudaStreamSynchronize((cudaStream_t)stream);
   if (e != cudaSuccess) return fail(PS_ERR_CUDA, "workers_dense_status: %s", cudaGetErrorString(e));
-  return word == 0 ? PS_OK : fail(PS_ERR_DEVICE_STATUS, "a bounded wait in a dense-layer kernel gave up: results since the last call are not to be used");
+  if (count == seen[dev]) return PS_OK;
+  seen[dev] = count;
+  return fail(PS_ERR_DEVICE_STATUS, "a bounded wait in a dense-layer kernel gave up: results since the last call are not to be used");
+}
+
+int32_t workers_dense_selftest_wait_timeout(int64_t limit_cycles, void* stream) {
+  if (limit_cycles < 1 || limit_cycles > WAIT_LIMIT_CYCLES) return fail(PS_ERR_BAD_ARG, "limit_cycles must be 1..2e9");
+  dense_wait_probe<<<1, 32, 0, (cudaStream_t)stream>>>(limit_cycles);
+  const cudaError_t e = cudaGetLastError();
+  return e == cudaSuccess ? PS_OK : fail(PS_ERR_CUDA, "probe launch: %s", cudaGetErrorString(e));
 }
 
 int32_t workers_dense_forward(const ps_dense_layer* l, const ps_dense_output* o) {

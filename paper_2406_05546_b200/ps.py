@@ -30,7 +30,8 @@ EXPORTS = ["ps_query_bytes", "ps_create", "ps_destroy", "ps_pull_snapshot", "ps_
            "ps_tick_host_submit", "ps_tick_host_wait",
            "ps_profile", "ps_profile_read", "ps_selftest_wait_timeout", "ps_last_error", "ps_replay_sum_static", "ps_replay_sum_static_error",
            "ps_apply_adamw", "ps_adamw_query_bytes", "ps_adamw_create", "ps_adamw_destroy", "ps_adamw_set_grads", "ps_adamw_step", "ps_adamw_read_info",
-           "workers_dense_workspace", "workers_dense_forward", "workers_dense_backward", "workers_dense_selftest_backward", "workers_dense_status"]
+           "workers_dense_workspace", "workers_dense_forward", "workers_dense_backward", "workers_dense_selftest_backward", "workers_dense_status",
+           "workers_dense_selftest_wait_timeout"]
 
 
 class PSError(RuntimeError):
@@ -154,6 +155,7 @@ def load(path=None):
     sig["workers_dense_backward"] = [C.POINTER(DenseLayer), C.POINTER(DenseGradients)]
     sig["workers_dense_selftest_backward"] = [C.POINTER(DenseLayer), C.POINTER(DenseGradients), i64]
     sig["workers_dense_status"] = [vp]
+    sig["workers_dense_selftest_wait_timeout"] = [i64, vp]
     sig["ps_profile"] = [vp, i32]
     sig["ps_selftest_wait_timeout"] = [vp, i64]
     sig["ps_profile_read"] = [vp, i32, C.POINTER(C.c_char_p), C.POINTER(C.c_double), C.POINTER(i64)]
@@ -274,7 +276,7 @@ def workers_dense_backward(dy, x, weight, rows, weight_of=None, x_pre=None, acti
 
 
 def workers_dense_status():
-    """Waits for torch's current stream; raises if a dense-layer kernel on the current device gave up a wait since the last call."""
+    """Waits for torch's current stream; raises if a dense-layer kernel on the current device gave up a wait since this thread's last call."""
     import torch
     rc = load().workers_dense_status(torch.cuda.current_stream().cuda_stream)
     if rc != 0:

@@ -522,6 +522,35 @@ def test_no_wait_grows_with_the_work(kind, result):
         assert ((dw[g][:, cols].double() - want).abs() <= limit).all(), g
 
 
+@gpu
+def test_a_wait_that_gave_up_is_reported_to_every_thread_once():
+    """A thread that asks takes the answer from no other, and failures that come later are reported anew."""
+    from concurrent.futures import ThreadPoolExecutor
+
+    def ask():
+        try:
+            workers_dense_status()
+        except ps.PSError as e:
+            assert "PS_ERR_DEVICE_STATUS" in str(e)
+            return True
+        return False
+    side = torch.cuda.Stream()
+    with ThreadPoolExecutor(1) as one, ThreadPoolExecutor(1) as two:
+        for pool in (one, two):
+            pool.submit(ask).result()
+        ask()
+        assert not ask() and not one.submit(ask).result()
+        for stream in (torch.cuda.current_stream(), side):
+            assert ps.load().workers_dense_selftest_wait_timeout(10000, stream.cuda_stream) == 0
+            torch.cuda.synchronize()
+            assert one.submit(ask).result() and ask() and two.submit(ask).result()
+            assert not ask() and not two.submit(ask).result() and not one.submit(ask).result()
+    # and the next call is as good as any
+    x, w = torch.ones(3, 16, device="cuda").bfloat16(), torch.ones(1, 8, 16, device="cuda").bfloat16()
+    assert (workers_dense_forward(x, w, [3]) == 16).all()
+    workers_dense_status()
+
+
 # Sums of one sign so long that an accumulator's truncation would come near the result's rounding and pass it.  An instruction cuts its sixteen products and the
 # accumulator at 2^-25 of a power of two that is not above their sum: half of that each in the mean, 17 / 2 * 2^-25 of the partial sum, and half as much
 # of the whole, since partial sums grow evenly: n instructions lose 17 / 4 * 2^-25 n of it.  (Measured, of 1,024: 1.04e-4, where this gives 1.3e-4.)
@@ -622,6 +651,7 @@ def test_refused_gradients(bad):
 def test_refused_limits():
     for limit in (0, -1, 2000000001):
         assert ps.load().workers_dense_selftest_backward(C.byref(layer()), C.byref(ps.DenseGradients()), limit) == -1
+        assert ps.load().workers_dense_selftest_wait_timeout(limit, None) == -1
 
 
 def test_workspace_is_asked_for_where_tile_copies_cannot_read():
