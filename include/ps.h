@@ -225,7 +225,9 @@ int32_t ps_apply_stale(ps_ctx* ctx, ps_mode mode, float lr, float scale, const i
  *   p = p (1 - lr weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
  * in fp32; the moments' operations are rounded one by one, the quotient is within 8 units in the last place (its root is taken of at least 2^-126),
  * and the constants are made in fp64 and rounded once.  f = grad_scale * min(1, clip_norm / norm), norm
- * being that of grad_scale * gradient; clip_norm 0 = no clipping.  A gradient that is not finite makes its own element's moments and weight NaN. */
+ * being that of grad_scale * gradient; clip_norm 0 = no clipping.  A gradient that is not finite makes its own element's moments and weight NaN.  With
+ * clipping it has a part in the norm too: a norm that is infinite makes f zero, one that is NaN makes f, and with it every element, NaN (skip_nonfinite
+ * keeps either from happening). */
 typedef struct ps_adamw_hyper {
   double   lr, beta1, beta2, eps;   /* finite; 0 <= beta < 1; eps >= 2^-126 (as fp32) */
   double   grad_scale;              /* 1 = none */

@@ -355,7 +355,7 @@ __device__ void finish_state(double total, bool has_norm, const Call& call, DevS
     const double norm = fabs(call.grad_scale) * sqrt(total);
     st->norm = (float)norm;
     skip = call.skip_nonfinite && !isfinite(norm);
-    if (call.clip > 0.0) factor *= fmin(1.0, call.clip / norm);      // a zero gradient keeps its factor (clip / 0 = inf)
+    if (call.clip > 0.0) factor *= isnan(norm) ? norm : fmin(1.0, call.clip / norm);      // a zero gradient keeps its factor (clip / 0 = inf)
   }
   st->skip = skip ? 1 : 0;
   if (skip) { st->skipped += 1; return; }

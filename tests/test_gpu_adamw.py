@@ -122,6 +122,31 @@ def test_a_gradient_that_is_not_finite(bad):
 
 
 @gpu
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("bits", [32, 8])
+def test_clipping_a_gradient_that_is_not_finite(bad, bits):
+    """An infinite norm makes the factor zero: every other element takes the step of a zero gradient.  A norm that is NaN reaches all of them."""
+    gen = torch.Generator("cuda").manual_seed(4)
+    p, q = ([torch.ones(k, device="cuda") for k in (3000, 77)] for _ in range(2))
+    g = [torch.randn(k, generator=gen, device="cuda") for k in (3000, 77)]
+    g[0][1234] = bad
+    opt, ref = AdamW(p, g, state_bits=bits, weight_decay=0.1), AdamW(q, [torch.zeros_like(x) for x in g], state_bits=bits, weight_decay=0.1)
+    for o in (opt, ref):
+        o.ps_adamw_step(step=3, clip_norm=1.0, **HYPER)
+    kind = (lambda xs: xs) if bits == 32 else (lambda xs: [x.view(torch.float8_e4m3fn).float() for x in xs])
+    second = (lambda xs: xs) if bits == 32 else (lambda xs: [x.view(torch.float8_e5m2).float() for x in xs])
+    for got, want in ((p, q), (kind(opt.m), kind(ref.m)), (second(opt.v), second(ref.v))):
+        if math.isnan(bad):
+            assert all(torch.isnan(x).all() for x in got)
+        else:
+            assert torch.isnan(got[0][1234])
+            fine = torch.ones(3000, dtype=torch.bool, device="cuda")
+            fine[1234] = False
+            assert torch.equal(got[0][fine], want[0][fine]) and torch.equal(got[1], want[1])
+    assert opt.ps_adamw_read_info()["grad_factor"] == pytest.approx(math.nan if math.isnan(bad) else 0.0, nan_ok=True)
+
+
+@gpu
 def test_a_captured_step_counts_and_follows_its_schedule():
     gen = torch.Generator("cuda").manual_seed(6)
     make = lambda: [torch.randn(k, generator=torch.Generator("cuda").manual_seed(k), device="cuda") for k in (300, 9001)]
