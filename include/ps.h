@@ -210,7 +210,7 @@ int32_t ps_apply(ps_ctx* ctx, ps_mode mode, float lr, float scale, const int32_t
  * stateless server, as alternatives to a smaller learning rate for many pending gradients (gradient clipping, an
  * adaptive learning rate).  Readings taken here:
  *   clip_norm c > 0        every queued gradient g is scaled by min(1, c / ||g||_2) (clipping by global norm, per
- *                          gradient); costs one extra pass over the queue that takes the norms;
+ *                          gradient; one whose norm is NaN is not scaled); costs one extra pass over the queue that takes the norms;
  *   staleness_alpha a > 0  gradient k is scaled by 1 / (1 + a * tau_k), tau_k = the version its update is applied to
  *                          (the head for PS_SYNC / PS_REPLAY, head + j for the j-th gradient of PS_ASYNC) minus the
  *                          base_version given at ps_enqueue.  A base version newer than that is PS_ERR_BAD_ARG.
@@ -242,7 +242,8 @@ typedef struct ps_adamw_hyper {
 /* ps_apply with AdamW as the server's optimizer.  The gradients are taken as in ps_apply_stale, without the learning rate:
  *   PS_SYNC / PS_REPLAY   one update with grad_scale * scale / K (or / W_tick) * sum of the queued gradients ; version + 1
  *   PS_ASYNC              one update per gradient in order, with grad_scale * scale * g_k; update k counts as step h->step + k
- * clip_norm and staleness_alpha act on every queued gradient by itself (clip_norm on the gradient as queued), as in ps_apply_stale.
+ * clip_norm and staleness_alpha act on every queued gradient by itself (clip_norm on the gradient as queued), as in ps_apply_stale; but a gradient whose
+ * norm is NaN gets the factor NaN, as in ps_adamw_step, and with it every weight becomes NaN.  (An infinite norm makes the factor zero.)
  * m_dev, v_dev: the moments, PS_PARAM_STRIDE floats each (dev, 16-byte aligned, read and written; zeros before the first step; their padding
  * is written zero).  They are the caller's: ps_restore, ps_failover and ps_import_params leave them alone, and a caller who rolls the weights
  * back decides whether to keep, restore or clear them.  Versions, checkpoints, replication, order and result are as in ps_apply.

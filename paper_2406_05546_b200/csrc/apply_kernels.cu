@@ -49,6 +49,7 @@ __device__ __forceinline__ float2 compensated(u64 acc, u64 err) {
 
 // What becomes of a column's sum s of gradients (and the factor c that they share): t - c s, or AdamW of c s.
 struct Sgd {
+  static constexpr bool NAN_STAYS = false;      // does a norm that is NaN make a gradient's factor NaN? (Or 1, as a comparison with it has it.)
   __device__ __forceinline__ float4 operator()(int, float4 t, float c, const float4& s) const {
     t.x = fmaf(-c, s.x, t.x); t.y = fmaf(-c, s.y, t.y);
     t.z = fmaf(-c, s.z, t.z); t.w = fmaf(-c, s.w, t.w);
@@ -64,6 +65,7 @@ __device__ __forceinline__ float4 without_padding(int col, float4 v) {
   return v;
 }
 struct AdamW {
+  static constexpr bool NAN_STAYS = true;
   AdamColumns a;
   __device__ __forceinline__ float4 operator()(int col, float4 t, float c, const float4& s) const {
     float4 m = reinterpret_cast<const float4*>(a.m)[col], v = reinterpret_cast<const float4*>(a.v)[col];
@@ -269,13 +271,16 @@ __global__ void __launch_bounds__(TPB) sq_norm_partial(const float4* __restrict_
   }
 }
 
-__global__ void __launch_bounds__(TPB) clip_coef_finish(const float* __restrict__ norm_part, int64_t K, float clip, float* __restrict__ coef_k) {
+// What a gradient with squared norm n2 is multiplied with; a zero gradient keeps its factor (clip / 0 = inf).
+__device__ __forceinline__ float clip_factor(float clip, float n2, bool nan_stays) { return nan_stays && n2 != n2 ? n2 : fminf(1.0f, clip / sqrtf(n2)); }
+
+__global__ void __launch_bounds__(TPB) clip_coef_finish(const float* __restrict__ norm_part, int64_t K, float clip, float* __restrict__ coef_k, bool nan_stays) {
   const int64_t k = (int64_t)blockIdx.x * TPB + threadIdx.x;
   if (k >= K) return;
   float n2 = 0.f;
 #pragma unroll
   for (int c = 0; c < NORM_CHUNKS; ++c) n2 += norm_part[k * NORM_CHUNKS + c];
-  coef_k[k] *= fminf(1.0f, clip / sqrtf(n2));      // a zero gradient keeps its factor (clip / 0 = inf)
+  coef_k[k] *= clip_factor(clip, n2, nan_stays);
 }
 
 // ---- clipping by global norm, summed and applied in one pass over a long queue ------------------------------------
@@ -461,7 +466,7 @@ __global__ void __launch_bounds__(CS_THREADS, 1) clip_sum_apply(const float4* __
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
       if (lane == 0) {
-        sh->coef[k % CS_DEPTH] = coef_k[k] * fminf(1.0f, clip / sqrtf(t));      // a zero gradient keeps its factor (clip / 0 = inf)
+        sh->coef[k % CS_DEPTH] = coef_k[k] * clip_factor(clip, t, Update::NAN_STAYS);
         mbar_arrive(&sh->coef_ready[k % CS_DEPTH]);
       }
     }
@@ -517,9 +522,9 @@ int launch_sum_apply(const SumApplyArgs& a, cudaStream_t st, Profiler* prof) {
   return a.adam.m ? run_sum_apply(a, n_split, q, tin, tout, rep, AdamW{a.adam}, st, prof) : run_sum_apply(a, n_split, q, tin, tout, rep, Sgd{}, st, prof);
 }
 
-int launch_clip_factors(const float* queue, int64_t K, float clip, float* coef_k, float* norm_part, cudaStream_t st, Profiler* prof) {
+int launch_clip_factors(const float* queue, int64_t K, float clip, bool nan_stays, float* coef_k, float* norm_part, cudaStream_t st, Profiler* prof) {
   TIMED(K_SQ_NORM, (sq_norm_partial<<<dim3(NORM_CHUNKS, (unsigned)K), TPB, 0, st>>>(reinterpret_cast<const float4*>(queue), norm_part)));
-  TIMED(K_COEF_FINISH, (clip_coef_finish<<<(unsigned)((K + TPB - 1) / TPB), TPB, 0, st>>>(norm_part, K, clip, coef_k)));
+  TIMED(K_COEF_FINISH, (clip_coef_finish<<<(unsigned)((K + TPB - 1) / TPB), TPB, 0, st>>>(norm_part, K, clip, coef_k, nan_stays)));
   return cudaGetLastError() == cudaSuccess ? 2 : -1;
 }
 

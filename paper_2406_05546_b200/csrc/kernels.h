@@ -281,7 +281,8 @@ constexpr int CLIP_EXCHANGE_BYTES = NORM_WORDS * CS_RING * CS_COPIES * 8;
 int configure_apply_kernels();
 bool clip_sum_fits(int sms);
 int launch_clip_sum_apply(const SumApplyArgs& a, float clip, uint64_t* words, uint32_t* status, cudaStream_t st, Profiler* prof);
-int launch_clip_factors(const float* queue, int64_t K, float clip, float* coef_k, float* norm_part, cudaStream_t st, Profiler* prof);
+// nan_stays: a norm that is NaN makes its factor NaN; otherwise the factor stays what it is.
+int launch_clip_factors(const float* queue, int64_t K, float clip, bool nan_stays, float* coef_k, float* norm_part, cudaStream_t st, Profiler* prof);
 
 // Evaluation pass: forward only, no dropout; loss [W] mean cross-entropy, argmax [W][b], correct [W] = samples whose
 // argmax equals the label.  Returns the number of kernels launched or -1.

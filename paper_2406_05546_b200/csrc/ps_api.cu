@@ -611,7 +611,7 @@ static int32_t apply_impl(ps_ctx* x, ps_mode mode, float lr, float scale, const 
   }
   const bool treated = clip_norm > 0.f || staleness_alpha > 0.f;
   auto clip_factors = [&]() -> int32_t {
-    int n = psk::launch_clip_factors(x->queue, K, clip_norm, x->coef_dev, x->norm_part, x->st, &x->prof);
+    int n = psk::launch_clip_factors(x->queue, K, clip_norm, adam != nullptr, x->coef_dev, x->norm_part, x->st, &x->prof);
     if (n < 0) return cuda_fail(cudaGetLastError(), "clipping launch");
     x->launches += n;
     return PS_OK;

@@ -430,6 +430,44 @@ def test_queue_in_order(K, treated):
 
 
 @gpu
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("mode", ["SYNC", "REPLAY", "ASYNC"])
+def test_queue_clipping_a_gradient_that_is_not_finite(bad, mode):
+    """Its factor is zero where its norm is infinite, as if the gradient were zero elsewhere, and NaN where it is NaN.  What SGD makes of it is unchanged:
+    a norm that is NaN clips nothing."""
+    where, fine = 5000, torch.arange(ps.P_PAD, device="cuda") < ps.P
+    results = []
+    for value in (bad, 0.0):
+        srv, _, _, m, v = server(3)
+        if value == 0.0:
+            srv.slot_tensor(1).zero_()
+        else:
+            srv.slot_tensor(1)[where] = value
+        enqueue(srv, 3, 3)
+        srv.ps_apply_adamw(getattr(ps, mode), m, v, step=2, clip_norm=0.5, **HYPER)
+        results.append((srv.head_tensor().clone(), m, v))
+        srv.close()
+    for got, want in zip(*results):
+        assert not got[ps.P:].any()
+        if math.isnan(bad):
+            assert torch.isnan(got[:ps.P]).all()
+        else:
+            assert torch.isnan(got[where])
+            fine[where] = False
+            assert torch.equal(got[fine], want[fine])
+    if math.isnan(bad):
+        srv, theta, rows, _, _ = server(1)
+        srv.slot_tensor(0)[where] = bad
+        enqueue(srv, 1, 1)
+        srv.ps_apply_stale(getattr(ps, mode), 1.0, clip_norm=0.5)
+        new = srv.head_tensor()[:ps.P].double()
+        fine = fine[:ps.P]
+        fine[where] = False
+        assert torch.isnan(new[where]) and ((new - (theta - rows[0])).abs() <= U * (theta - rows[0]).abs() * 1.01)[fine].all()
+        srv.close()
+
+
+@gpu
 def test_queue_padding_stays_zero():
     srv, theta, rows, m, v = server(3)
     m[ps.P:], v[ps.P:] = 1.0, 1.0
