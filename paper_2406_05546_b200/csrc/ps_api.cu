@@ -13,6 +13,7 @@
 #include <cstdio>
 #include <cstring>
 #include <new>
+#include <limits>
 #include <string>
 #include <vector>
 
@@ -761,7 +762,8 @@ int32_t ps_apply_adamw(ps_ctx* x, ps_mode mode, const ps_adamw_hyper* h, double 
   if (!m_dev || !v_dev || m_dev == v_dev || ((uintptr_t)m_dev & 15) != 0 || ((uintptr_t)v_dev & 15) != 0)
     return fail(PS_ERR_BAD_ARG, "m_dev and v_dev must be two 16-byte aligned device vectors of PS_PARAM_STRIDE floats");
   const AdamApply adam = {{h->lr, h->beta1, h->beta2, h->eps}, weight_decay, h->step, m_dev, v_dev};
-  return apply_impl(x, mode, 1.f, (float)(h->grad_scale * scale), order, (float)h->clip_norm, staleness_alpha, out, &adam);
+  const float clip = h->clip_norm > 0.0 ? std::max((float)h->clip_norm, std::numeric_limits<float>::denorm_min()) : 0.f;      // 0 would mean no clipping
+  return apply_impl(x, mode, 1.f, (float)(h->grad_scale * scale), order, clip, staleness_alpha, out, &adam);
 }
 
 int32_t ps_kill(ps_ctx* x, int32_t server) {

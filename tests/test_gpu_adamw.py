@@ -468,6 +468,22 @@ def test_queue_clipping_a_gradient_that_is_not_finite(bad, mode):
 
 
 @gpu
+@pytest.mark.parametrize("mode", ["SYNC", "ASYNC"])
+def test_queue_clipping_to_less_than_fp32_holds(mode):
+    """A clip_norm below the smallest fp32 value clips to nothing; it does not switch clipping off."""
+    results = []
+    for clip in (1e-60, 0.0):
+        srv, _, _, m, v = server(3)
+        if clip == 0.0:
+            srv.slot_tensor(0).view(1, -1).as_strided((3, ps.P_PAD), (ps.P_PAD, 1)).zero_()
+        enqueue(srv, 3, 3)
+        srv.ps_apply_adamw(getattr(ps, mode), m, v, step=2, clip_norm=clip, **HYPER)
+        results.append((srv.head_tensor().clone(), m, v))
+        srv.close()
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+
+
+@gpu
 def test_queue_padding_stays_zero():
     srv, theta, rows, m, v = server(3)
     m[ps.P:], v[ps.P:] = 1.0, 1.0
