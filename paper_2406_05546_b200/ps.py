@@ -339,7 +339,7 @@ class AdamW:
             cfg.arena, cfg.arena_bytes, cfg.stream = self.arena.data_ptr(), size.value, self.stream.cuda_stream
             self.stream.wait_stream(torch.cuda.current_stream())
             self._check(self.lib.ps_adamw_create(C.byref(cfg), table, n, C.byref(opt)))
-        self.opt, self._addr = opt, opt.value
+        self.opt, self._addr, self._lr_dev = opt, opt.value, None
 
     def _check(self, rc):
         if rc != 0:
@@ -350,6 +350,9 @@ class AdamW:
         if lr_dev is not None:
             import torch
             assert lr_dev.device == self.device and lr_dev.dtype == torch.float32 and lr_dev.numel() >= 1
+            if self._lr_dev is not lr_dev:
+                self._release([self._lr_dev] if self._lr_dev is not None else [])
+                self._lr_dev = lr_dev
             lr_dev = lr_dev.data_ptr()
         _marshal.adamw_step(self._addr, lr, beta1, beta2, eps, step, clip_norm, grad_scale, seed, lr_dev, skip_nonfinite)
 
@@ -362,7 +365,13 @@ class AdamW:
             if t.device != self.device or not t.is_contiguous() or t.dtype != g.dtype or t.numel() != p.numel():
                 raise ValueError("grads: contiguous tensors of the weights' device and sizes and the first gradients' type are wanted")
         self._check(self.lib.ps_adamw_set_grads(self.opt, (C.c_void_p * len(grads))(*[t.data_ptr() for t in grads])))
+        self._release(self.grads)
         self.grads = grads
+
+    def _release(self, tensors):
+        """Steps under way may still read these: their memory goes to no one else before the stream is past them."""
+        for t in tensors:
+            t.record_stream(self.stream)
 
     def ps_adamw_read_info(self):
         """counted_steps, skipped_steps, grad_norm, grad_factor; waits for the stream."""

@@ -171,6 +171,32 @@ def test_a_captured_step_counts_and_follows_its_schedule():
     del graph
 
 
+@gpu
+@pytest.mark.parametrize("what", ["grads", "lr_dev"])
+def test_replaced_tensors_stay_until_the_steps_that_read_them_are_done(what):
+    """The optimizer works on a stream of its own, which is behind; what a step there reads is replaced and let go, and the other stream allocates anew."""
+    n = 1 << 16
+    side = torch.cuda.Stream()
+    p, q = ([torch.ones(n, device="cuda")] for _ in range(2))
+    grads, lr = [torch.full((n,), 0.5, device="cuda")], torch.full((n,), 1e-3, device="cuda")
+    ref = AdamW(q, [grads[0].clone()])
+    ref.ps_adamw_step(lr=0.0, step=1, lr_dev=lr.clone())
+    opt, other_grads, other_lr = AdamW(p, grads, stream=side), [torch.full((n,), 3.0, device="cuda")], torch.zeros(n, device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(200_000_000)
+    opt.ps_adamw_step(lr=0.0, step=1, lr_dev=lr)
+    if what == "grads":
+        opt.ps_adamw_set_grads(other_grads)
+    else:
+        opt.ps_adamw_step(lr=0.0, step=2, lr_dev=other_lr)
+    del grads, lr
+    new = [torch.full((n,), -77.0, device="cuda") for _ in range(4)]
+    torch.cuda.synchronize()
+    # (a step with learning rate 0 changes no weight)
+    assert torch.equal(p[0], q[0]) and all((t == -77).all() for t in new)
+
+
 # ---- 8-bit moments, emulated ---------------------------------------------------------------------------------------------
 def philox(counter, key):
     """Philox4x32-10 on Python integers."""
