@@ -420,7 +420,8 @@ typedef struct {
 /* Size of the arena for these tensors (of which n and copy are read). */
 int32_t ps_adamw_query_bytes(const ps_adamw_config* cfg, const ps_adamw_tensor* tensors, int32_t n_tensors, uint64_t* arena_bytes);
 /* Lays the list out in the arena; synchronous.  Call it with the arena's device current.  Tensors need only their type's alignment; those that
- * start on 32 bytes (fp32), 16 (16 bits) or 8 (codes) are read in vectors.  Errors: PS_ERR_BAD_ARG, PS_ERR_ARENA_TOO_SMALL, PS_ERR_CUDA. */
+ * start on 32 bytes (fp32), 16 (16 bits) or 8 (codes) are read in vectors.  What a step writes may not share memory: a weight that two layers use is
+ * given once.  Errors: PS_ERR_BAD_ARG, PS_ERR_ARENA_TOO_SMALL, PS_ERR_CUDA. */
 int32_t ps_adamw_create(const ps_adamw_config* cfg, const ps_adamw_tensor* tensors, int32_t n_tensors, ps_adamw** out);
 int32_t ps_adamw_destroy(ps_adamw* opt);      /* synchronises the stream; frees host state only */
 /* Gives the following steps other gradients (host array [n_tensors] of dev pointers).  Not to be captured into a graph. */

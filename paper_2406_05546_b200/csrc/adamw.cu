@@ -482,6 +482,35 @@ int32_t check(const ps_adamw_config* c, const ps_adamw_tensor* t, int32_t n, boo
   return PS_OK;
 }
 
+// Two pieces that write the same memory would race: a tensor given twice, moments that two tensors share.
+int32_t check_written(const ps_adamw_config* c, const ps_adamw_tensor* t, int32_t n) {
+  struct Range { uintptr_t first, end; int32_t tensor; };
+  std::vector<Range> list;
+  try {
+    list.reserve((size_t)n * (c->state_bits == 8 ? 6 : 4));
+  } catch (const std::exception&) {
+    return fail(PS_ERR_BAD_ARG, "out of host memory");
+  }
+  const size_t state = c->state_bits == 32 ? 4 : 1;
+  for (int32_t i = 0; i < n; ++i) {
+    if (t[i].n == 0) continue;
+    auto add = [&](const void* p, size_t bytes) { if (p) list.push_back(Range{(uintptr_t)p, (uintptr_t)p + bytes, i}); };
+    const size_t count = (size_t)t[i].n, blocks = (count + BLOCK8 - 1) / BLOCK8;
+    add(t[i].param, count * type_size(c->param_type));
+    add(t[i].copy, count * 2);
+    add(t[i].m, count * state);
+    add(t[i].v, count * state);
+    if (c->state_bits == 8) {
+      add(t[i].m_scale, blocks);
+      add(t[i].v_scale, blocks);
+    }
+  }
+  std::sort(list.begin(), list.end(), [](const Range& a, const Range& b) { return a.first < b.first; });
+  for (size_t i = 1; i < list.size(); ++i)
+    if (list[i].first < list[i - 1].end) return fail(PS_ERR_BAD_ARG, "weights, copies or moments of tensors %d and %d share memory", list[i - 1].tensor, list[i].tensor);
+  return PS_OK;
+}
+
 uint64_t arena_layout(ps_adamw* o, void* base, int32_t n, int64_t pieces) {
   uint64_t at = 0;
   auto take = [&](uint64_t bytes) { const uint64_t a = (uint64_t)base + at; at = align256(at + bytes); return a; };
@@ -559,6 +588,7 @@ int32_t ps_adamw_create(const ps_adamw_config* cfg, const ps_adamw_tensor* tenso
   int64_t n_pieces = 0;
   int32_t rc = check(cfg, tensors, n_tensors, true, &n_pieces);
   if (rc != PS_OK) return rc;
+  if ((rc = check_written(cfg, tensors, n_tensors)) != PS_OK) return rc;
   if (!out) return fail(PS_ERR_BAD_ARG, "NULL argument");
   if (!cfg->arena || ((uint64_t)cfg->arena & 255) != 0) return fail(PS_ERR_BAD_ARG, "arena must be a 256-byte aligned device pointer");
   const uint64_t need = arena_layout(nullptr, nullptr, n_tensors, n_pieces);

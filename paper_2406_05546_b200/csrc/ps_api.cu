@@ -759,8 +759,9 @@ int32_t ps_apply_adamw(ps_ctx* x, ps_mode mode, const ps_adamw_hyper* h, double 
   if (!(weight_decay >= 0.0) || !std::isfinite(weight_decay)) return fail(PS_ERR_BAD_ARG, "weight_decay must be >= 0");
   if (!(staleness_alpha >= 0.f)) return fail(PS_ERR_BAD_ARG, "staleness_alpha must be >= 0");
   if (!std::isfinite(h->grad_scale) || !std::isfinite((float)(h->grad_scale * scale))) return fail(PS_ERR_BAD_ARG, "grad_scale and scale must be finite");
-  if (!m_dev || !v_dev || m_dev == v_dev || ((uintptr_t)m_dev & 15) != 0 || ((uintptr_t)v_dev & 15) != 0)
-    return fail(PS_ERR_BAD_ARG, "m_dev and v_dev must be two 16-byte aligned device vectors of PS_PARAM_STRIDE floats");
+  const uintptr_t m = (uintptr_t)m_dev, v = (uintptr_t)v_dev;
+  if (!m || !v || (m > v ? m - v : v - m) < psk::P_PAD * sizeof(float) || (m & 15) != 0 || (v & 15) != 0)
+    return fail(PS_ERR_BAD_ARG, "m_dev and v_dev must be two 16-byte aligned device vectors of PS_PARAM_STRIDE floats that share no memory");
   const AdamApply adam = {{h->lr, h->beta1, h->beta2, h->eps}, weight_decay, h->step, m_dev, v_dev};
   const float clip = h->clip_norm > 0.0 ? std::max((float)h->clip_norm, std::numeric_limits<float>::denorm_min()) : 0.f;      // 0 would mean no clipping
   return apply_impl(x, mode, 1.f, (float)(h->grad_scale * scale), order, clip, staleness_alpha, out, &adam);

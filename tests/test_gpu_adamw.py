@@ -551,7 +551,46 @@ def test_refusals():
     srv.close()
 
 
+@gpu
+def test_queue_moments_that_share_memory_are_refused():
+    srv, _, _, _, _ = server(2)
+    enqueue(srv, 2, 2)
+    both = torch.zeros(ps.P_PAD + 4, device="cuda")
+    for one, other in ((both[:-4], both[4:]), (both[4:], both[:-4])):
+        with pytest.raises(ps.PSError, match="PS_ERR_BAD_ARG"):
+            srv.ps_apply_adamw(ps.SYNC, one, other, **HYPER)
+    assert srv.ps_stats()["queue_len"] == 2 and srv.ps_stats()["version"] == 0
+    srv.close()
+
+
 # ---- without a GPU -------------------------------------------------------------------------------------------------------
+def test_shared_memory_is_refused():
+    """A tensor given twice, or moments that two share, would be stepped by two pieces at once.  (Nothing is launched: the addresses are never read.)"""
+    import ctypes as C
+    lib = ps.load()
+
+    def create(*places, bits=32):
+        """places: (n, param, copy, m, v, m_scale, v_scale)"""
+        cfg, t, opt = ps.AdamWConfig(), (ps.AdamWTensor * len(places))(), C.c_void_p()
+        cfg.state_bits, cfg.copy_type = bits, ps.TYPE_BF16
+        for a, (n, p, c, m, v, ms, vs) in zip(t, places):
+            a.n, a.param, a.grad, a.copy, a.m, a.v, a.m_scale, a.v_scale = n, p, 1 << 30, c, m, v, ms, vs
+        rc = lib.ps_adamw_create(C.byref(cfg), t, len(places), C.byref(opt))      # no arena: refused in any case, with a message of its own
+        text = lib.ps_last_error(None).decode()
+        assert rc == -1 and ("share memory" in text) != ("arena" in text)
+        return "share memory" in text
+    K = 1 << 20
+    one, two = (100, K, None, 2 * K, 3 * K, None, None), (100, 4 * K, None, 5 * K, 6 * K, None, None)
+    assert not create(one) and not create(one, two) and not create(one, (100, K + 400, None, 2 * K + 400, 3 * K + 400, None, None))
+    assert create(one, one) and create(one, two, (100, K + 396, None, 7 * K, 8 * K, None, None))
+    assert create((100, K, None, 2 * K, 2 * K, None, None)) and create((100, K, None, K, 2 * K, None, None)) and create((100, K, K, 2 * K, 3 * K, None, None))
+    assert create(one, (100, 4 * K, None, 2 * K, 6 * K, None, None)) and create(one, (100, 4 * K, None, 5 * K, 3 * K, None, None))
+    assert not create(one, (0, K, None, 2 * K, 3 * K, None, None))
+    small = (257, K, None, 2 * K, 3 * K, 4 * K, 5 * K)
+    assert not create(small, bits=8) and create((257, K, None, 2 * K, 2 * K + 256, 4 * K, 5 * K), bits=8) and create((257, K, None, 2 * K, 3 * K, 4 * K, 4 * K + 1), bits=8)
+    assert not create((257, K, None, 2 * K, 3 * K, 4 * K, 4 * K + 2), bits=8)
+
+
 def test_query_bytes_checks_its_arguments():
     import ctypes as C
     lib = ps.load()
