@@ -424,7 +424,8 @@ int32_t ps_adamw_query_bytes(const ps_adamw_config* cfg, const ps_adamw_tensor* 
  * given once.  Errors: PS_ERR_BAD_ARG, PS_ERR_ARENA_TOO_SMALL, PS_ERR_CUDA. */
 int32_t ps_adamw_create(const ps_adamw_config* cfg, const ps_adamw_tensor* tensors, int32_t n_tensors, ps_adamw** out);
 int32_t ps_adamw_destroy(ps_adamw* opt);      /* synchronises the stream; frees host state only */
-/* Gives the following steps other gradients (host array [n_tensors] of dev pointers).  Not to be captured into a graph. */
+/* Gives the following steps other gradients (host array [n_tensors] of dev pointers).  Not to be captured into a graph.  Errors: PS_ERR_BAD_ARG,
+ * PS_ERR_CUDA; the gradients stay what they were then. */
 int32_t ps_adamw_set_grads(ps_adamw* opt, const void* const* grads);
 /* One step.  Values in *h are read at the call: a step captured into a graph repeats them, so a graph gives step 0 (the device counts its own
  * steps, from 1, leaving out those that skip_nonfinite skips) and, for a schedule, lr_dev.  A given step does not touch that count.  One step of

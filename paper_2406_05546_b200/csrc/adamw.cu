@@ -532,6 +532,12 @@ int32_t upload_tensors(ps_adamw* o) {      // the copy's source is pageable: it 
   return e == cudaSuccess ? PS_OK : fail(PS_ERR_CUDA, "table upload: %s", cudaGetErrorString(e));
 }
 
+int32_t check_device(const ps_adamw* o) {
+  int device = -1;
+  if (cudaGetDevice(&device) == cudaSuccess && device == o->device) return PS_OK;
+  return fail(PS_ERR_BAD_ARG, "the optimizer lives on device %d, the current one is %d", o->device, device);
+}
+
 template <typename P, typename G, typename C, bool HAS_COPY>
 void launch_step(const ps_adamw* o, const Call& call, const DevState* state) {
   const int n = (int)o->n_pieces;
@@ -642,11 +648,25 @@ int32_t ps_adamw_set_grads(ps_adamw* o, const void* const* grads) {
   const size_t size = type_size(o->cfg.grad_type);
   for (size_t i = 0; i < o->host.size(); ++i)
     if (o->host[i].n > 0 && (!grads[i] || (uintptr_t)grads[i] % size)) return fail(PS_ERR_BAD_ARG, "gradient %zu is NULL or not aligned to its type", i);
-  for (size_t i = 0; i < o->host.size(); ++i) {
-    o->host[i].g = grads[i];
-    set_wide(o->cfg, o->host[i]);
+  int32_t rc = check_device(o);
+  if (rc != PS_OK) return rc;
+  cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+  if (cudaStreamIsCapturing(o->st, &capture) != cudaSuccess || capture != cudaStreamCaptureStatusNone)
+    return fail(PS_ERR_BAD_ARG, "ps_adamw_set_grads is not to be captured into a graph");
+  std::vector<DevTensor> now;
+  try {
+    now = o->host;
+  } catch (const std::exception&) {
+    return fail(PS_ERR_BAD_ARG, "out of host memory");
   }
-  return upload_tensors(o);
+  for (size_t i = 0; i < now.size(); ++i) {
+    now[i].g = grads[i];
+    set_wide(o->cfg, now[i]);
+  }
+  now.swap(o->host);
+  rc = upload_tensors(o);
+  if (rc != PS_OK) now.swap(o->host);
+  return rc;
 }
 
 int32_t ps_adamw_step(ps_adamw* o, const ps_adamw_hyper* h) {
@@ -654,8 +674,7 @@ int32_t ps_adamw_step(ps_adamw* o, const ps_adamw_hyper* h) {
   int32_t rc = check_adamw_hyper(h);
   if (rc != PS_OK) return rc;
   if (!std::isfinite(h->grad_scale)) return fail(PS_ERR_BAD_ARG, "grad_scale must be finite");
-  int device = -1;
-  if (cudaGetDevice(&device) != cudaSuccess || device != o->device) return fail(PS_ERR_BAD_ARG, "the optimizer lives on device %d, the current one is %d", o->device, device);
+  if ((rc = check_device(o)) != PS_OK) return rc;
   if (o->n_pieces == 0) return PS_OK;
   Call c;
   c.h = AdamHyper{h->lr, h->beta1, h->beta2, h->eps};

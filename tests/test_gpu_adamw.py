@@ -197,6 +197,32 @@ def test_replaced_tensors_stay_until_the_steps_that_read_them_are_done(what):
     assert torch.equal(p[0], q[0]) and all((t == -77).all() for t in new)
 
 
+@gpu
+def test_gradients_that_are_refused_change_nothing():
+    p, q = ([torch.ones(5000, device="cuda"), torch.ones(3, device="cuda")] for _ in range(2))
+    grads, others = ([torch.full((k,), s, device="cuda") for k in (5000, 3)] for s in (0.5, -0.5))
+    side = torch.cuda.Stream()
+    opt, ref = AdamW(p, grads, stream=side), AdamW(q, grads)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        with pytest.raises(ps.PSError, match="PS_ERR_BAD_ARG"):
+            opt.ps_adamw_set_grads(others)
+        opt.ps_adamw_step(step=1, **HYPER)      # the capture goes on
+    with pytest.raises(ValueError):
+        opt.ps_adamw_set_grads(others[:1])
+    with pytest.raises(ValueError):
+        opt.ps_adamw_set_grads(others[::-1])
+    graph.replay()
+    torch.cuda.synchronize()
+    opt.ps_adamw_step(step=2, **HYPER)
+    for t in (1, 2):
+        ref.ps_adamw_step(step=t, **HYPER)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(p, q))
+    del graph
+
+
 # ---- 8-bit moments, emulated ---------------------------------------------------------------------------------------------
 def philox(counter, key):
     """Philox4x32-10 on Python integers."""
