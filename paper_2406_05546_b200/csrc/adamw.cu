@@ -367,9 +367,10 @@ __device__ void finish_state(double total, bool has_norm, const Call& call, DevS
   st->s = adam_scalars(h, st->step, factor);
 }
 
-__global__ void adamw_begin(Call call, DevState* st) {
+// has_norm: of no gradients at all, zero
+__global__ void adamw_begin(bool has_norm, Call call, DevState* st) {
   pdl_enter();
-  finish_state(0.0, false, call, st);
+  finish_state(0.0, has_norm, call, st);
 }
 
 // The sum of all gradients' squares in fp64 (squares of fp32 values are exact in it), in an order that depends on the sizes alone; the CTA
@@ -675,24 +676,25 @@ int32_t ps_adamw_step(ps_adamw* o, const ps_adamw_hyper* h) {
   if (rc != PS_OK) return rc;
   if (!std::isfinite(h->grad_scale)) return fail(PS_ERR_BAD_ARG, "grad_scale must be finite");
   if ((rc = check_device(o)) != PS_OK) return rc;
-  if (o->n_pieces == 0) return PS_OK;
   Call c;
   c.h = AdamHyper{h->lr, h->beta1, h->beta2, h->eps};
   c.grad_scale = h->grad_scale; c.clip = h->clip_norm; c.lr_dev = h->lr_dev; c.step = h->step; c.seed = h->seed;
   c.skip_nonfinite = h->skip_nonfinite;
   const bool norm = h->clip_norm > 0.0 || h->skip_nonfinite, on_device = norm || h->step == 0 || h->lr_dev;
   c.s = on_device ? AdamScalars{} : adam_scalars(c.h, h->step, h->grad_scale);
-  if (norm) {
+  if (norm && o->n_pieces) {
     if (o->cfg.grad_type == PS_TYPE_FP32) launch_norm<float>(o, c);
     else if (o->cfg.grad_type == PS_TYPE_BF16) launch_norm<__nv_bfloat16>(o, c);
     else launch_norm<__half>(o, c);
   } else if (on_device) {
-    launch_pdl(adamw_begin, dim3(1), 1, 0, o->st, c, o->state);
+    launch_pdl(adamw_begin, dim3(1), 1, 0, o->st, norm, c, o->state);
   }
   const DevState* state = on_device ? o->state : nullptr;
-  if (o->cfg.param_type == PS_TYPE_FP32) launch_grad<float>(o, c, state);
-  else if (o->cfg.param_type == PS_TYPE_BF16) launch_grad<__nv_bfloat16>(o, c, state);
-  else launch_grad<__half>(o, c, state);
+  if (o->n_pieces) {      // the steps of a list without elements are counted, and that is all
+    if (o->cfg.param_type == PS_TYPE_FP32) launch_grad<float>(o, c, state);
+    else if (o->cfg.param_type == PS_TYPE_BF16) launch_grad<__nv_bfloat16>(o, c, state);
+    else launch_grad<__half>(o, c, state);
+  }
   const cudaError_t e = cudaGetLastError();
   return e == cudaSuccess ? PS_OK : fail(PS_ERR_CUDA, "adamw launch: %s", cudaGetErrorString(e));
 }

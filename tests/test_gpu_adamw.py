@@ -223,6 +223,16 @@ def test_gradients_that_are_refused_change_nothing():
     del graph
 
 
+@gpu
+@pytest.mark.parametrize("bits", [32, 8])
+def test_steps_of_a_list_without_elements_count(bits):
+    empty = lambda: [torch.empty(0, device="cuda")]
+    opt = AdamW(empty(), empty(), state_bits=bits)
+    for more in (dict(step=0), dict(step=0, clip_norm=1.0), dict(step=0, skip_nonfinite=True), dict(step=5, clip_norm=1.0), dict(step=6)):
+        opt.ps_adamw_step(**more, **HYPER)
+    assert opt.ps_adamw_read_info() == {"counted_steps": 3, "skipped_steps": 0, "grad_norm": 0.0, "grad_factor": 1.0}
+
+
 # ---- 8-bit moments, emulated ---------------------------------------------------------------------------------------------
 def philox(counter, key):
     """Philox4x32-10 on Python integers."""
