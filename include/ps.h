@@ -445,6 +445,8 @@ int32_t ps_adamw_read_info(ps_adamw* opt, ps_adamw_info* out);      /* synchroni
  * written.  BF16 or FP16 operands, FP32 accumulation, every result rounded once.  Matrices have their columns next to each other and any pitch
  * (elements from row to row) not below their width.  x, weight and dy are read by tile copies, which want a base on 16 bytes and pitches and
  * strides that are multiples of 8: others are first laid out anew in the workspace (workers_dense_workspace says how much; 0 if nothing has to be).
+ * Activations are computed in FP32, of a sum z that is not rounded yet: GELU within 2^-19 + z^2 2^-22 of its value, SiLU within 2^-19 + |z| 2^-22 of its own
+ * (values below 2^-110 may come out as zero), their derivatives within 2^-20 + 2^-22 |z|.
  * rows and weight_of are read at the call, so a captured graph repeats them; everything on the device must stay until the work is done.  The
  * entry points keep nothing between calls and may be used from several threads and streams at once, each call with its own workspace. */
 enum { PS_ACT_NONE = 0, PS_ACT_RELU = 1, PS_ACT_GELU = 2 /* z (1 + erf(z / sqrt 2)) / 2 */, PS_ACT_SILU = 3 /* z / (1 + e^-z) */ };

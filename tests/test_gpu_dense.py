@@ -492,6 +492,32 @@ def test_weight_gradients_past_32_bits():
         assert ((dw[g][-64:].double() - want).abs() <= half_step(want, torch.bfloat16) * 1.01).all()
 
 
+@gpu
+@pytest.mark.parametrize("kind", ["bf16", "fp16"])
+@pytest.mark.parametrize("activation", ["gelu", "silu"])
+def test_activations_keep_their_digits(kind, activation):
+    """The values of a 16-bit type through an identity matrix: a sum is one product and exact, so that only the activation's own error is left, within what the
+    header states (relative, in the tails too)."""
+    t = TYPES[kind]
+    z = torch.arange(65536, device="cuda").to(torch.int32).to(torch.int16).view(t)
+    z = z[torch.isfinite(z) & (z.abs() < 1000)]
+    z = torch.cat([z, z.new_zeros(-z.numel() % 64)]).view(-1, 64)
+    M = z.shape[0]
+    eye, rows = torch.eye(64, device="cuda", dtype=t).view(1, 64, 64), [M]
+    y = workers_dense_forward(z, eye, rows, activation=activation, out_dtype=torch.float32)
+    zd = z.double()
+    want = act(zd, activation)
+    grow = zd.square() if activation == "gelu" else zd.abs()
+    assert ((y.double() - want).abs() <= want.abs() * (2.0 ** -19 + grow * 2.0 ** -22) + 2.0 ** -110).all()
+    # the derivative, through a gradient of one: its 16-bit result is rounded once
+    dy, dz = torch.zeros(M, 64, device="cuda", dtype=t), torch.empty_like(z)
+    workers_dense_backward(dy, z, eye, rows, x_pre=z, activation=activation, dx_add=torch.ones_like(z), dx_pre=dz)
+    workers_dense_status()
+    want = slope(zd, activation)
+    e = 2.0 ** -20 + 2.0 ** -22 * zd.abs()
+    assert ((dz.double() - want).abs() <= e + half_step(want.abs() + e, t)).all()
+
+
 def backward_within(limit, dy, x, w, rows, dw):
     """dw of a backward call whose waits end after `limit` clocks."""
     counts, G, N, K = np.array(rows, dtype=np.int32), len(rows), dy.shape[1], x.shape[1]
