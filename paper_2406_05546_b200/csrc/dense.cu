@@ -6,7 +6,7 @@
 // Every operand is read as it lies, with k contiguous or its row index contiguous (128-byte swizzle, blocks of 64), and every result is
 // rounded once, in the epilogue that also does everything elementwise.
 //
-// Tiles, by the work there is (the rules are in run_rows and run_weights):
+// Tiles, by the work there is (the rules are in plan_rows and plan_weights):
 //   Pair   256 x 256 by two CTAs that share each MMA (cta_group::2): half of the right operand each, so that a CTA brings in 32 KB for
 //          128 x 256 x 64 products.  Two accumulators of 256 columns are used in turn: one is read out while the other fills.
 //   Single 128 x 256 by one CTA: workers with less than 256 rows.
@@ -1415,65 +1415,62 @@ int split_for(int64_t tiles, int blocks, int room) {
   return split;
 }
 
-// Forward and input gradient: rows of groups x `features` columns, reduction over `red`.
-template <int OP>
-int32_t run_rows(Problem& p, int features, int red) {
-  DenseTab& tab = p.tab;
+// The tiles of a product, in numbers that tests ask for as well (dense_plan).
+enum { PLAN_TOO_MANY = -1, PLAN_PAIR = 0, PLAN_SINGLE = 1, PLAN_THIN = 2, PLAN_SPLIT = 3, PLAN_FEW16 = 4, PLAN_FEW32 = 5, PLAN_FEW64 = 6 };
+struct Plan { int tiles, split; bool drain; };
+
+// Forward and input gradient: rows of groups x `features` columns, reduction over `red`.  Fills in the tiles' numbers and the groups' prefix sums.
+Plan plan_rows(int op, DenseTab& tab, DenseArgs& a, const DenseEpi& epi, int features, int red, int sms) {
   int most = 0;
   int64_t rows = 0;
   for (int g = 0; g < tab.groups; ++g) {
     most = std::max(most, tab.row1[g] - tab.row0[g]);
     rows += tab.row1[g] - tab.row0[g];
   }
-  const int blocks = div_up(red, BK), sms = g_sm_count;
-  DenseArgs& a = p.args;
+  const int blocks = div_up(red, BK);
   a.n_side = features;
   a.red = red;
   a.rows = (int32_t)rows;
-  const bool drain = blocks > drain_blocks(p.epi);      // a shorter sum takes one accumulator either way
+  const bool drain = blocks > drain_blocks(epi);      // a shorter sum takes one accumulator either way
   if (rows <= 48ll * tab.groups) {
     const int bn = most <= 16 ? 16 : (most <= 32 ? 32 : 64);
     a.n_tiles_n = div_up(features, BM);
     const int64_t t = cut_rows(tab, bn, false, a.n_tiles_n);
-    if (t >= 1 << 30) return fail(PS_ERR_BAD_ARG, "too many tiles");
+    if (t >= 1 << 30) return {PLAN_TOO_MANY, 1, false};
     a.n_tiles = (int)t;
-    const int split = split_for(t, blocks, 2 * sms);
-    if (bn == 16) return launch<Few<OP, 16>>(p, split);
-    if (bn == 32) return launch<Few<OP, 32>>(p, split);
-    return launch<Few<OP, 64>>(p, split);
+    return {bn == 16 ? PLAN_FEW16 : (bn == 32 ? PLAN_FEW32 : PLAN_FEW64), split_for(t, blocks, 2 * sms), drain};
   }
   // Thin tiles lack the registers to turn pieces of 16 bytes: such rows go to the others (us, 8,192 x 200 -> 5000 with pre: Thin 124, Pair 81; with everything
   // 142, 114); rows that go by columns stay (8,192 x 200 -> 4999 with everything: Thin 118, Pair 163).
-  if constexpr (OP == D_FWD) {
+  if (op == D_FWD) {
     a.n_tiles_n = div_up(features, 128);
     const int64_t row_blocks = cut_rows(tab, BM, false), t = row_blocks * a.n_tiles_n;
-    if (red <= THIN_RED_FWD && (p.epi.wide || !p.epi.rows) && t > sms && t < 1 << 30) {
+    if (red <= THIN_RED_FWD && (epi.wide || !epi.rows) && t > sms && t < 1 << 30) {
       a.m_tiles = (int)row_blocks;
       a.n_tiles = (int)t;
-      return launch<Thin<OP>>(p, 1);
+      return {PLAN_THIN, 1, false};
     }
   }
   a.n_tiles_n = div_up(features, 256);
   const int64_t row_blocks = cut_rows(tab, BM, false), pairs = cut_rows(tab, BM, true), singles = row_blocks * a.n_tiles_n;
-  if (singles >= 1 << 30) return fail(PS_ERR_BAD_ARG, "too many tiles");
+  if (singles >= 1 << 30) return {PLAN_TOO_MANY, 1, false};
   if (pairs * a.n_tiles_n * 2 >= sms && pairs * 10 <= row_blocks * 6) {
     a.m_tiles = (int)pairs;
     a.n_tiles = (int)pairs * a.n_tiles_n;
-    return drain ? launch<Pair<OP, true>>(p, 1) : launch<Pair<OP, false>>(p, 1);
+    return {PLAN_PAIR, 1, drain};
   }
   a.m_tiles = (int)row_blocks;
   if (singles * 3 >= sms * 2 || row_blocks * div_up(features, 128) > sms) {
     a.n_tiles = (int)singles;
-    return drain ? launch<Single<OP, true>>(p, 1) : launch<Single<OP, false>>(p, 1);
+    return {PLAN_SINGLE, 1, drain};
   }
   a.n_tiles_n = div_up(features, 128);
   a.n_tiles = (int)row_blocks * a.n_tiles_n;
-  return launch<Split<OP>>(p, split_for(a.n_tiles, blocks, sms));
+  return {PLAN_SPLIT, split_for(a.n_tiles, blocks, sms), drain};
 }
 
-int32_t run_weights(Problem& p, int N, int K) {
-  DenseTab& tab = p.tab;
-  DenseArgs& a = p.args;
+// Weight gradient: N x K for every worker, reduction over its rows.
+Plan plan_weights(DenseTab& tab, DenseArgs& a, const DenseEpi& epi, int N, int K, int sms) {
   int most = 0;
   int64_t rows = 0;
   for (int g = 0; g < tab.groups; ++g) {
@@ -1481,29 +1478,43 @@ int32_t run_weights(Problem& p, int N, int K) {
     rows += tab.row1[g] - tab.row0[g];
   }
   const bool few = most <= THIN_RED_DW || (most <= THIN_MOST_DW && rows <= (int64_t)THIN_MEAN_DW * tab.groups);
-  const bool drain = div_up(most, BK) > drain_blocks(p.epi);
-  const int sms = g_sm_count;
+  const bool drain = div_up(most, BK) > drain_blocks(epi);
   a.m_side = N; a.n_side = K; a.red = 0;
   auto tiles = [&](int tm) { a.m_tiles = div_up(N, tm); return (int64_t)tab.groups * a.m_tiles * a.n_tiles_n; };
   a.n_tiles_n = div_up(K, 128);
   if (few && tiles(128) > sms && tiles(128) < 1 << 30) {
     a.n_tiles = (int)tiles(128);
-    return launch<Thin<D_DW>>(p, 1);
+    return {PLAN_THIN, 1, false};
   }
   a.n_tiles_n = div_up(K, 256);
   const int64_t pairs = tiles(256), singles = tiles(128);
-  if (singles >= 1 << 30) return fail(PS_ERR_BAD_ARG, "too many tiles");
+  if (singles >= 1 << 30) return {PLAN_TOO_MANY, 1, false};
   if (pairs * 2 >= sms && pairs * 2 <= singles + singles / 5) {
     a.n_tiles = (int)tiles(256);
-    return drain ? launch<Pair<D_DW, true>>(p, 1) : launch<Pair<D_DW, false>>(p, 1);
+    return {PLAN_PAIR, 1, drain};
   }
   if (singles * 3 >= sms * 2 || singles / a.n_tiles_n * div_up(K, 128) > sms) {
     a.n_tiles = (int)tiles(128);
-    return drain ? launch<Single<D_DW, true>>(p, 1) : launch<Single<D_DW, false>>(p, 1);
+    return {PLAN_SINGLE, 1, drain};
   }
   a.n_tiles_n = div_up(K, 128);
   a.n_tiles = (int)tiles(128);
-  return launch<Split<D_DW>>(p, split_for(a.n_tiles, div_up(most, BK), sms));
+  return {PLAN_SPLIT, split_for(a.n_tiles, div_up(most, BK), sms), drain};
+}
+
+template <int OP>
+int32_t run(Problem& p, const Plan& plan) {
+  if (plan.tiles == PLAN_TOO_MANY) return fail(PS_ERR_BAD_ARG, "too many tiles");
+  if (plan.tiles == PLAN_PAIR) return plan.drain ? launch<Pair<OP, true>>(p, 1) : launch<Pair<OP, false>>(p, 1);
+  if (plan.tiles == PLAN_SINGLE) return plan.drain ? launch<Single<OP, true>>(p, 1) : launch<Single<OP, false>>(p, 1);
+  if constexpr (OP != D_DX)
+    if (plan.tiles == PLAN_THIN) return launch<Thin<OP>>(p, 1);
+  if constexpr (OP != D_DW) {
+    if (plan.tiles == PLAN_FEW16) return launch<Few<OP, 16>>(p, plan.split);
+    if (plan.tiles == PLAN_FEW32) return launch<Few<OP, 32>>(p, plan.split);
+    if (plan.tiles == PLAN_FEW64) return launch<Few<OP, 64>>(p, plan.split);
+  }
+  return launch<Split<OP>>(p, plan.split);
 }
 
 // The groups that have rows, by their weights; those that follow one another, in that order and in memory, are one.
@@ -1527,6 +1538,15 @@ void sort_groups(const int32_t* rows, const int32_t* weight_of, int groups, Dens
     tab.w[g] = (uint16_t)list[g].w;
     tab.row0[g] = list[g].row0;
     tab.row1[g] = list[g].row1;
+  }
+}
+
+// All groups, each by itself (weight gradient, bias gradient).
+void list_workers(const int32_t* rows, int groups, DenseTab& tab) {
+  tab.groups = groups;
+  for (int g = 0; g < groups; ++g) {
+    tab.row0[g] = g ? tab.row1[g - 1] : 0;
+    tab.row1[g] = tab.row0[g] + rows[g];
   }
 }
 
@@ -1603,6 +1623,21 @@ int list_used(DenseTab& tab) {
 
 }  // namespace
 
+// What a call on a device of `sms` SMs would take: the tiles (PLAN_*), + 16 where sums are drained, + 32 * log2 of the CTAs that share a tile.  wide: bytes that
+// its results' rows are moved in (32, 16, or 0 for columns).
+int dense_plan(int op, const int32_t* rows, const int32_t* weight_of, int groups, int N, int K, int fp32, int bf16, int wide, int sms) {
+  DenseTab tab = {};
+  DenseArgs a = {};
+  DenseEpi e = {};
+  e.out0_fp32 = fp32; e.bf16 = bf16; e.wide = wide == 32; e.rows = wide != 0;
+  if (op == D_DW) list_workers(rows, groups, tab);
+  else sort_groups(rows, weight_of, groups, tab);
+  const Plan p = op == D_DW ? plan_weights(tab, a, e, N, K, sms) : plan_rows(op, tab, a, e, op == D_FWD ? N : K, op == D_FWD ? K : N, sms);
+  int shared = 0;
+  while (1 << shared < p.split) ++shared;
+  return p.tiles + (p.drain ? 16 : 0) + 32 * shared;
+}
+
 }  // namespace psk
 
 using namespace psk;
@@ -1671,7 +1706,7 @@ int32_t workers_dense_forward(const ps_dense_layer* l, const ps_dense_output* o)
   e.out1 = o->pre; e.out1_pitch = o->pre_pitch;
   e.act = l->activation; e.bf16 = l->type == PS_TYPE_BF16;
   set_moves(e, N, {{o->residual, o->residual_pitch, 0, 2}, {o->y, o->y_pitch, 0, ys}, {o->pre, o->pre_pitch, 0, 2}});
-  return run_rows<D_FWD>(p, N, K);
+  return run<D_FWD>(p, plan_rows(D_FWD, p.tab, p.args, e, N, K, g_sm_count));
 }
 
 static int32_t backward(const ps_dense_layer* l, const ps_dense_gradients* o, int64_t limit) {
@@ -1712,11 +1747,7 @@ static int32_t backward(const ps_dense_layer* l, const ps_dense_gradients* o, in
     return ce == cudaSuccess ? PS_OK : fail(PS_ERR_CUDA, "clearing gradients: %s", cudaGetErrorString(ce));
   }
   DenseTab workers = {};
-  workers.groups = l->groups;
-  for (int g = 0; g < l->groups; ++g) {
-    workers.row0[g] = g ? workers.row1[g - 1] : 0;
-    workers.row1[g] = workers.row0[g] + l->rows[g];
-  }
+  list_workers(l->rows, l->groups, workers);
   if (o->db) {
     ColumnSumArgs c = {};
     c.dy = dy.p; c.db = o->db; c.pitch = dy.pitch; c.db_stride = o->db_stride;
@@ -1743,7 +1774,7 @@ static int32_t backward(const ps_dense_layer* l, const ps_dense_gradients* o, in
     set_moves(e, K, {{o->dx_add, o->dx_add_pitch, 0, 2}, {o->dx_pre ? o->x_pre : nullptr, o->x_pre_pitch, 0, 2}, {o->dx, o->dx_pitch, 0, 2}, {o->dx_pre, o->dx_pre_pitch, 0, 2}});
     p.limit = limit;
     p.args.join = !o->db ? JOIN_FIRST : (o->dw ? JOIN_BETWEEN : JOIN_LAST);
-    if ((rc = run_rows<D_DX>(p, K, N)) != PS_OK) return rc;
+    if ((rc = run<D_DX>(p, plan_rows(D_DX, p.tab, p.args, e, K, N, g_sm_count))) != PS_OK) return rc;
   }
   if (o->dw) {
     Problem p = {};
@@ -1757,7 +1788,7 @@ static int32_t backward(const ps_dense_layer* l, const ps_dense_gradients* o, in
     set_moves(e, K, {{o->dw, o->dw_pitch, l->groups > 1 ? o->dw_stride : 0, ds}});
     p.limit = limit;
     p.args.join = o->db || o->dx || o->dx_pre ? JOIN_LAST : JOIN_FIRST;
-    if ((rc = run_weights(p, N, K)) != PS_OK) return rc;
+    if ((rc = run<D_DW>(p, plan_weights(p.tab, p.args, e, N, K, g_sm_count))) != PS_OK) return rc;
   }
   return PS_OK;
 }

@@ -227,6 +227,64 @@ def test_rows_on_sixteen_and_on_thirty_two_bytes(shape, pad, kind, wide_results)
         one_backward(shape, kind, "silu", True, True, True, wide_results, accumulate, pad=(pad,) * 4, extra=3)
 
 
+# Every tile shape of every product, with and without its sums handed over on the way (+): the shapes that a device of 148 SMs takes are asked for, so that a
+# change of the rules cannot leave one out unseen.  (shape, operands, forward in 16 bits and FP32, input gradient, weight gradient in 16 bits and FP32)
+PLANS = [
+    (([128, 100, 77, 0, 64] * 12, 60, None, 648, 1032), "bf16", "Single", "Single+", "Single", "Thin", "Thin"),      # many workers on weights of their own
+    (([128, 100, 77, 0, 64] * 12, 60, None, 648, 1027), "fp16", "Single", "Single+", "Single", "Thin", "Thin"),
+    (([200, 1, 2, 3, 1, 1, 0, 1, 1], 9, None, 520, 264), "bf16", "Few64/4", "Few64+/4", "Few64/2", "Split", "Split"),      # one worker with more rows than a tile has
+    (([100, 30, 90, 70, 1, 2, 0, 1], 3, [0, 1, 0, 2, 0, 1, 2, 2], 1096, 328), "fp16", "Few64/8", "Few64+/8", "Few64/2", "Thin", "Thin"),
+    (([900, 1000, 530, 1], 4, None, 1288, 1416), "bf16", "Single", "Single+", "Single", "Pair", "Pair+"),
+    (([600, 520, 700], 3, None, 1032, 1000), "fp16", "Split", "Split+", "Split", "Single", "Single+"),
+    (([2701, 2299], 2, None, 776, 1032), "fp16", "Pair", "Pair+", "Pair", "Split", "Split+"),
+    (([1300], 1, None, 8200, 1032), "fp16", "Split+", "Split+", "Pair", "Pair", "Pair+"),      # reductions past 8,192 in FP16
+    (([2600], 1, None, 8200, 2056), "fp16", "Pair+", "Pair+", "Pair", "Pair", "Pair+"),
+    (([2600], 1, None, 2056, 8200), "fp16", "Pair", "Pair+", "Pair+", "Pair", "Pair+"),
+    (([128, 100, 77, 0, 64] * 8, 40, None, 648, 8200), "fp16", "Single", "Single+", "Single+", "Thin", "Thin"),
+    (([300], 1, None, 400, 8200), "fp16", "Single", "Single", "Split+/8", "Single", "Single"),
+    (([3, 0, 2], 3, None, 8200, 200), "fp16", "Few16+/8", "Few16+/8", "Few16/2", "Thin", "Thin"),
+    (([30, 0, 25], 3, None, 8200, 200), "fp16", "Few32+/8", "Few32+/8", "Few32/2", "Thin", "Thin"),
+]
+plan_id = lambda p: f"{len(p[0][0])}x{sum(p[0][0])}-{p[0][3]}-{p[0][4]}-{p[1]}"
+
+
+def plan(op, shape, kind, fp32, wide):
+    """The tiles that a call takes, and how many CTAs share one."""
+    f = ps.load()["_ZN3psk10dense_planEiPKiS1_iiiiiii"]
+    f.restype, f.argtypes = C.c_int, [C.c_int, C.c_void_p, C.c_void_p] + [C.c_int] * 7
+    rows, _, weight_of, K, N = shape
+    r, w = np.array(rows, dtype=np.int32), np.array(weight_of if weight_of else range(len(rows)), dtype=np.int32)
+    code = f(op, r.ctypes.data, w.ctypes.data, len(rows), N, K, int(fp32), int(kind == "bf16"), wide, 148)
+    return ["Pair", "Single", "Thin", "Split", "Few16", "Few32", "Few64"][code % 16] + ("+" if code & 16 else "") + (f"/{1 << (code >> 5)}" if code >> 5 else "")
+
+
+@pytest.mark.parametrize("entry", PLANS, ids=plan_id)
+@pytest.mark.parametrize("wide", [32, 16, 0])
+def test_planned_tiles(entry, wide):
+    shape, kind, *want = entry
+    got = [plan(0, shape, kind, False, wide), plan(0, shape, kind, True, wide), plan(1, shape, kind, False, wide), plan(2, shape, kind, False, wide), plan(2, shape, kind, True, wide)]
+    assert got == want
+
+
+def test_planned_tiles_leave_no_shape_out():
+    seen = {(op, w.split("/")[0]) for _, _, *want in PLANS for op, w in zip("ffxww", want)}
+    assert seen >= {(op, name) for op in "fxw" for name in ("Pair", "Pair+", "Single", "Single+", "Split")} | {("w", "Split+"), ("f", "Split+"), ("x", "Split+"), ("w", "Thin")}
+    assert seen >= {("f", "Few16+"), ("f", "Few32+"), ("f", "Few64"), ("f", "Few64+"), ("x", "Few16"), ("x", "Few32"), ("x", "Few64")}
+    assert plan(0, SHAPES[7], "bf16", False, 32) == plan(0, SHAPES[8], "fp16", True, 0) == "Thin" and plan(0, SHAPES[0], "bf16", False, 32) == "Few16"
+
+
+@gpu
+@pytest.mark.parametrize("entry", PLANS, ids=plan_id)
+@pytest.mark.parametrize("pad", [(0, 0, 0, 0), (8, 8, 8, 8), (1, 2, 3, 5)], ids=str)
+def test_every_tile_shape(entry, pad):
+    shape, kind = entry[:2]
+    for wide_results in (False, True):
+        one_forward(shape, kind, "gelu", True, True, True, wide_results, pad=pad, extra=3)
+        one_backward(shape, kind, "silu", True, True, True, wide_results, accumulate=int(wide_results), pad=pad, extra=3)
+    one_forward(shape, kind, "none", False, False, False, False, pad=pad)
+    one_backward(shape, kind, "relu", False, True, False, True, pad=pad)
+
+
 @gpu
 @pytest.mark.parametrize("rows", [[70, 5, 0, 33, 200], [1000, 1, 77]])
 @pytest.mark.parametrize("N,K", [(136, 200), (2048, 2304)])
