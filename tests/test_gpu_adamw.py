@@ -546,6 +546,56 @@ def test_queue_clipping_to_less_than_fp32_holds(mode):
 
 
 @gpu
+@pytest.mark.parametrize("rows", [[64, 9, 0, 130], [16] * 6])
+@pytest.mark.parametrize("mode", ["SYNC", "ASYNC"])
+def test_the_dense_layer_writes_where_the_servers_step_reads(rows, mode):
+    """The CNN's dense layer, 1568 -> 512, on the workers' own batches: its weight and bias gradients go straight into the workers' rows of the gradient queue,
+    beside what other layers have put there, and the server's step takes them from there; the next forward call reads the new weights."""
+    F1W, F1B, K, N, G = 4800, 807616, 1568, 512, len(rows)
+    srv, theta, other, m, v = server(G)
+    gen = torch.Generator("cuda").manual_seed(3)
+    M = sum(rows)
+    x, dy = torch.randn(M, K, generator=gen, device="cuda").bfloat16(), (torch.randn(M, N, generator=gen, device="cuda") * 0.02).bfloat16()
+    layer = lambda: srv.head_tensor()[F1W:F1W + N * K].view(1, N, K).bfloat16()
+    queue = torch.as_strided(srv.slot_tensor(0), (G, ps.P_PAD), (ps.P_PAD, 1))
+    at = lambda first, shape, strides: torch.as_strided(queue, shape, strides, queue.storage_offset() + first)
+    ps.workers_dense_backward(dy, x, layer(), rows, [0] * G, dw=at(F1W, (G, N, K), (ps.P_PAD, K, 1)), db=at(F1B, (G, N), (ps.P_PAD, 1)))
+    ps.workers_dense_status()
+    grads = queue[:, :ps.P].double()
+    first = 0
+    for g, n in enumerate(rows):
+        gx, gy = x[first:first + n].double(), dy[first:first + n].double()
+        first += n
+        want = other[g].clone()
+        want[F1W:F1W + N * K], want[F1B:F1B + N] = (gy.T @ gx).view(-1), gy.sum(0)
+        bound = torch.zeros_like(want)      # an accumulator drops less than 2^-22 of its terms a time, sixteen products each; the result is rounded once
+        bound[F1W:F1W + N * K], bound[F1B:F1B + N] = (gy.abs().T @ gx.abs()).view(-1), gy.abs().sum(0)
+        near(queue[g, :ps.P], want, bound * (n / 16 + 2) * 2.0 ** -22 + (bound > 0) * want.abs() * 2.0 ** -23)
+    assert not queue[:, ps.P:].any()
+    m0, v0 = m[:ps.P].cpu().numpy(), v[:ps.P].cpu().numpy()
+    enqueue(srv, G, G)
+    srv.ps_apply_adamw(getattr(ps, mode), m, v, step=3, weight_decay=0.1, **HYPER)
+    head = srv.head_tensor()[:ps.P]
+    if mode == "ASYNC":
+        p = theta.float().cpu().numpy()
+        bound = 0.0
+        for j in range(G):
+            p, m0, v0, step = fp32_update(p, grads[j].float().cpu().numpy(), m0, v0, 3 + j, 0.1)
+            bound = bound + 4 * U * np.abs(p) + 24 * U * step      # as in test_queue_in_order
+        assert (np.abs(head.cpu().numpy() - p) <= bound).all()
+    else:
+        new, em, ev, e_p, _, _ = formula(theta, grads.mean(0), torch.from_numpy(m0).cuda().double(), torch.from_numpy(v0).cuda().double(), 3, 0.1)
+        e_g, d = (G / 8 + 25) * U * grads.abs().mean(0), (ev / (1 - 0.999 ** 3)).sqrt() + 1e-8      # as in test_queue_summed
+        near(head, new, e_p + 2e-3 / (1 - 0.9 ** 3) * (0.1 * e_g / d + em.abs() / d * (0.001 * (2 * grads.mean(0).abs() + e_g) * e_g / ev)))
+    w = layer()
+    y = ps.workers_dense_forward(x, w, rows, [0] * G, out_dtype=torch.float32)
+    terms = x.double().abs() @ w[0].double().abs().T
+    assert torch.equal(w[0].view(-1), head[F1W:F1W + N * K].bfloat16())
+    near(y, x.double() @ w[0].double().T, terms * (32 + K / 512 + 12) * 2.0 ** -22)
+    srv.close()
+
+
+@gpu
 def test_queue_padding_stays_zero():
     srv, theta, rows, m, v = server(3)
     m[ps.P:], v[ps.P:] = 1.0, 1.0
