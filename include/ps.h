@@ -482,6 +482,7 @@ typedef struct {
 } ps_dense_output;
 
 /* pre = x W^T + bias ;  y = activation(pre) + residual  (of the sum before it is rounded to pre).
+ * No output may overlap an input or another output, but for y (of the operands' type) and residual, which may be the same matrix.
  * Errors: PS_ERR_BAD_ARG, PS_ERR_ARENA_TOO_SMALL (workspace), PS_ERR_CUDA; nothing of the product is launched then. */
 int32_t workers_dense_forward(const ps_dense_layer* layer, const ps_dense_output* out);
 
@@ -506,7 +507,7 @@ typedef struct {
 
 /* dx = dy W + dx_add ;  dx_pre = dx * activation'(x_pre)  (of dx before it is rounded; with PS_ACT_RELU zero wherever x_pre is not above zero) ;
  * dw_g = dy_g^T x_g and db_g = the column sums of dy_g over the rows of group g, zero for a group without rows.  Each may be left out (NULL).
- * No output may overlap an input, but for dx and dx_add.  Errors as workers_dense_forward. */
+ * No output may overlap an input or another output, but for dx and dx_add, which may be the same matrix.  Errors as workers_dense_forward. */
 int32_t workers_dense_backward(const ps_dense_layer* layer, const ps_dense_gradients* out);
 
 /* workers_dense_backward whose products give up a wait after limit_cycles (1..2e9; 2e9, about a second, in every other call): shows that no wait

@@ -485,6 +485,20 @@ def test_the_added_gradient_may_lie_where_the_result_goes(rows, N):
 
 
 @gpu
+@pytest.mark.parametrize("entry", PLANS + [((rows, len(rows), None, K, N), "bf16") for rows, K, N in (([5, 2], 264, 250), ([140, 60], 264, 251), ([2600], 136, 2056))], ids=plan_id)
+def test_the_residual_may_lie_where_the_result_goes(entry):
+    (rows, n_weights, weight_of, K, N), t = entry[0], TYPES[entry[1]]
+    gen = torch.Generator("cuda").manual_seed(4)
+    make = lambda *s: torch.randn(*s, generator=gen, device="cuda").to(t)
+    M = sum(rows)
+    for width in (N, N + 8 if N % 8 == 0 else N):
+        x, w, both, pre = make(M, K), make(n_weights, N, K), make(M, width)[:, :N], torch.empty(M, N, device="cuda", dtype=t)
+        apart = workers_dense_forward(x, w, rows, weight_of, residual=both.clone(), activation="gelu", pre=pre)
+        assert workers_dense_forward(x, w, rows, weight_of, residual=both, activation="gelu", y=both, pre=pre) is both
+        assert torch.equal(apart, both)
+
+
+@gpu
 def test_odd_sizes_captured_and_replayed():
     """Operands that are laid out anew: the workspace is the graph's own."""
     gen = torch.Generator("cuda").manual_seed(5)
