@@ -442,7 +442,9 @@ int32_t ps_adamw_read_info(ps_adamw* opt, ps_adamw_info* out);      /* synchroni
 
 /* The dense layer of `groups` workers, each with a mini-batch of its own length and on a weight snapshot of its own choice, forward and backward.
  * The rows of the groups lie one after another in every matrix of rows; a group may have none; rows behind the last group's are neither read nor
- * written.  BF16 or FP16 operands, FP32 accumulation, every result rounded once.  Matrices have their columns next to each other and any pitch
+ * written.  BF16 or FP16 operands, FP32 accumulation, every result rounded once.  (The tensor cores' accumulators cut what they add instead of rounding it:
+ * sums of products of one sign come out too small by up to 2.6e-6 of themselves in FP32 results, whatever their length, and in 16-bit results
+ * by a fifth of their own rounding at most; sums of both signs by a tenth of that.)  Matrices have their columns next to each other and any pitch
  * (elements from row to row) not below their width.  x, weight and dy are read by tile copies, which want a base on 16 bytes and pitches and
  * strides that are multiples of 8: others are first laid out anew in the workspace (workers_dense_workspace says how much; 0 if nothing has to be).
  * Activations are computed in FP32, of a sum z that is not rounded yet: GELU within 2^-19 + z^2 2^-22 of its value, SiLU within 2^-19 + |z| 2^-22 of its own

@@ -190,8 +190,8 @@ __global__ void __launch_bounds__(TPB) async_apply(AsyncApplyArgs a, AsyncOrder 
 }
 
 // The same with AdamW: the moments stay in registers as well, and every update has its own constants.  Measured (B200), us for 37 and 200 updates:
-// 33.4 and 156, with registers for three CTAs on an SM 31.8 and 148 (for four 33.3 and 156); their bytes at the copy rate take 21 and 102.  Two
-// special-function instructions an element (the root, the reciprocal) and their latency are what is left.
+// 33.4 and 156, with registers for three CTAs on an SM 31.8 and 148 (for four 33.3 and 156); their bytes at the copy rate take 21 and 102.  What is
+// left: the branches around every update and its stores keep the roots and reciprocals of successive updates, which depend on v alone, apart.
 __global__ void __launch_bounds__(TPB, 3) async_adamw(const __grid_constant__ AsyncApplyArgs a, const __grid_constant__ AsyncOrder ord, const __grid_constant__ AsyncAdam adam) {
   int col = blockIdx.x * TPB + threadIdx.x;
   if (col >= P_VEC4) return;

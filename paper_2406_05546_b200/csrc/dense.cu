@@ -17,11 +17,12 @@
 // Pair, Single and Thin run as many CTAs (pairs) as the SMs hold, which walk over the tiles; the others one cluster per tile.
 //
 // What bounds it, by size (us a call, cold; in brackets the library's product alone, without anything elementwise):
-//   16,384 x 4096 x 4096, BF16   the tensor pipe (80 % of its cycles; weight gradient 72 %): forward 346 (320), input gradient 349 (320), weight
-//                                gradient 381 (332), in FP32 426; with GELU's derivative, a matrix added and two results the input gradient 415,
-//                                which moves 670 MB
-//   16,384 x 1568 -> 512         what it moves: 111 MB, 37 (17 at the copy rate)
-//   41 rows on 16 of 4096 x 4096 reading the weights: 404 MB, 75, 5.4 TB/s
+//   16,384 x 4096 x 4096, BF16   the tensor pipe (80 % of its cycles; weight gradient 72 %): forward 338 (317), in FP32 392, input gradient 343 (320),
+//                                weight gradient 376 (332), in FP32 412, added to what is there 423; with GELU's derivative, a matrix added and
+//                                two results the input gradient 410, which moves 670 MB
+//   16,384 x 1568 -> 512         128 tiles on 74 pairs of SMs, two waves, and 7,700 of 52,000 clocks before the first operands: 36 (17 at the copy rate)
+//   41 rows on 16 of 4096 x 4096 reading the weights: 404 MB, 74, 5.4 TB/s
+//   8,192 x 200 -> 4999          the epilogue, two bytes a lane: with everything on 120 (38 at the copy rate), backward 159
 //   1 row, 1568 -> 512           the host's call, 5 to 7
 //
 // Precision: the accumulators drop low bits with every instruction (16 products), of each of its terms and always towards zero: of products of both signs
@@ -61,7 +62,8 @@ constexpr int BM = 128, BK = 64;
 // 64 53 -> 44, 256 57 -> 52, 384 61 -> 57, 512 65 -> 64, 768 72 -> 76; weight gradient, 16 workers of 1568 x 512 in FP32, 64 rows each 16.6 -> 13.2,
 // 300 20.6 -> 19.5, 500 24.7 -> 26.3, 8 workers of 2048 x 2048, 300 rows 30 -> 33;
 // a few larger workers among small ones (16 workers, 290 rows the most of 1,024: 23.6 -> 21.5, 480 of 930: 25.6 -> 23.6; 600 of 1,340: no gain; half with
-// 400, half with 100: 27.7 -> 31.7).  The input gradient, which reads two matrices more, has not the
+// 400, half with 100: 27.7 -> 31.7).  Results of 16 bits, half the writing, and wider ones gain less or nothing: 64 workers of 512 x 1568, 200 rows each, FP32
+// 72 -> 70, BF16 49 -> 53; 16 of 2048 x 2048, 64 rows each, 66 -> 70 and 35 -> 37.  The input gradient, which reads two matrices more, has not the
 // registers for it (64 -> 117).
 constexpr int THIN_RED_FWD = 384, THIN_RED_DW = 256, THIN_MOST_DW = 512, THIN_MEAN_DW = 128;
 constexpr int DRAIN_FP32 = 8, DRAIN_FP16 = 128, DRAIN_BF16 = 1024;      // blocks of k whose sums share an accumulator, by the result's type
@@ -69,6 +71,9 @@ constexpr int SMEM_MOST = 227 * 1024, BARRIER_BYTES = 256;
 
 template <int OP_, int CTAS_, int BN_, int STAGES_, bool SPLIT_, bool FEW_, bool DRAIN_, int PER_SM_ = 1> struct DenseShape {
   static constexpr int OP = OP_, CTAS = CTAS_, BN = BN_, STAGES = STAGES_, TM = BM * CTAS;
+  // DRAIN: the sums of a bounded part of the reduction go to registers, 128 a lane (64 for Split, which has 128 columns).  With what the epilogue reads ahead
+  // that is more than there is: 90 bytes (weight gradient) to 330 (forward, input gradient) of a thread spill.  us, 16,384 x 4096 x 4096, 16-bit result with
+  // one accumulator -> FP32: forward 338 -> 392, weight gradient 376 -> 412.
   static constexpr bool SPLIT = SPLIT_, FEW = FEW_, DRAIN = DRAIN_;
   static constexpr int PER_SM = PER_SM_;      // CTAs that an SM holds
   static constexpr bool A_MN = FEW ? OP == D_DX : OP == D_DW, B_MN = !FEW && OP != D_FWD;      // is the operand's row index contiguous?
@@ -1409,6 +1414,9 @@ int64_t cut_rows(DenseTab& tab, int tm, bool pairs, int per_block = 0) {
 int div_up(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
 // CTAs that share a tile's blocks of k: as many as the chip has room for, at least two blocks each.
+// us of captured calls, cold, with 1, 2, 4 and 8 CTAs (*: what the rule takes): 1 row 1568 -> 512 18, 14, 12*, 14; 4096 -> 4096 31, 23, 18, 20*; 4 workers of 40
+// rows 4096 -> 4096 47, 41*, 49, 64; 16 of 3 rows 107*, 115, 133, 178; 512 rows 4096 -> 1024 33, 25, 20*, 43; 1,024 33, 25*, 35, 68; weight gradient 512 x 512 of
+// 4,000 rows twice 33, 25, 20*, 43; of 2,000 rows once 23, 18, 16, 27*.
 int split_for(int64_t tiles, int blocks, int room) {
   int split = 1;
   while (split < 8 && tiles * split * 2 <= room && blocks >= split * 4) split *= 2;
@@ -1432,6 +1440,10 @@ Plan plan_rows(int op, DenseTab& tab, DenseArgs& a, const DenseEpi& epi, int fea
   a.red = red;
   a.rows = (int32_t)rows;
   const bool drain = blocks > drain_blocks(epi);      // a shorter sum takes one accumulator either way
+  // Few tiles for few rows a worker.  us of captured calls, cold, each worker on weights of its own, Few -> the other shape that there is: 4 workers
+  // 4096 -> 4096, 48 rows each 41 -> 45 (Split), 64 41 -> 45, 96 49 -> 45; 16 workers 1568 -> 512, 48 rows 20.5 -> 20.5 (Split), 96 22.5 -> 20.5.  Where Single has
+  // tiles enough for the chip it reads weights as fast: 16 workers 4096 -> 4096, 16 rows 108 -> 106, 48 115 -> 111, 96 143 -> 111; 64 workers 1024 -> 1024, 16
+  // rows 47 -> 41, 96 70 -> 43.  The mean alone is asked for: a worker with 2,000 rows beside 63 with one, 2048 -> 2048, takes 143 (Single 117).
   if (rows <= 48ll * tab.groups) {
     const int bn = most <= 16 ? 16 : (most <= 32 ? 32 : 64);
     a.n_tiles_n = div_up(features, BM);
@@ -1454,11 +1466,14 @@ Plan plan_rows(int op, DenseTab& tab, DenseArgs& a, const DenseEpi& epi, int fea
   a.n_tiles_n = div_up(features, 256);
   const int64_t row_blocks = cut_rows(tab, BM, false), pairs = cut_rows(tab, BM, true), singles = row_blocks * a.n_tiles_n;
   if (singles >= 1 << 30) return {PLAN_TOO_MANY, 1, false};
+  // Pair -> Single, us as above, 16 workers 2048 -> 2048 with so many blocks of rows each: one 45 -> 41, two 47 -> 51, three (two pairs) 65 -> 63, four 68 -> 74, five
+  // (three pairs) 86 -> 84, seven 100 -> 104.  Of one group's tiles, 4096 -> 2048: 64 pairs 37 -> 37, 80 55 -> 59.
   if (pairs * a.n_tiles_n * 2 >= sms && pairs * 10 <= row_blocks * 6) {
     a.m_tiles = (int)pairs;
     a.n_tiles = (int)pairs * a.n_tiles_n;
     return {PLAN_PAIR, 1, drain};
   }
+  // Single -> Split, 4096 -> N, single tiles: 32 33 -> 25, 48 35 -> 35, 64 35 -> 35, 80 (its 128 x 128 tiles are more than the SMs) 37 -> 59.
   a.m_tiles = (int)row_blocks;
   if (singles * 3 >= sms * 2 || row_blocks * div_up(features, 128) > sms) {
     a.n_tiles = (int)singles;
@@ -1489,6 +1504,8 @@ Plan plan_weights(DenseTab& tab, DenseArgs& a, const DenseEpi& epi, int N, int K
   a.n_tiles_n = div_up(K, 256);
   const int64_t pairs = tiles(256), singles = tiles(128);
   if (singles >= 1 << 30) return {PLAN_TOO_MANY, 1, false};
+  // Pair -> Single, us of captured calls, cold, 16 workers of 1,000 rows, K = 2048, FP32 and BF16: N = 384 47 -> 41, 43 -> 37; 512 49 -> 49, 45 -> 43; 640 63 -> 57, 55 -> 49; 896
+  // 74 -> 74, 63 -> 61.  Single -> Split, 2,000 rows, 1024 x 1024: one worker 22 -> 18, two 25 -> 25, four 27 -> 41.
   if (pairs * 2 >= sms && pairs * 2 <= singles + singles / 5) {
     a.n_tiles = (int)tiles(256);
     return {PLAN_PAIR, 1, drain};
