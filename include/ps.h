@@ -399,8 +399,8 @@ typedef struct {
   void*       copy;          /* [n] copy_type, written: the new weight rounded to nearest; NULL in every tensor = none */
   void*       m;             /* first moments, read and written: [n] float, or [n] e4m3 codes (state_bits 8) */
   void*       v;             /* second moments: [n] float, or [n] e5m2 codes */
-  uint8_t*    m_scale;       /* state_bits 8: [ceil(n / 256)] scales, element i stands for code[i] * 2^(scale[i / 256] - 127); a zero moment is */
-  uint8_t*    v_scale;       /*   code 0, with any scale.  Zeroed buffers are zero moments. */
+  uint8_t*    m_scale;       /* state_bits 8: [ceil(n / 256)] scales of 1..254, element i stands for code[i] * 2^(scale[i / 256] - 127); a zero */
+  uint8_t*    v_scale;       /*   moment is code 0.  A scale of 0 makes its block zero: zeroed buffers are zero moments. */
   double      weight_decay;  /* >= 0 */
 } ps_adamw_tensor;
 
@@ -443,8 +443,8 @@ int32_t ps_adamw_read_info(ps_adamw* opt, ps_adamw_info* out);      /* synchroni
 /* The dense layer of `groups` workers, each with a mini-batch of its own length and on a weight snapshot of its own choice, forward and backward.
  * The rows of the groups lie one after another in every matrix of rows; a group may have none; rows behind the last group's are neither read nor
  * written.  BF16 or FP16 operands, FP32 accumulation, every result rounded once.  (The tensor cores' accumulators cut what they add instead of rounding it:
- * sums of products of one sign come out too small by up to 2.6e-6 of themselves in FP32 results, whatever their length, and in 16-bit results
- * by a fifth of their own rounding at most; sums of both signs by a tenth of that.)  Matrices have their columns next to each other and any pitch
+ * sums of products of one sign come out too small by 2.6e-6 of themselves in the mean in FP32 results, whatever their length, and in 16-bit results
+ * by a fifth of the rounding to 16 bits at most; sums of both signs by a tenth of that.)  Matrices have their columns next to each other and any pitch
  * (elements from row to row) not below their width.  x, weight and dy are read by tile copies, which want a base on 16 bytes and pitches and
  * strides that are multiples of 8: others are first laid out anew in the workspace (workers_dense_workspace says how much; 0 if nothing has to be).
  * Activations are computed in FP32, of a sum z that is not rounded yet: GELU within 2^-19 + z^2 2^-22 of its value, SiLU within 2^-19 + |z| 2^-22 of its own
